@@ -314,6 +314,83 @@ tardis_status_t tardis_set_next_layer(tardis_handle_t L, tardis_handle_t next);
 tardis_status_t tardis_dense_forward(tardis_handle_t L, const void* x, int64_t n, void* y,
                                      void* stream);
 
+/* ------------------------------------------------- layers by themselves, experts */
+
+/* The products of feed-forward networks that are not folded: a linear layer with
+ * its epilogue, and the steps of a mixture of expert networks
+ *     route -> grouped product (up) -> grouped product (down) -> combine,
+ * where a token's experts are chosen by a router, the rows of all chosen (token,
+ * expert) pairs are multiplied group by group, and the results are summed onto the
+ * residual stream.  None of these calls needs a handle, allocates or
+ * synchronises; what the device alone knows (how many rows an expert has) stays on
+ * the device.  Pointers need the alignment of their elements only (rows of x and W that
+ * are whole, aligned pieces of 16 bytes are the fast case).  Sums are fp32, in
+ * an order that depends on the sizes alone: results are the same bits in every
+ * run.  A call with no rows is TARDIS_OK and does nothing. */
+typedef struct {
+    int64_t n_in;        /* 1 .. 2^22 */
+    int64_t n_out;       /* 1 .. 2^22 */
+    int32_t dtype;       /* tardis_dtype_t of x, W and b: TARDIS_F32 or TARDIS_BF16 */
+    int32_t out_dtype;   /* of the residual and of y: TARDIS_F32 or TARDIS_BF16 */
+    int32_t act;         /* tardis_act_t */
+    int32_t reserved;    /* 0 */
+    const void* W;       /* n_out x n_in row-major; of a grouped product experts x n_out x n_in */
+    const void* b;       /* n_out (experts x n_out), or NULL for zero */
+} tardis_linear_desc;
+
+/* y = sigma(x W^T + b) + residual, rounded once.
+ *   x         n rows of n_in values, x_pitch >= n_in values apart.
+ *   residual  n x n_out, out_dtype, or NULL; may be y itself.
+ *   y         n x n_out, out_dtype; must not overlap x, W or b.
+ *   work      device memory for sums of ranges of n_in, at least 4-byte aligned; its
+ *             content is not used again.  tardis_linear_workspace says how much the
+ *             call can use (0 for most); with less, or NULL, n_in is not divided
+ *             and a product of few rows and columns takes longer. */
+tardis_status_t tardis_linear(const tardis_linear_desc* desc, const void* x, int64_t n, int64_t x_pitch,
+                              const void* residual, void* y, void* work, int64_t work_bytes, void* stream);
+tardis_status_t tardis_linear_workspace(const tardis_linear_desc* desc, int64_t n, int64_t* bytes);
+
+/* Rows by groups: positions offsets[e] <= p < offsets[e+1] have the weights of
+ * expert e,
+ *     y[p] = sigma(x[row(p)] W_e^T + b_e),
+ * row(p) = order[p] / per_token where there is an order (the slots of the tokens'
+ * choices sorted by expert, as tardis_moe_route gives them, so that the rows of the
+ * experts are read from the tokens), else p.
+ *   experts    1 .. 65536.   offsets  experts + 1 ints, ascending, device memory;
+ *              values outside of 0 .. positions count as the nearest of the two.
+ *   order      positions ints, or NULL.  A row of y whose order is no slot of a token
+ *              (negative, or row(p) >= x_rows), or whose position is in no group, is left
+ *              as it is.
+ *   x          x_rows rows, x_pitch >= n_in values apart (without an order: positions of them).
+ *   y          positions x n_out, out_dtype. */
+tardis_status_t tardis_grouped_linear(const tardis_linear_desc* desc, int64_t experts, const void* x, int64_t x_rows,
+                                      int64_t x_pitch, const int32_t* offsets, const int32_t* order,
+                                      int64_t per_token, int64_t positions, void* y, void* stream);
+
+/* The k experts of every token: those of its largest logits, the lower index first
+ * among equal ones; weights are the softmax over the chosen ones (renormalise = 1) or over all
+ * experts of the token (0).  A logit of minus infinity, or a NaN, is an expert that is not there:
+ * a token with fewer than k others has ids of -1 and weights of 0 behind them.
+ *   logits   n x experts, TARDIS_F32 or TARDIS_BF16.   1 <= experts <= 1024, 1 <= k <= 16, k <= experts.
+ *   ids      n x k ints, from the largest logit down.   weights  n x k floats.
+ *   offsets  experts + 1 ints: the chosen slots (token k + place) sorted by expert, stable;
+ *            expert e has positions offsets[e] .. offsets[e+1].
+ *   order    n k ints: the slot at a position; -1 behind the last.
+ *   place    n x k ints: the position of a slot, or -1.
+ *   work     tardis_moe_route_workspace bytes (0: may be NULL), 4-byte aligned. */
+tardis_status_t tardis_moe_route(const void* logits, int64_t n, int64_t experts, int64_t k, int32_t dtype,
+                                 int32_t renormalise, int32_t* ids, float* weights, int32_t* offsets, int32_t* order,
+                                 int32_t* place, void* work, int64_t work_bytes, void* stream);
+tardis_status_t tardis_moe_route_workspace(int64_t n, int64_t experts, int64_t* bytes);
+
+/* y[t] = residual[t] + sum_j weights[t][j] z[place[t][j]] over the k slots of a token, in
+ * this order, rounded once; a place outside of 0 .. rows - 1 is a dropped slot.
+ *   z         rows x d, dtype.   place, weights  n x k.   1 <= k <= 1024.
+ *   residual  n x d, out_dtype, or NULL; may be y itself.   y  n x d, out_dtype. */
+tardis_status_t tardis_moe_combine(const void* z, int64_t rows, const int32_t* place, const float* weights, int64_t n,
+                                   int64_t k, int64_t d, int32_t dtype, const void* residual, void* y,
+                                   int32_t out_dtype, void* stream);
+
 /* ------------------------------------------------------------- inspection */
 
 /* Copies of the folded state (stream-ordered).  Wp: d x d in desc dtype; bp: d

@@ -15,6 +15,9 @@ constexpr int64_t kMaxH = 1 << 22;
 constexpr int64_t kMaxCal = 32768;        // one neuron's samples are sorted in LDS
 constexpr int64_t kMaxSearchCal = 8192;   // range search also keeps sigma of every sample there, in fp64
 constexpr int64_t kMaxBatch = 4096;
+constexpr int64_t kMaxWidth = 1 << 22, kMaxPitch = (int64_t)1 << 30;   // linear layers
+constexpr int64_t kMaxRows = (int64_t)1 << 30;
+constexpr int64_t kMaxExperts = 1024, kMaxChosen = 16;   // the router: an expert for a thread of a block, a choice for a lane of 16
 // 4-bit layers folded for at most this many tokens, and for fewer than run as products, keep the packed sketch alone.  More
 // tokens are groups of 8 and 16, which read one-byte codes (blocks of 1024 threads), and were groups of 4 and 2 without them; us at
 // d = 4096, h = 16384, 1 / 5 / 15 % fallback, packed alone and with codes (67 MB more for the layer): 5 tokens 79 / 92 / 115 and
@@ -544,6 +547,87 @@ tardis_status_t tardis_get_handover(tardis_handle_t L, int64_t n, void* out, voi
     TD_HIP(hipMemcpyAsync(out, L->xnext, (size_t)n * L->d * td_elem_size(L->dtype), hipMemcpyDeviceToDevice,
                           static_cast<hipStream_t>(stream)));
     return TARDIS_OK;
+}
+
+namespace {
+
+bool linear_dtype(int32_t t) { return t == TARDIS_F32 || t == TARDIS_BF16; }
+bool aligned_to(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+tardis_status_t check_linear(const tardis_linear_desc* d) {
+    if (!d || !d->W || d->reserved != 0) return TARDIS_ERR_INVALID_ARG;
+    if (!linear_dtype(d->dtype) || !linear_dtype(d->out_dtype)) return TARDIS_ERR_DTYPE;
+    if (d->act < TARDIS_ACT_GELU_ERF || d->act > TARDIS_ACT_IDENTITY) return TARDIS_ERR_INVALID_ARG;
+    if (d->n_in < 1 || d->n_out < 1 || d->n_in > kMaxWidth || d->n_out > kMaxWidth) return TARDIS_ERR_SHAPE;
+    const size_t es = td_elem_size(d->dtype);
+    return aligned_to(d->W, es) && aligned_to(d->b, es) ? TARDIS_OK : TARDIS_ERR_INVALID_ARG;
+}
+bool rows_fit(int64_t rows, int64_t pitch) { return rows >= 0 && rows <= kMaxRows && pitch <= kMaxPitch; }
+
+}  // namespace
+
+tardis_status_t tardis_linear_workspace(const tardis_linear_desc* desc, int64_t n, int64_t* bytes) {
+    TD_TRY(check_linear(desc));
+    if (!bytes) return TARDIS_ERR_INVALID_ARG;
+    if (!rows_fit(n, 0)) return TARDIS_ERR_SHAPE;
+    *bytes = n > 0 ? (int64_t)td_linear_work_bytes(desc, n) : 0;
+    return TARDIS_OK;
+}
+
+tardis_status_t tardis_linear(const tardis_linear_desc* desc, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y,
+                              void* work, int64_t work_bytes, void* stream) {
+    TD_TRY(check_linear(desc));
+    if (!rows_fit(n, x_pitch) || x_pitch < desc->n_in) return TARDIS_ERR_SHAPE;
+    if (n == 0) return TARDIS_OK;
+    const size_t es = td_elem_size(desc->dtype), eo = td_elem_size(desc->out_dtype);
+    if (!x || !y || !aligned_to(x, es) || !aligned_to(y, eo) || !aligned_to(residual, eo) || !aligned_to(work, 4) || work_bytes < 0) return TARDIS_ERR_INVALID_ARG;
+    return td_linear(desc, x, n, x_pitch, residual, y, work, work ? work_bytes : 0, static_cast<hipStream_t>(stream));
+}
+
+tardis_status_t tardis_grouped_linear(const tardis_linear_desc* desc, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch,
+                                      const int32_t* offsets, const int32_t* order, int64_t per_token, int64_t positions, void* y, void* stream) {
+    TD_TRY(check_linear(desc));
+    if (experts < 1 || experts > 65536 || !rows_fit(x_rows, x_pitch) || x_pitch < desc->n_in || !rows_fit(positions, 0)) return TARDIS_ERR_SHAPE;
+    if (order ? per_token < 1 || per_token > kMaxRows : x_rows < positions) return TARDIS_ERR_SHAPE;
+    if (positions == 0) return TARDIS_OK;
+    if (!offsets || !aligned_to(offsets, 4) || !aligned_to(order, 4)) return TARDIS_ERR_INVALID_ARG;
+    if (x_rows == 0) return TARDIS_OK;                   // (no slot is one of a token)
+    const size_t es = td_elem_size(desc->dtype), eo = td_elem_size(desc->out_dtype);
+    if (!x || !y || !aligned_to(x, es) || !aligned_to(y, eo)) return TARDIS_ERR_INVALID_ARG;
+    return td_grouped_linear(desc, experts, x, x_rows, x_pitch, offsets, order, order ? per_token : 1, positions, y, static_cast<hipStream_t>(stream));
+}
+
+tardis_status_t tardis_moe_route_workspace(int64_t n, int64_t experts, int64_t* bytes) {
+    if (!bytes) return TARDIS_ERR_INVALID_ARG;
+    if (!rows_fit(n, 0) || experts < 1 || experts > kMaxExperts) return TARDIS_ERR_SHAPE;
+    *bytes = n > 0 ? (int64_t)td_route_work_bytes(n, experts) : 0;
+    return TARDIS_OK;
+}
+
+tardis_status_t tardis_moe_route(const void* logits, int64_t n, int64_t experts, int64_t k, int32_t dtype, int32_t renormalise, int32_t* ids,
+                                 float* weights, int32_t* offsets, int32_t* order, int32_t* place, void* work, int64_t work_bytes, void* stream) {
+    if (!linear_dtype(dtype)) return TARDIS_ERR_DTYPE;
+    if (experts < 1 || experts > kMaxExperts || k < 1 || k > kMaxChosen || k > experts || !rows_fit(n, 0) || n * k > kMaxRows) return TARDIS_ERR_SHAPE;
+    if (renormalise != 0 && renormalise != 1) return TARDIS_ERR_INVALID_ARG;
+    if (!offsets || !aligned_to(offsets, 4)) return TARDIS_ERR_INVALID_ARG;
+    if (n > 0 && (!logits || !ids || !weights || !order || !place)) return TARDIS_ERR_INVALID_ARG;
+    if (!aligned_to(logits, td_elem_size(dtype)) || !aligned_to(ids, 4) || !aligned_to(weights, 4) || !aligned_to(order, 4) || !aligned_to(place, 4) ||
+        !aligned_to(work, 4))
+        return TARDIS_ERR_INVALID_ARG;
+    if (n > 0 && td_route_work_bytes(n, experts) > 0 && (!work || work_bytes < (int64_t)td_route_work_bytes(n, experts))) return TARDIS_ERR_INVALID_ARG;
+    return td_moe_route(logits, n, experts, k, dtype, renormalise, ids, weights, offsets, order, place, work, static_cast<hipStream_t>(stream));
+}
+
+tardis_status_t tardis_moe_combine(const void* z, int64_t rows, const int32_t* place, const float* weights, int64_t n, int64_t k, int64_t d,
+                                   int32_t dtype, const void* residual, void* y, int32_t out_dtype, void* stream) {
+    if (!linear_dtype(dtype) || !linear_dtype(out_dtype)) return TARDIS_ERR_DTYPE;
+    if (!rows_fit(rows, 0) || !rows_fit(n, 0) || k < 1 || k > 1024 || d < 1 || d > kMaxWidth) return TARDIS_ERR_SHAPE;
+    if (n == 0) return TARDIS_OK;
+    const size_t es = td_elem_size(dtype), eo = td_elem_size(out_dtype);
+    if (!place || !weights || !y || (rows > 0 && !z) || !aligned_to(z, es) || !aligned_to(place, 4) || !aligned_to(weights, 4) ||
+        !aligned_to(residual, eo) || !aligned_to(y, eo))
+        return TARDIS_ERR_INVALID_ARG;
+    return td_moe_combine(z, rows, place, weights, n, k, d, dtype, residual, y, out_dtype, static_cast<hipStream_t>(stream));
 }
 
 tardis_status_t tardis_destroy(tardis_handle_t L) {

@@ -1,0 +1,512 @@
+// y = sigma(x W^T + b) + r for one weight matrix, or for one of several by groups of rows (mixture of experts): the kernel, for one
+// element type of x, W and b (linear_bf16.hip, linear_f32.hip); which tile a call takes is linear.hip's.
+#pragma once
+#include "linear.h"
+#include "sigma.h"
+#include "tiles.h"
+
+namespace {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+// 16 bytes at any element's address
+typedef uint32_t u32x4_any_t __attribute__((ext_vector_type(4), aligned(2)));
+
+__device__ __forceinline__ td_u32x4 load_any16(const void* p) { return *static_cast<const u32x4_any_t*>(p); }
+__device__ __forceinline__ void store_any16(void* p, const td_u32x4& v) { *static_cast<u32x4_any_t*>(p) = v; }
+
+// One 16 x 16 block of sums: w, x hold 16 bytes of row lane % 16 at piece lane / 16 of 64 bytes of K.  (fp32: element q of all four
+// pieces in one instruction, so K is summed in another order, the same for both operands.)
+template <typename T> __device__ __forceinline__ void mma_pieces(f32x4_t& c, const td_u32x4& w, const td_u32x4& x);
+template <> __device__ __forceinline__ void mma_pieces<bf16_t>(f32x4_t& c, const td_u32x4& w, const td_u32x4& x) {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w), __builtin_bit_cast(bf16x8_t, x), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ void mma_pieces<float>(f32x4_t& c, const td_u32x4& w, const td_u32x4& x) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[q]), __uint_as_float(x[q]), c, 0, 0, 0);
+}
+
+// n / d for n < 2^21
+__device__ __forceinline__ uint32_t divide(uint32_t n, uint32_t d, uint32_t& rest) {
+    uint32_t q = (uint32_t)((float)n * __builtin_amdgcn_rcpf((float)d));
+    int r = (int)(n - q * d);
+    if (r < 0) { --q; r += (int)d; }
+    if (r >= (int)d) { ++q; r -= (int)d; }
+    rest = (uint32_t)r;
+    return q;
+}
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Tile number t of a tiles_m x tiles_n grid: eight tile rows are walked together, column by column, so that the blocks an XCD runs at
+// once cover a patch and share the slices of both operands in its L2.
+__device__ __forceinline__ void tile_of(uint32_t t, uint32_t tiles_m, uint32_t tiles_n, int& tile_m, int& tile_n) {
+    uint32_t in_walk, row;
+    const uint32_t walk = divide(t, 8 * tiles_n, in_walk) * 8, rows = min(8u, tiles_m - walk);
+    tile_n = uniform((int)divide(in_walk, rows, row));
+    tile_m = uniform((int)(walk + row));
+}
+
+// What a block computes: rows [first, first + rows) of C, columns from n0 on, slices [s0, s0 + nk) of K, with the weights of `expert`
+struct LinearBlock {
+    int64_t first, n0;
+    int rows, expert, s0, nk, range;
+};
+
+// Number `t` of `all` tiles for block b: an XCD (blocks b, b + 8, ...) has consecutive ones.  false: none
+__device__ __forceinline__ bool number_of(uint32_t block, uint32_t all, uint32_t& t) {
+    const uint32_t per = (all + 7) / 8, local = block >> 3;
+    t = (block & 7) * per + local;
+    return local < per && t < all;
+}
+
+// inclusive sums over the lanes
+__device__ __forceinline__ int wave_scan(int v, int lane) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(v, o, 64);
+        v += lane >= o ? u : 0;
+    }
+    return v;
+}
+
+// Which group's tile this block has: the rows of a group are known on the device alone, so every wavefront adds up the groups' tiles
+// (a lane has a group) and looks for its own number.  Offsets outside of 0 .. n count as the nearest of the two.
+template <int TM> __device__ __forceinline__ bool find_group(const LinearArgs& p, int lane, LinearBlock& b, int& tile_n) {
+    const int positions = (int)p.n;
+    auto group = [&](int e, int& from) {
+        from = e < p.experts ? min(max(p.offsets[e], 0), positions) : 0;
+        const int to = e < p.experts ? min(max(p.offsets[e + 1], 0), positions) : 0;
+        return max(to - from, 0);
+    };
+    int from0;
+    const int rows0 = group(lane, from0), sum0 = wave_scan((rows0 + TM - 1) / TM, lane);
+    uint32_t all = (uint32_t)__builtin_amdgcn_readlane(sum0, 63);
+    for (int c = 64; c < p.experts; c += 64) {
+        int from;
+        const int rows = group(c + lane, from);
+        all += (uint32_t)__builtin_amdgcn_readlane(wave_scan((rows + TM - 1) / TM, lane), 63);
+    }
+    uint32_t t;
+    if (!number_of(blockIdx.x, all * (uint32_t)p.tiles_n, t)) return false;
+    uint32_t before = 0;                              // tiles of the groups before the 64 that are looked at
+    for (int c = 0; c < p.experts; c += 64) {
+        int from = from0, rows = rows0, sum = sum0;
+        if (c > 0) {
+            rows = group(c + lane, from);
+            sum = wave_scan((rows + TM - 1) / TM, lane);
+        }
+        const uint64_t past = __ballot((before + (uint32_t)sum) * (uint32_t)p.tiles_n > t);
+        if (past) {
+            const int at = __builtin_ctzll(past);
+            from = __builtin_amdgcn_readlane(from, at);
+            rows = __builtin_amdgcn_readlane(rows, at);
+            const int tiles = (rows + TM - 1) / TM;
+            const uint32_t mine = before + (uint32_t)__builtin_amdgcn_readlane(sum, at) - (uint32_t)tiles;
+            int tile_m;
+            tile_of(t - mine * (uint32_t)p.tiles_n, (uint32_t)tiles, (uint32_t)p.tiles_n, tile_m, tile_n);
+            b.expert = c + at;
+            b.first = from + (int64_t)tile_m * TM;
+            b.rows = min(TM, rows - tile_m * TM);
+            return true;
+        }
+        before += (uint32_t)__builtin_amdgcn_readlane(sum, 63);
+    }
+    return false;
+}
+
+// The tile of a block: TM = 16 FA WM rows (tokens) x TN = 16 FB WN columns (rows of W), 8 wavefronts in a grid of WM x WN, times WK that
+// divide K: a slice is 64 WK bytes of every row, of which a wavefront multiplies 64, and every fragment of a slice is
+// read from LDS by WN (of W: WM) wavefronts only.  D slices are in LDS.
+template <typename T, bool DIRECT, int FA, int FB, int WM, int WN, int WK, int D>
+struct LinearTile {
+    static constexpr int TM = 16 * FA * WM, TN = 16 * FB * WN, SL = 64 * WK;
+    static constexpr int UA = TM * SL, UB = TN * SL, LA = UA / 8192, LB = UB / 8192;    // bytes of a slice, loads (16 bytes a lane) of a wavefront
+    static constexpr int kRing = D * (UA + UB);
+    // row blocks of a wavefront that pass through LDS at a time behind the products: as many as the ring has room for
+    static constexpr int kRowBytes = WK * WM * 16 * TN * 4;
+    static constexpr int fit(int n) { return n == 1 || (FA % n == 0 && n * kRowBytes <= kRing) ? n : fit(n - 1); }
+    static constexpr int RB = fit(FA), kLds = RB * kRowBytes > kRing ? RB * kRowBytes : kRing;
+    static_assert(WM * WN * WK == 8 && UA % 8192 == 0 && UB % 8192 == 0 && kLds <= kLdsBytes, "eight wavefronts, whole loads");
+    static_assert(DIRECT ? D >= 3 && (D - 1) * (LA + LB) <= 63 : D == 2, "slices in LDS");
+};
+
+// What bounds it: few rows - the weights' stream from HBM; many - the way from L2 to LDS (tiles below 192 x 128) and the matrix cores.
+// DIRECT: x and W in whole, aligned pieces of 16 bytes, which go from memory straight to LDS; D - 1 slices are under way.  Else (odd
+// widths, odd pitches, rows that are 4 GB apart): through registers, two slices ahead, whatever the alignment.
+template <typename T, bool GROUPED, bool DIRECT, int FA, int FB, int WM, int WN, int WK, int D>
+__global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
+    typedef LinearTile<T, DIRECT, FA, FB, WM, WN, WK, D> G;
+    constexpr int TM = G::TM, TN = G::TN, SL = G::SL, LA = G::LA, LB = G::LB, PS = SL / 16, RPL = 64 / PS, SWZ = PS < 16 ? PS - 1 : 15;
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
+    const int wk = wave % WK, wn = wave / WK % WN, wm = wave / WK / WN, frow = lane & 15, fp = lane >> 4;
+
+    LinearBlock b;
+    int tile_n;
+    const int slices = (int)((p.k + SL - 1) / SL);
+    if constexpr (GROUPED) {
+        if (!find_group<TM>(p, lane, b, tile_n)) return;
+        b.s0 = b.range = 0;
+        b.nk = slices;
+    } else {
+        uint32_t t, in_range;
+        if (!number_of(blockIdx.x, (uint32_t)(p.tiles_m * p.tiles_n * p.splits), t)) return;
+        int tile_m;
+        b.range = uniform((int)divide(t, (uint32_t)(p.tiles_m * p.tiles_n), in_range));
+        tile_of(in_range, (uint32_t)p.tiles_m, (uint32_t)p.tiles_n, tile_m, tile_n);
+        b.expert = 0;
+        b.first = (int64_t)tile_m * TM;
+        b.rows = (int)min((int64_t)TM, p.n - b.first);
+        b.s0 = b.range * p.slices;
+        b.nk = max(0, min(p.slices, slices - b.s0));
+    }
+    b.n0 = (int64_t)tile_n * TN;
+    const int rows_w = (int)min((int64_t)TN, p.N - b.n0);
+    const unsigned char* W = p.W + ((size_t)b.expert * p.N + b.n0) * p.k;
+    // whole slices from a starting point of this block's own, then one that is not whole
+    const int whole = max(0, min(b.nk, (int)(p.k / SL) - b.s0));
+    const int rot = first_slice((int)blockIdx.x & 7, (int)blockIdx.x >> 3, whole);
+    auto slice_of = [&](int t) { return b.s0 + (t >= whole ? t : t + rot >= whole ? t + rot - whole : t + rot); };
+
+    // A load is RPL rows x SL bytes: lane -> row lane / PS, slot lane % PS, which holds piece slot ^ row (so the 16 rows of a fragment
+    // hit all banks).  Wavefront w loads rows [w TM / 8, (w + 1) TM / 8) of x, of W alike.
+    const int row_a = wave * (TM / 8) + lane / PS, row_b = wave * (TN / 8) + lane / PS;
+    auto piece_of_row = [&](int row) { return (uint32_t)((lane % PS) ^ (row & SWZ)) * 16u; };
+    // the row of x that is row m of this block's; -1: none
+    auto token_of = [&](int m) -> int64_t {
+        if (m >= b.rows) return -1;
+        if (!GROUPED || !p.order) return b.first + m;
+        const uint32_t slot = (uint32_t)p.order[b.first + m];
+        uint32_t token = __umulhi(slot, p.inv_per_token);   // the quotient, or one less
+        if (slot - token * (uint32_t)p.per_token >= (uint32_t)p.per_token) ++token;
+        return (int64_t)token < p.x_rows ? (int64_t)token : -1;   // (a negative slot is a large token)
+    };
+
+    f32x4_t acc[FA][FB];
+#pragma unroll
+    for (int i = 0; i < FA; ++i)
+#pragma unroll
+        for (int j = 0; j < FB; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
+    // fragments: lane holds 16 bytes of row lane % 16 at piece 4 wk + lane / 16 of a slice
+    const uint32_t frag = (uint32_t)(frow * SL + (((4 * wk + fp) ^ (frow & SWZ)) * 16));
+    struct Fragments {
+        td_u32x4 a[FA], b[FB];
+    };
+    auto read = [&](Fragments& f, const unsigned char* at_a, const unsigned char* at_b) {
+#pragma unroll
+        for (int i = 0; i < FA; ++i) f.a[i] = *reinterpret_cast<const td_u32x4*>(at_a + (wm * FA + i) * (16 * SL) + frag);
+#pragma unroll
+        for (int j = 0; j < FB; ++j) f.b[j] = *reinterpret_cast<const td_u32x4*>(at_b + (wn * FB + j) * (16 * SL) + frag);
+    };
+    auto multiply = [&](const Fragments& f) {
+#pragma unroll
+        for (int i = 0; i < FA; ++i)
+#pragma unroll
+            for (int j = 0; j < FB; ++j) mma_pieces<T>(acc[i][j], f.b[j], f.a[i]);
+    };
+
+    if constexpr (DIRECT) {
+        const uint32_t base = (uint32_t)uniform((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds);
+        const bool gather = GROUPED && p.order;
+        // (p.x_bytes: up to the last row's end; offsets of rows that are not there lie past it, where nothing is fetched)
+        const i32x4_t ra = gather ? buffer_of(p.x, (uint32_t)p.x_bytes)
+                                  : buffer_of(p.x + b.first * p.x_pitch, (uint32_t)((b.rows - 1) * p.x_pitch) + p.k);
+        const i32x4_t rb = buffer_of(W, (uint32_t)rows_w * p.k);
+        uint32_t off_a[LA], off_b[LB];
+#pragma unroll
+        for (int i = 0; i < LA; ++i) {
+            const int row = row_a + i * RPL;
+            uint32_t at;
+            if (gather) {
+                const int64_t token = token_of(row);
+                at = token < 0 ? kNowhere : (uint32_t)token * (uint32_t)p.x_pitch;
+            } else {
+                at = row < b.rows ? (uint32_t)row * (uint32_t)p.x_pitch : kNowhere;
+            }
+            off_a[i] = at + piece_of_row(row);
+        }
+#pragma unroll
+        for (int i = 0; i < LB; ++i) {
+            const int row = row_b + i * RPL;
+            off_b[i] = (row < rows_w ? (uint32_t)row * p.k : kNowhere) + piece_of_row(row);
+        }
+#pragma unroll
+        for (int i = 0; i < LA; ++i) asm volatile("" : "+v"(off_a[i]));   // (waited for here, not between the loads below)
+        const uint32_t to_a = base + (uint32_t)wave * (G::UA / 8), to_b = base + (uint32_t)(D * G::UA) + (uint32_t)wave * (G::UB / 8);
+        auto load_slice = [&](int t, uint32_t slot) {     // (past the last slice: an empty buffer)
+            const bool live = t < b.nk;
+            const uint32_t soff = live ? (uint32_t)slice_of(t) * SL : 0u;
+            i32x4_t a = ra, w = rb;
+            a.z = live ? a.z : 0;
+            w.z = live ? w.z : 0;
+            const uint32_t last = p.k - soff;             // bytes of the row from here on
+            if (live && last < (uint32_t)SL) {            // the pieces that the row has not: its first one of this slice
+#pragma unroll
+                for (int i = 0; i < LB; ++i) {
+                    const uint32_t pc = piece_of_row(row_b + i * RPL);
+                    load_to_lds(to_b + slot * G::UB + i * 1024u, off_b[i] - (pc < last ? 0u : pc), w, soff);
+                }
+#pragma unroll
+                for (int i = 0; i < LA; ++i) {
+                    const uint32_t pc = piece_of_row(row_a + i * RPL);
+                    load_to_lds(to_a + slot * G::UA + i * 1024u, off_a[i] - (pc < last ? 0u : pc), a, soff);
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < LB; ++i) load_to_lds(to_b + slot * G::UB + i * 1024u, off_b[i], w, soff);
+#pragma unroll
+                for (int i = 0; i < LA; ++i) load_to_lds(to_a + slot * G::UA + i * 1024u, off_a[i], a, soff);
+            }
+        };
+        auto arrived = [&](auto behind) {                 // all but the newest D - behind slices; the barrier makes it everybody's
+            __builtin_amdgcn_s_waitcnt(0xc07f);           // lgkmcnt(0): the fragments read before are in registers
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - decltype(behind)::value) * (LA + LB)) : "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+#pragma unroll 1
+        for (int s = 0; s < D; ++s) load_slice(s, (uint32_t)s);
+        uint32_t slot = 0;                                // of the slice that is read next
+        auto fetch = [&](Fragments& f, int t) {
+            read(f, lds + slot * G::UA, lds + D * G::UA + slot * G::UB);
+            if (t >= whole) {                             // a slice that is not whole: what the row has not is zero
+                const uint32_t at = (uint32_t)slice_of(t) * SL + (uint32_t)(4 * wk + fp) * 16u;
+                const td_u32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < FA; ++i) f.a[i] = at < p.k ? f.a[i] : zero;
+#pragma unroll
+                for (int j = 0; j < FB; ++j) f.b[j] = at < p.k ? f.b[j] : zero;
+            }
+        };
+        Fragments f[2];
+        auto step = [&](const Fragments& now, Fragments& next, int t) {
+            arrived(num<2>{});                            // slice t + 1 is here, and slice t's place is free
+            const uint32_t free = slot;
+            slot = slot + 1 == D ? 0 : slot + 1;
+            load_slice(t + D, free);
+            if (t + 1 < b.nk) fetch(next, t + 1);
+            multiply(now);
+        };
+        if (b.nk > 0) {
+            arrived(num<1>{});
+            fetch(f[0], 0);
+        }
+#pragma unroll 1
+        for (int t = 0; t < b.nk; t += 2) {
+            step(f[0], f[1], t);
+            if (t + 1 < b.nk) step(f[1], f[0], t + 1);
+        }
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    } else {
+        const unsigned char *from_a[LA], *from_b[LB];     // (rows that are not there: null)
+#pragma unroll
+        for (int i = 0; i < LA; ++i) {
+            const int64_t token = token_of(row_a + i * RPL);
+            from_a[i] = token < 0 ? nullptr : p.x + token * p.x_pitch + piece_of_row(row_a + i * RPL);
+        }
+#pragma unroll
+        for (int i = 0; i < LB; ++i) {
+            const int row = row_b + i * RPL;
+            from_b[i] = row < rows_w ? W + (size_t)row * p.k + piece_of_row(row) : nullptr;
+        }
+        struct Pieces {
+            td_u32x4 a[LA], b[LB];
+        };
+        auto load_piece = [&](const unsigned char* from, uint32_t soff, uint32_t pc) {
+            const td_u32x4 zero = {0, 0, 0, 0};
+            if (!from || soff + pc >= p.k) return zero;
+            if (soff + pc + 16 <= p.k) return load_any16(from + soff);
+            td_u32x4 v = zero;                            // the row's last elements
+            const T* el = reinterpret_cast<const T*>(from + soff);
+            const uint32_t n = (p.k - soff - pc) / sizeof(T);
+#pragma unroll
+            for (uint32_t u = 0; u < 16 / sizeof(T); ++u)
+                if (u < n) {
+                    if constexpr (sizeof(T) == 2) v[u / 2] |= (uint32_t)el[u] << (16 * (u & 1));
+                    else v[u] = __float_as_uint(el[u]);
+                }
+            return v;
+        };
+        auto load_slice = [&](Pieces& v, int t) {
+            if (t >= b.nk) return;
+            const uint32_t soff = (uint32_t)slice_of(t) * SL;
+            if (t < whole) {
+                const td_u32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+                for (int i = 0; i < LB; ++i) v.b[i] = from_b[i] ? load_any16(from_b[i] + soff) : zero;
+#pragma unroll
+                for (int i = 0; i < LA; ++i) v.a[i] = from_a[i] ? load_any16(from_a[i] + soff) : zero;
+            } else {
+#pragma unroll
+                for (int i = 0; i < LB; ++i) v.b[i] = load_piece(from_b[i], soff, piece_of_row(row_b + i * RPL));
+#pragma unroll
+                for (int i = 0; i < LA; ++i) v.a[i] = load_piece(from_a[i], soff, piece_of_row(row_a + i * RPL));
+            }
+        };
+        Pieces v[2];
+        auto step = [&](Pieces& now, int t) {             // (the place in LDS was read two slices ago, before the last barrier)
+            unsigned char* at_a = lds + (t & 1) * G::UA;
+            unsigned char* at_b = lds + 2 * G::UA + (t & 1) * G::UB;
+#pragma unroll
+            for (int i = 0; i < LA; ++i) *reinterpret_cast<td_u32x4*>(at_a + wave * (G::UA / 8) + i * 1024 + lane * 16) = now.a[i];
+#pragma unroll
+            for (int i = 0; i < LB; ++i) *reinterpret_cast<td_u32x4*>(at_b + wave * (G::UB / 8) + i * 1024 + lane * 16) = now.b[i];
+            __syncthreads();
+            load_slice(now, t + 2);
+            Fragments f;
+            read(f, at_a, at_b);
+            multiply(f);
+        };
+        load_slice(v[0], 0);
+        load_slice(v[1], 1);
+#pragma unroll 1
+        for (int t = 0; t < b.nk; t += 2) {
+            step(v[0], t);
+            if (t + 1 < b.nk) step(v[1], t + 1);
+        }
+    }
+    __syncthreads();
+
+    // acc[i][j][q] = row (wm FA + i) 16 + lane % 16, column (wn FB + j) 16 + 4 (lane / 16) + q of the tile.  The parts of K meet in LDS, some
+    // row blocks at a time; a thread finishes 8 neighbouring columns at once.
+    constexpr int RB = G::RB, UNITS = TN / 8, STRIDE = 512 / UNITS;
+    float* stage = reinterpret_cast<float*>(lds);
+    auto place_of = [&](int part, int row, int piece) { return (part * (WM * RB * 16) + row) * TN + ((piece ^ (row & 15 & (TN / 4 - 1))) * 4); };
+    const int unit = tid % UNITS;
+    const int64_t n = b.n0 + unit * 8;
+    const int columns = (int)min((int64_t)8, p.N - n);    // (of this thread; none or less: none)
+    auto load8 = [&](const void* from, int64_t at, bool f32, float (&v)[8]) {
+        if (columns >= 8) {
+            if (f32) {
+                const td_u32x4 lo = load_any16(static_cast<const float*>(from) + at), hi = load_any16(static_cast<const float*>(from) + at + 4);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    v[q] = __uint_as_float(lo[q]);
+                    v[4 + q] = __uint_as_float(hi[q]);
+                }
+            } else {
+                const td_u32x4 w = load_any16(static_cast<const bf16_t*>(from) + at);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    v[2 * q] = __uint_as_float(w[q] << 16);
+                    v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                v[q] = q >= columns ? 0.0f : f32 ? static_cast<const float*>(from)[at + q] : td_bf16_to_f32(static_cast<const bf16_t*>(from)[at + q]);
+        }
+    };
+    float bias[8] = {};
+    if (p.b && !p.part && columns > 0) load8(p.b, (int64_t)b.expert * p.N + n, sizeof(T) == 4, bias);
+    for_constants<FA / RB>([&](auto batch) {
+        constexpr int i0 = decltype(batch)::value * RB;
+        if constexpr (i0 > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+            for (int j = 0; j < FB; ++j)
+                *reinterpret_cast<f32x4_t*>(stage + place_of(wk, (wm * RB + i) * 16 + frow, (wn * FB + j) * 4 + fp)) = acc[i0 + i][j];
+        __syncthreads();
+        with_act(p.act, [&](auto act) {
+#pragma unroll 1
+            for (int at = tid / UNITS; at < WM * RB * 16; at += STRIDE) {
+                const int m = (at / (RB * 16) * FA + i0) * 16 + at % (RB * 16);       // row of the tile
+                if (m >= b.rows || columns <= 0) continue;
+                if (GROUPED && p.order && token_of(m) < 0) continue;
+                const int64_t row = b.first + m, to = row * p.N + n;
+                float r[8] = {}, v[8];
+                if (p.r && !p.part) load8(p.r, to, p.out_f32, r);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    f32x4_t sum = *reinterpret_cast<const f32x4_t*>(stage + place_of(0, at, unit * 2 + h));
+#pragma unroll
+                    for (int part = 1; part < WK; ++part) sum += *reinterpret_cast<const f32x4_t*>(stage + place_of(part, at, unit * 2 + h));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[4 * h + q] = sum[q];
+                }
+                if (!p.part) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) v[q] = act_flat<decltype(act)::value>(v[q] + bias[q]) + r[q];
+                }
+                if (p.part || p.out_f32) {
+                    float* y = p.part ? p.part + (int64_t)b.range * p.n * p.N + to : static_cast<float*>(p.y) + to;
+                    if (columns >= 8) {
+                        store_any16(y, td_u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+                        store_any16(y + 4, td_u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            if (q < columns) y[q] = v[q];
+                    }
+                } else {
+                    bf16_t* y = static_cast<bf16_t*>(p.y) + to;
+                    const td_u32x4 o = {to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
+                    if (columns >= 8) {
+                        store_any16(y, o);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            if (q < columns) y[q] = (bf16_t)(o[q / 2] >> (16 * (q & 1)));
+                    }
+                }
+            }
+        });
+    });
+}
+
+}  // namespace
+
+// ---------------------------------------------------------------- launches, for one element type
+namespace {
+
+template <typename F> void for_linear_shape(bool direct, int shape, F f) {
+    if (direct) {
+        switch (shape) {
+            case 0: f(std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<5>{}); break;
+            case 1: f(std::true_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<3>{}); break;
+            case 2: f(std::true_type{}, num<1>{}, num<4>{}, num<1>{}, num<1>{}, num<8>{}, num<4>{}); break;
+            case 3: f(std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<5>{}); break;
+            case 4: f(std::true_type{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<6>{}); break;
+            case 5: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}, num<6>{}); break;
+            case 6: f(std::true_type{}, num<4>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<5>{}); break;
+            case 7: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<5>{}); break;
+            case 8: f(std::true_type{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<6>{}); break;
+            case 9: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<5>{}); break;
+            default: f(std::true_type{}, num<6>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<4>{}); break;
+        }
+    } else {
+        switch (shape) {
+            case 0: f(std::false_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<2>{}); break;
+            case 1: f(std::false_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}); break;
+            default: f(std::false_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}); break;
+        }
+    }
+}
+
+template <typename T> tardis_status_t linear_init() {
+    bool ok = true;
+    for (int direct = 0; direct < 2; ++direct)
+        for (int shape = 0; shape < (direct ? kLinearShapes : kLinearStagedShapes); ++shape)
+            for_linear_shape(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ring) {
+                typedef LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ring> G;
+                const LinearShape& is = direct ? kLinearShape[shape] : kLinearStaged[shape];
+                ok &= is.m == G::TM && is.n == G::TN && is.slice == G::SL;
+                auto raise = [&](auto kernel) {
+                    ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds) == hipSuccess;
+                };
+                raise(linear_kernel<T, false, decltype(d)::value, fa, fb, wm, wn, wk, ring>);
+                raise(linear_kernel<T, true, decltype(d)::value, fa, fb, wm, wn, wk, ring>);
+            });
+    return ok ? TARDIS_OK : TARDIS_ERR_HIP;
+}
+
+template <typename T> void linear_launch(const LinearArgs& p, bool grouped, bool direct, int shape, int blocks, hipStream_t s) {
+    for_linear_shape(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ring) {
+        constexpr int bytes = LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ring>::kLds;
+        if (grouped) hipLaunchKernelGGL((linear_kernel<T, true, decltype(d)::value, fa, fb, wm, wn, wk, ring>), dim3((unsigned)blocks), dim3(512), bytes, s, p);
+        else hipLaunchKernelGGL((linear_kernel<T, false, decltype(d)::value, fa, fb, wm, wn, wk, ring>), dim3((unsigned)blocks), dim3(512), bytes, s, p);
+    });
+}
+
+}  // namespace

@@ -8,6 +8,7 @@ built (``python -m paper_2501_10054_amd.build``); there is no fallback path.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -25,6 +26,7 @@ EXPORTS = (
     "tardis_calibrate", "tardis_calibrate_search", "tardis_estimate_errors", "tardis_assign_thresholds", "tardis_fold", "tardis_ffn_forward", "tardis_ffn_forward_batched",
     "tardis_ffn_forward_static", "tardis_stack_forward", "tardis_dense_forward", "tardis_get_folded", "tardis_get_predictor_state",
     "tardis_get_sketch_groups", "tardis_get_last_outliers", "tardis_get_last_union", "tardis_get_handover", "tardis_set_next_layer",
+    "tardis_linear", "tardis_linear_workspace", "tardis_grouped_linear", "tardis_moe_route", "tardis_moe_route_workspace", "tardis_moe_combine",
     "tardis_destroy", "tardis_release_memory", "tardis_status_string", "tardis_version",
 )
 
@@ -43,6 +45,11 @@ class tardis_ffn_desc(C.Structure):
 class tardis_fold_opts(C.Structure):
     _fields_ = [("sketch_bits", C.c_int32), ("folded_dtype", C.c_int32), ("max_batch", C.c_int64),
                 ("deterministic", C.c_int32), ("margin", C.c_float)]
+
+
+class tardis_linear_desc(C.Structure):
+    _fields_ = [("n_in", C.c_int64), ("n_out", C.c_int64), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("act", C.c_int32),
+                ("reserved", C.c_int32), ("W", C.c_void_p), ("b", C.c_void_p)]
 
 
 _lib_handle = None
@@ -74,6 +81,12 @@ def lib() -> C.CDLL:
         L.tardis_get_last_outliers.argtypes = [vp, i64, vp, vp, vp, vp]
         L.tardis_get_last_union.argtypes = [vp, i64, vp, vp, vp]
         L.tardis_get_handover.argtypes = [vp, i64, vp, vp]
+        L.tardis_linear.argtypes = [C.POINTER(tardis_linear_desc), vp, i64, i64, vp, vp, vp, i64, vp]
+        L.tardis_linear_workspace.argtypes = [C.POINTER(tardis_linear_desc), i64, C.POINTER(i64)]
+        L.tardis_grouped_linear.argtypes = [C.POINTER(tardis_linear_desc), i64, vp, i64, i64, vp, vp, i64, i64, vp, vp]
+        L.tardis_moe_route.argtypes = [vp, i64, i64, i64, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.tardis_moe_route_workspace.argtypes = [i64, i64, C.POINTER(i64)]
+        L.tardis_moe_combine.argtypes = [vp, i64, vp, vp, i64, i64, i64, C.c_int32, vp, vp, C.c_int32, vp]
         L.tardis_destroy.argtypes = [vp]
         L.tardis_release_memory.argtypes = []
         L.tardis_status_string.argtypes = [C.c_int]
@@ -303,3 +316,101 @@ def tardis_get_last_union(L: Layer, n: int, want_mask: bool = False, stream=None
 def tardis_release_memory():
     """Returns to the device the memory that the library keeps of the layer closed last (see tardis_destroy)."""
     _check(lib().tardis_release_memory(), "tardis_release_memory")
+
+
+@functools.lru_cache(maxsize=1024)
+def _linear_work_bytes(n, n_in, n_out, dtype, out_dtype, act):
+    """Of a call of these sizes (weights at an aligned address stand in for those of the call)."""
+    bytes_ = C.c_int64()
+    desc = tardis_linear_desc(n_in, n_out, dtype, out_dtype, act, 0, 256, None)
+    _check(lib().tardis_linear_workspace(desc, n, bytes_), "tardis_linear_workspace")
+    return bytes_.value
+
+
+@functools.lru_cache(maxsize=1024)
+def _route_work_bytes(n, experts):
+    bytes_ = C.c_int64()
+    _check(lib().tardis_moe_route_workspace(n, experts, bytes_), "tardis_moe_route_workspace")
+    return bytes_.value
+
+
+def _rows(x, n_in):
+    """Rows that may lie further apart than they are long -> their number and distance."""
+    assert x.is_cuda and x.dim() == 2 and x.shape[1] == n_in
+    n, (pitch, step) = x.shape[0], x.stride()
+    assert (step == 1 or n_in == 1) and (pitch >= n_in or n <= 1)
+    return n, max(pitch, n_in)
+
+
+def tardis_linear(x, W, b=None, act: str = "identity", residual=None, out_dtype=None, y=None, stream=None):
+    """-> n x n_out: act(x W^T + b) + residual.  Rows of x may have a pitch; out_dtype: of residual and y (default: x's)."""
+    n_out, n_in = W.shape
+    n, pitch = _rows(x, n_in)
+    dt = x.dtype
+    out_dtype = out_dtype or dt
+    assert W.is_contiguous() and W.dtype == dt and W.device == x.device
+    assert b is None or (b.is_contiguous() and b.dtype == dt and b.numel() == n_out and b.device == x.device)
+    assert residual is None or (residual.is_contiguous() and residual.dtype == out_dtype and residual.shape == (n, n_out) and residual.device == x.device)
+    if y is None:
+        y = torch.empty(n, n_out, dtype=out_dtype, device=x.device)
+    else:
+        assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, n_out) and y.device == x.device
+    code, out_code, act_code = _DTYPE_CODE[dt], _DTYPE_CODE[out_dtype], ACT[act]
+    desc = tardis_linear_desc(n_in, n_out, code, out_code, act_code, 0, W.data_ptr(), None if b is None else b.data_ptr())
+    bytes_ = _linear_work_bytes(n, n_in, n_out, code, out_code, act_code)
+    work = torch.empty(bytes_, dtype=torch.uint8, device=x.device) if bytes_ else None
+    _check(lib().tardis_linear(desc, x.data_ptr(), n, pitch, _ptr(residual), y.data_ptr(), _ptr(work), bytes_, _stream(stream)), "tardis_linear")
+    return y
+
+
+def tardis_grouped_linear(x, W, offsets, b=None, act: str = "identity", order=None, per_token: int = 1, out_dtype=None, y=None, stream=None):
+    """-> positions x n_out: act(x[order[p] // per_token] W[e]^T + b[e]) at positions offsets[e] <= p < offsets[e + 1]; without
+    an order x[p].  W: experts x n_out x n_in.  Rows of y in no group are not written."""
+    experts, n_out, n_in = W.shape
+    x_rows, pitch = _rows(x, n_in)
+    dt = x.dtype
+    out_dtype = out_dtype or dt
+    assert W.is_contiguous() and W.dtype == dt and W.device == x.device
+    assert b is None or (b.is_contiguous() and b.dtype == dt and b.numel() == experts * n_out and b.device == x.device)
+    assert offsets.is_contiguous() and offsets.dtype == torch.int32 and offsets.numel() == experts + 1 and offsets.device == x.device
+    assert order is None or (order.is_contiguous() and order.dtype == torch.int32 and order.device == x.device)
+    positions = x_rows if order is None else order.numel()
+    if y is None:
+        y = torch.empty(positions, n_out, dtype=out_dtype, device=x.device)
+    else:
+        assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (positions, n_out) and y.device == x.device
+    desc = tardis_linear_desc(n_in, n_out, _DTYPE_CODE[dt], _DTYPE_CODE[out_dtype], ACT[act], 0, W.data_ptr(), None if b is None else b.data_ptr())
+    _check(lib().tardis_grouped_linear(desc, experts, x.data_ptr(), x_rows, pitch, offsets.data_ptr(), _ptr(order), per_token, positions, y.data_ptr(),
+                                       _stream(stream)), "tardis_grouped_linear")
+    return y
+
+
+def tardis_moe_route(logits, k: int, renormalise: bool = True, stream=None):
+    """logits n x experts -> (ids int32[n, k], weights float32[n, k], offsets int32[experts + 1], order int32[n k], place int32[n, k])."""
+    n, experts = logits.shape
+    assert logits.is_cuda and logits.is_contiguous()
+    dev = logits.device
+    words = torch.empty(3 * n * k + experts + 1, dtype=torch.int32, device=dev)
+    ids, order, place, offsets = words[:n * k].view(n, k), words[n * k:2 * n * k], words[2 * n * k:3 * n * k].view(n, k), words[3 * n * k:]
+    weights = torch.empty(n, k, dtype=torch.float32, device=dev)
+    bytes_ = _route_work_bytes(n, experts)
+    work = torch.empty(bytes_, dtype=torch.uint8, device=dev) if bytes_ else None
+    _check(lib().tardis_moe_route(logits.data_ptr(), n, experts, k, _DTYPE_CODE[logits.dtype], 1 if renormalise else 0, ids.data_ptr(), weights.data_ptr(),
+                                  offsets.data_ptr(), order.data_ptr(), place.data_ptr(), _ptr(work), bytes_, _stream(stream)), "tardis_moe_route")
+    return ids, weights, offsets, order, place
+
+
+def tardis_moe_combine(z, place, weights, residual=None, out_dtype=None, y=None, stream=None):
+    """-> n x d: residual[t] + sum_j weights[t, j] z[place[t, j]]; a place below 0 is a dropped slot.  out_dtype: of residual and y (default: z's)."""
+    (rows, d), (n, k) = z.shape, place.shape
+    out_dtype = out_dtype or z.dtype
+    assert z.is_cuda and z.is_contiguous() and place.is_contiguous() and place.dtype == torch.int32 and place.device == z.device
+    assert weights.is_contiguous() and weights.dtype == torch.float32 and weights.shape == (n, k) and weights.device == z.device
+    assert residual is None or (residual.is_contiguous() and residual.dtype == out_dtype and residual.shape == (n, d) and residual.device == z.device)
+    if y is None:
+        y = torch.empty(n, d, dtype=out_dtype, device=z.device)
+    else:
+        assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, d) and y.device == z.device
+    _check(lib().tardis_moe_combine(z.data_ptr(), rows, place.data_ptr(), weights.data_ptr(), n, k, d, _DTYPE_CODE[z.dtype], _ptr(residual), y.data_ptr(),
+                                    _DTYPE_CODE[out_dtype], _stream(stream)), "tardis_moe_combine")
+    return y

@@ -1,0 +1,213 @@
+"""The linear layer with its epilogue and the grouped product of experts against their definition in 64 bits.
+
+Tolerance of an element.  Products are exact or rounded once in fp32, and an output is a chain of at most K / 32 (bf16; fp32: K / 4)
+matrix instructions and 40 more additions (inside of an instruction, of the wavefronts' and the ranges' parts), each of which may be off by 2^-23 of a
+partial sum.  Partial sums stay below 4 q + |z|, q = sqrt(sum (w x)^2) (terms of either sign).  No activation has a slope above 1.13, and its own
+error is below 2^-20 of z.  The result is rounded once, by at most eps / 2 of itself, to the type of y; an fp32 addition of the bias and
+of the residual rounds by 2^-24 of its sum."""
+import math
+
+import pytest
+import torch
+
+from paper_2501_10054_amd import tardis as T
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+ACTS = ("identity", "gelu_erf", "gelu_tanh", "relu")
+
+
+def sigma(z, act):
+    if act == "gelu_erf":
+        return 0.5 * z * torch.erfc(-z / math.sqrt(2.0))
+    if act == "gelu_tanh":
+        return z / (1.0 + torch.exp(-2.0 * math.sqrt(2.0 / math.pi) * (z + 0.044715 * z ** 3)))
+    return z.clamp_min(0.0) if act == "relu" else z
+
+
+def inside(shape, dtype, gen, std=1.0, gap=0, lead=0):
+    """Normal values of this shape whose memory is surrounded by NaNs: before and behind, and `gap` columns behind every row."""
+    n, k = shape[-2], shape[-1]
+    rows = math.prod(shape[:-1])
+    store = torch.full((lead + rows * (k + gap) + 4096,), math.nan, dtype=dtype, device=DEV)
+    t = store[lead:lead + rows * (k + gap)].view(rows, k + gap)[:, :k]
+    t.copy_(torch.randn(rows, k, device=DEV, generator=gen) * std)
+    return t if gap or len(shape) == 2 else t.view(shape)
+
+
+def layer64(x, W, b, act):
+    """z's layer in 64 bits, and the bound on what fp32 sums are off by"""
+    per = 32 if W.dtype == torch.bfloat16 else 4
+    w64, x64 = W.double(), x.double()
+    z = torch.mm(w64, x64.t().contiguous()).t()
+    q = torch.mm(w64 ** 2, (x64 ** 2).t().contiguous()).t().sqrt()
+    if b is not None:
+        z = z + b.double()
+    off = (W.shape[1] / per + 40) * 2.0 ** -23 * (4.0 * q + z.abs())
+    return sigma(z, act), 1.13 * off + 2.0 ** -20 * z.abs()
+
+
+def check(y, want, off):
+    eps = torch.finfo(y.dtype).eps / 2
+    err = (y.double() - want).abs()
+    bound = off + (eps + 2.0 ** -22) * (want.abs() + off) + 1e-30
+    worst = (err / bound).max().item() if err.numel() else 0.0
+    assert not torch.isnan(err).any() and worst <= 1.0, worst
+
+
+# n, n_in, n_out
+SIZES = [(1, 1, 1), (3, 7, 5), (1, 16384, 96), (2, 512, 16), (5, 2048, 300), (16, 4096, 64), (17, 40, 65), (31, 1000, 129), (64, 4096, 64),
+         (64, 1408, 1000), (65, 129, 1030), (130, 1000, 257), (200, 2048, 2048), (333, 1416, 1000), (509, 1000, 1500), (700, 264, 776), (1025, 520, 1032)]
+
+
+@pytest.mark.parametrize("case", range(len(SIZES)))
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("gap", [0, 8, 3])
+def test_linear(case, dtype, gap):
+    n, n_in, n_out = SIZES[case]
+    gen = torch.Generator(device=DEV).manual_seed(1000 + 7 * case + gap)
+    act = ACTS[(case + gap) % 4]
+    x = inside((n, n_in), dtype, gen, gap=gap)
+    W = inside((n_out, n_in), dtype, gen, std=2.0 / math.sqrt(n_in))
+    b = torch.randn(n_out, device=DEV, generator=gen).to(dtype) if case % 2 == 0 else None
+    for out in (torch.float32, torch.bfloat16):
+        r = torch.randn(n, n_out, device=DEV, generator=gen).to(out) if (case + gap) % 3 != 1 else None
+        y = T.tardis_linear(x, W, b, act=act, residual=r, out_dtype=out)
+        want, off = layer64(x, W, b, act)
+        check(y, want if r is None else want + r.double(), off)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_linear_at_any_address(dtype):
+    """Operands, residual and output that begin at an odd element."""
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    for n, n_in, n_out in [(4, 256, 64), (70, 512, 200), (150, 1024, 136)]:
+        x, W = inside((n, n_in), dtype, gen, lead=1), inside((n_out, n_in), dtype, gen, std=0.1, lead=3)
+        b = inside((1, n_out), dtype, gen, lead=5)[0]
+        for out in (torch.float32, torch.bfloat16):
+            r = inside((n, n_out), out, gen, lead=1)
+            y = torch.zeros(n * n_out + 8, dtype=out, device=DEV)
+            got = T.tardis_linear(x, W, b, act="gelu_erf", residual=r, out_dtype=out, y=y[1:1 + n * n_out].view(n, n_out))
+            want, off = layer64(x, W, b, "gelu_erf")
+            check(got, want + r.double(), off)
+            assert y[0] == 0 and (y[1 + n * n_out:] == 0).all()          # nothing else was written
+
+
+def test_linear_writes_onto_its_residual():
+    gen = torch.Generator(device=DEV).manual_seed(6)
+    for n, n_in, n_out in [(1, 4096, 512), (64, 4096, 64), (333, 1408, 1000)]:
+        x, W = inside((n, n_in), torch.bfloat16, gen), inside((n_out, n_in), torch.bfloat16, gen, std=0.02)
+        r = torch.randn(n, n_out, device=DEV, generator=gen).bfloat16()
+        want = T.tardis_linear(x, W, residual=r)
+        T.tardis_linear(x, W, residual=r, y=r)
+        assert torch.equal(r, want)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_a_row_that_is_not_finite_stays_alone(dtype):
+    gen = torch.Generator(device=DEV).manual_seed(7)
+    for n, n_in, n_out in [(5, 1000, 40), (40, 1408, 96), (200, 1001, 130), (300, 520, 260)]:
+        x, W = inside((n, n_in), dtype, gen), inside((n_out, n_in), dtype, gen, std=0.05)
+        want = T.tardis_linear(x, W, act="relu")
+        bad = x.clone()
+        bad[n // 2, n_in - 1] = math.nan
+        bad[0, 0] = math.inf
+        got = T.tardis_linear(bad, W)
+        keep = [m for m in range(n) if m not in (0, n // 2)]
+        assert torch.equal(got.clamp_min(0.0)[keep], want[keep])
+        assert torch.isnan(got[n // 2]).all() and torch.isinf(got[0]).all()
+
+
+def test_no_rows():
+    W = torch.randn(8, 16, device=DEV)
+    assert T.tardis_linear(torch.empty(0, 16, device=DEV), W).shape == (0, 8)
+    offsets = torch.zeros(3, dtype=torch.int32, device=DEV)
+    y = T.tardis_grouped_linear(torch.empty(0, 16, device=DEV), torch.randn(2, 8, 16, device=DEV), offsets)
+    assert y.shape == (0, 8)
+    # no tokens at all, but slots: none of them is one of a token
+    y = torch.full((4, 8), 7.0, device=DEV)
+    T.tardis_grouped_linear(torch.empty(0, 16, device=DEV), torch.randn(2, 8, 16, device=DEV), torch.tensor([0, 2, 4], dtype=torch.int32, device=DEV),
+                            order=torch.arange(4, dtype=torch.int32, device=DEV), per_token=2, y=y)
+    assert (y == 7.0).all()
+
+
+def grouped64(x, W, b, offsets, order, per_token, positions, act):
+    n_out = W.shape[1]
+    want = torch.full((positions, n_out), math.nan, dtype=torch.float64, device=DEV)
+    off = torch.zeros_like(want)
+    ends = [min(max(o, 0), positions) for o in offsets.tolist()]
+    for e in range(W.shape[0]):
+        p = torch.arange(ends[e], max(ends[e], ends[e + 1]), device=DEV)
+        if order is not None:
+            token = torch.div(order[p].long(), per_token, rounding_mode="floor")
+            there = (order[p] >= 0) & (token < x.shape[0])
+            p, token = p[there], token[there]
+        else:
+            token = p
+        if p.numel():
+            want[p], off[p] = layer64(x[token], W[e], None if b is None else b[e], act)
+    return want, off
+
+
+def random_groups(gen, positions, experts, kind):
+    if kind == "one":                          # one expert has everything
+        cuts = torch.full((experts - 1,), positions if experts > 2 else 0)
+    elif kind == "even":
+        cuts = torch.arange(1, experts) * positions // experts
+    else:                                      # many of them empty
+        cuts = torch.randint(0, positions + 1, (experts - 1,), generator=gen).sort().values
+        cuts[::3] = cuts[1::3][:cuts[::3].numel()].clone() if cuts.numel() > 3 and cuts[1::3].numel() == cuts[::3].numel() else cuts[::3]
+    return torch.cat([torch.zeros(1), cuts.sort().values, torch.full((1,), positions)]).int().to(DEV)
+
+
+# tokens, k, n_in, n_out, experts
+GROUPED = [(1, 1, 64, 48, 1), (1, 2, 512, 64, 5), (16, 2, 1024, 256, 16), (33, 4, 200, 72, 70), (50, 8, 257, 130, 9), (300, 2, 512, 264, 3),
+           (257, 4, 1408, 136, 64), (90, 3, 96, 40, 200), (700, 2, 264, 520, 2)]
+
+
+@pytest.mark.parametrize("case", range(len(GROUPED)))
+@pytest.mark.parametrize("kind", ["even", "random", "one"])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_grouped_linear(case, kind, dtype):
+    n, k, n_in, n_out, experts = GROUPED[case]
+    seed = 3000 + 5 * case
+    gen, host = torch.Generator(device=DEV).manual_seed(seed), torch.Generator().manual_seed(seed)
+    W = inside((experts, n_out, n_in), dtype, gen, std=2.0 / math.sqrt(n_in))
+    b = torch.randn(experts, n_out, device=DEV, generator=gen).to(dtype) if case % 2 else None
+    act, out = ACTS[case % 4], (torch.float32, torch.bfloat16)[case % 2]
+    offsets = random_groups(host, n * k, experts, kind)
+    order = torch.randperm(n * k, generator=host).int().to(DEV)
+    for x, o in ((inside((n, n_in), dtype, gen, gap=(0, 8, 3)[case % 3]), order), (inside((n * k, n_in), dtype, gen), None)):
+        y = T.tardis_grouped_linear(x, W, offsets, b, act=act, order=o, per_token=k, out_dtype=out)
+        check(y, *grouped64(x, W, b, offsets, o, k, n * k, act))
+
+
+@pytest.mark.parametrize("n_in", [256, 255])
+def test_rows_in_no_group_and_slots_of_no_token_are_left(n_in):
+    """Offsets that begin late, end early, lie outside or go back; slots of -1 and past the last token."""
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    n, k, n_out, experts = 40, 3, 70, 4
+    x, W = inside((n, n_in), torch.bfloat16, gen), inside((experts, n_out, n_in), torch.bfloat16, gen, std=0.1)
+    order = torch.randperm(n * k, device=DEV, generator=gen).int()
+    order[[0, 5, 50, 51, 119]] = torch.tensor([-1, n * k, -2 ** 31, 2 ** 31 - 1, -1], device=DEV).int()
+    for ends in ([7, 30, 30, 90, 101], [0, 0, 0, 0, 0], [120] * 5, [-50, 20, 40, 100, 5000], [0, 60, 40, 40, 80], [120, 0, 0, 0, 0]):
+        offsets = torch.tensor(ends, device=DEV).int()
+        y = torch.full((n * k, n_out), 5.0, device=DEV)
+        T.tardis_grouped_linear(x, W, offsets, order=order, per_token=k, out_dtype=torch.float32, y=y)
+        if ends[2] < ends[1]:
+            continue                           # (groups that overlap: one of the two results, and no fault)
+        want, off = grouped64(x, W, None, offsets, order, k, n * k, "identity")
+        left = torch.isnan(want)
+        assert (y[left] == 5.0).all()
+        check(y[~left], want[~left], off[~left])
+
+
+def test_the_same_bits_in_every_run():
+    gen = torch.Generator(device=DEV).manual_seed(11)
+    x, W = inside((64, 4096), torch.bfloat16, gen), inside((64, 4096), torch.bfloat16, gen, std=0.02)
+    We = inside((8, 192, 4096), torch.bfloat16, gen, std=0.02)
+    offsets = torch.tensor([0, 3, 3, 9, 20, 21, 40, 50, 64], device=DEV).int()
+    a, g = T.tardis_linear(x, W, out_dtype=torch.float32), T.tardis_grouped_linear(x, We, offsets, out_dtype=torch.float32)
+    for _ in range(10):
+        assert torch.equal(a, T.tardis_linear(x, W, out_dtype=torch.float32))
+        assert torch.equal(g, T.tardis_grouped_linear(x, We, offsets, out_dtype=torch.float32))
