@@ -342,13 +342,14 @@ typedef struct {
  *   x         n rows of n_in values, x_pitch >= n_in values apart.
  *   residual  n x n_out, out_dtype, or NULL; may be y itself.
  *   y         n x n_out, out_dtype; must not overlap x, W or b.
- *   work      device memory for sums of ranges of n_in, at least 4-byte aligned; its
- *             content is not used again.  tardis_linear_workspace says how much the
- *             call can use (0 for most); with less, or NULL, n_in is not divided
- *             and a product of few rows and columns takes longer. */
+ *   work      device memory, 16-byte aligned, whose content is not used again: sums of ranges of
+ *             n_in, copies of operands with aligned rows.  tardis_linear_workspace says
+ *             how much the call can use (0 for many); with less, or NULL, the call does
+ *             without, and takes longer. */
 tardis_status_t tardis_linear(const tardis_linear_desc* desc, const void* x, int64_t n, int64_t x_pitch,
                               const void* residual, void* y, void* work, int64_t work_bytes, void* stream);
-tardis_status_t tardis_linear_workspace(const tardis_linear_desc* desc, int64_t n, int64_t* bytes);
+tardis_status_t tardis_linear_workspace(const tardis_linear_desc* desc, const void* x, int64_t n, int64_t x_pitch,
+                                        int64_t* bytes);
 
 /* Rows by groups: positions offsets[e] <= p < offsets[e+1] have the weights of
  * expert e,
@@ -362,10 +363,15 @@ tardis_status_t tardis_linear_workspace(const tardis_linear_desc* desc, int64_t 
  *              (negative, or row(p) >= x_rows), or whose position is in no group, is left
  *              as it is.
  *   x          x_rows rows, x_pitch >= n_in values apart (without an order: positions of them).
- *   y          positions x n_out, out_dtype. */
+ *   y          positions x n_out, out_dtype.
+ *   work       as tardis_linear's (ordered: 1 for a call with an order). */
 tardis_status_t tardis_grouped_linear(const tardis_linear_desc* desc, int64_t experts, const void* x, int64_t x_rows,
                                       int64_t x_pitch, const int32_t* offsets, const int32_t* order,
-                                      int64_t per_token, int64_t positions, void* y, void* stream);
+                                      int64_t per_token, int64_t positions, void* y, void* work, int64_t work_bytes,
+                                      void* stream);
+tardis_status_t tardis_grouped_linear_workspace(const tardis_linear_desc* desc, int64_t experts, const void* x,
+                                                int64_t x_rows, int64_t x_pitch, int32_t ordered, int64_t positions,
+                                                int64_t* bytes);
 
 /* The k experts of every token: those of its largest logits, the lower index first
  * among equal ones; weights are the softmax over the chosen ones (renormalise = 1) or over all

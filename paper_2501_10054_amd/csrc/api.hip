@@ -16,7 +16,7 @@ constexpr int64_t kMaxCal = 32768;        // one neuron's samples are sorted in 
 constexpr int64_t kMaxSearchCal = 8192;   // range search also keeps sigma of every sample there, in fp64
 constexpr int64_t kMaxBatch = 4096;
 constexpr int64_t kMaxWidth = 1 << 22, kMaxPitch = (int64_t)1 << 30;   // linear layers
-constexpr int64_t kMaxRows = (int64_t)1 << 30;
+constexpr int64_t kMaxRows = (int64_t)1 << 30, kMaxGroups = 65536;
 constexpr int64_t kMaxExperts = 1024, kMaxChosen = 16;   // the router: an expert for a thread of a block, a choice for a lane of 16
 // 4-bit layers folded for at most this many tokens, and for fewer than run as products, keep the packed sketch alone.  More
 // tokens are groups of 8 and 16, which read one-byte codes (blocks of 1024 threads), and were groups of 4 and 2 without them; us at
@@ -566,35 +566,59 @@ bool rows_fit(int64_t rows, int64_t pitch) { return rows >= 0 && rows <= kMaxRow
 
 }  // namespace
 
-tardis_status_t tardis_linear_workspace(const tardis_linear_desc* desc, int64_t n, int64_t* bytes) {
+namespace {
+
+tardis_status_t check_linear_rows(const tardis_linear_desc* d, int64_t rows, int64_t pitch) {
+    return rows_fit(rows, pitch) && pitch >= d->n_in ? TARDIS_OK : TARDIS_ERR_SHAPE;
+}
+tardis_status_t check_grouped_rows(const tardis_linear_desc* d, int64_t experts, int64_t x_rows, int64_t pitch, bool order, int64_t per_token, int64_t positions) {
+    TD_TRY(check_linear_rows(d, x_rows, pitch));
+    if (experts < 1 || experts > kMaxGroups || !rows_fit(positions, 0)) return TARDIS_ERR_SHAPE;
+    return (order ? per_token >= 1 && per_token <= kMaxRows : x_rows >= positions) ? TARDIS_OK : TARDIS_ERR_SHAPE;
+}
+bool work_ok(const void* work, int64_t bytes) { return aligned16(work) && bytes >= 0; }
+
+}  // namespace
+
+tardis_status_t tardis_linear_workspace(const tardis_linear_desc* desc, const void* x, int64_t n, int64_t x_pitch, int64_t* bytes) {
     TD_TRY(check_linear(desc));
+    TD_TRY(check_linear_rows(desc, n, x_pitch));
     if (!bytes) return TARDIS_ERR_INVALID_ARG;
-    if (!rows_fit(n, 0)) return TARDIS_ERR_SHAPE;
-    *bytes = n > 0 ? (int64_t)td_linear_work_bytes(desc, n) : 0;
+    *bytes = n > 0 ? td_linear_work_bytes(desc, 0, x, n, x_pitch, false, n) : 0;
     return TARDIS_OK;
 }
 
 tardis_status_t tardis_linear(const tardis_linear_desc* desc, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y,
                               void* work, int64_t work_bytes, void* stream) {
     TD_TRY(check_linear(desc));
-    if (!rows_fit(n, x_pitch) || x_pitch < desc->n_in) return TARDIS_ERR_SHAPE;
+    TD_TRY(check_linear_rows(desc, n, x_pitch));
     if (n == 0) return TARDIS_OK;
     const size_t es = td_elem_size(desc->dtype), eo = td_elem_size(desc->out_dtype);
-    if (!x || !y || !aligned_to(x, es) || !aligned_to(y, eo) || !aligned_to(residual, eo) || !aligned_to(work, 4) || work_bytes < 0) return TARDIS_ERR_INVALID_ARG;
+    if (!x || !y || !aligned_to(x, es) || !aligned_to(y, eo) || !aligned_to(residual, eo) || !work_ok(work, work_bytes)) return TARDIS_ERR_INVALID_ARG;
     return td_linear(desc, x, n, x_pitch, residual, y, work, work ? work_bytes : 0, static_cast<hipStream_t>(stream));
 }
 
-tardis_status_t tardis_grouped_linear(const tardis_linear_desc* desc, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch,
-                                      const int32_t* offsets, const int32_t* order, int64_t per_token, int64_t positions, void* y, void* stream) {
+tardis_status_t tardis_grouped_linear_workspace(const tardis_linear_desc* desc, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch,
+                                                int32_t ordered, int64_t positions, int64_t* bytes) {
     TD_TRY(check_linear(desc));
-    if (experts < 1 || experts > 65536 || !rows_fit(x_rows, x_pitch) || x_pitch < desc->n_in || !rows_fit(positions, 0)) return TARDIS_ERR_SHAPE;
-    if (order ? per_token < 1 || per_token > kMaxRows : x_rows < positions) return TARDIS_ERR_SHAPE;
+    TD_TRY(check_grouped_rows(desc, experts, x_rows, x_pitch, ordered != 0, 1, positions));
+    if (!bytes) return TARDIS_ERR_INVALID_ARG;
+    *bytes = x_rows > 0 && positions > 0 ? td_linear_work_bytes(desc, experts, x, x_rows, x_pitch, ordered != 0, positions) : 0;
+    return TARDIS_OK;
+}
+
+tardis_status_t tardis_grouped_linear(const tardis_linear_desc* desc, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch,
+                                      const int32_t* offsets, const int32_t* order, int64_t per_token, int64_t positions, void* y, void* work,
+                                      int64_t work_bytes, void* stream) {
+    TD_TRY(check_linear(desc));
+    TD_TRY(check_grouped_rows(desc, experts, x_rows, x_pitch, order != nullptr, per_token, positions));
     if (positions == 0) return TARDIS_OK;
-    if (!offsets || !aligned_to(offsets, 4) || !aligned_to(order, 4)) return TARDIS_ERR_INVALID_ARG;
+    if (!offsets || !aligned_to(offsets, 4) || !aligned_to(order, 4) || !work_ok(work, work_bytes)) return TARDIS_ERR_INVALID_ARG;
     if (x_rows == 0) return TARDIS_OK;                   // (no slot is one of a token)
     const size_t es = td_elem_size(desc->dtype), eo = td_elem_size(desc->out_dtype);
     if (!x || !y || !aligned_to(x, es) || !aligned_to(y, eo)) return TARDIS_ERR_INVALID_ARG;
-    return td_grouped_linear(desc, experts, x, x_rows, x_pitch, offsets, order, order ? per_token : 1, positions, y, static_cast<hipStream_t>(stream));
+    return td_grouped_linear(desc, experts, x, x_rows, x_pitch, offsets, order, order ? per_token : 1, positions, y, work, work ? work_bytes : 0,
+                             static_cast<hipStream_t>(stream));
 }
 
 tardis_status_t tardis_moe_route_workspace(int64_t n, int64_t experts, int64_t* bytes) {

@@ -19,17 +19,24 @@ struct LinearArgs {
     uint32_t inv_per_token;
 };
 
+constexpr int kActGelu16 = 4;                     // behind tardis_act_t's: GELU for outputs in bf16
 constexpr uint32_t kNowhere = 0xe0000000u;        // an offset past the end of any operand that is loaded by offsets
 
 // The tiles: rows, columns, wavefronts that divide K (a slice is 64 bytes of each).  f(row blocks, column blocks of a wavefront, grid of
 // wavefronts, wavefronts in K, slices in LDS)
 struct LinearShape { int m, n, slice; };
 constexpr LinearShape kLinearShape[] = {{16, 16, 512}, {16, 32, 512}, {16, 64, 512}, {32, 32, 256}, {32, 64, 256}, {64, 32, 256},
-                                        {64, 64, 256}, {64, 64, 128}, {128, 64, 128}, {128, 128, 128}, {192, 128, 128}};
+                                        {64, 64, 256}, {64, 64, 128}, {128, 64, 128}, {128, 128, 128}, {192, 128, 128},
+                                        {16, 16, 1024}, {32, 32, 512}};
 constexpr int kLinearShapes = sizeof(kLinearShape) / sizeof(LinearShape);
-constexpr LinearShape kLinearStaged[] = {{16, 32, 512}, {64, 64, 128}, {128, 128, 128}};
+constexpr LinearShape kLinearStaged[] = {{16, 16, 512}, {16, 32, 512}, {32, 32, 256}, {64, 64, 128}, {128, 128, 128}};
 constexpr int kLinearStagedShapes = sizeof(kLinearStaged) / sizeof(LinearShape);
+// of linear_quad_kernel (bf16, rows in whole pieces)
+constexpr LinearShape kLinearQuad[] = {{256, 256, 128}, {192, 256, 128}, {256, 128, 128}};
+constexpr int kLinearQuads = sizeof(kLinearQuad) / sizeof(LinearShape);
 
+tardis_status_t td_linear_init_quad();
+void td_linear_launch_quad(const LinearArgs& p, bool grouped, int shape, int blocks, hipStream_t s);
 tardis_status_t td_linear_init_bf16();
 tardis_status_t td_linear_init_f32();
 void td_linear_launch_bf16(const LinearArgs& p, bool grouped, bool direct, int shape, int blocks, hipStream_t s);

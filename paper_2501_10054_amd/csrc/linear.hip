@@ -1,81 +1,227 @@
-// A linear layer with its epilogue, y = sigma(x W^T + b) + r, alone or for rows grouped by expert: which tile a call takes, ranges of K
-// and their sum.  The kernel is in linear_tile.h.
+// A linear layer with its epilogue, y = sigma(x W^T + b) + r, alone or for rows grouped by expert: how a call is done - which tile, in how
+// many ranges of K, of which operands a copy with aligned rows is made first.  The kernels are in linear_tile.h and linear_quad.hip.
 #include <algorithm>
+#include <cmath>
 
-#include "linear.h"
-#include "sigma.h"
+#include "linear_act.h"
 #include "tiles.h"
 
 namespace {
 
 bool is_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+typedef uint32_t any16_t __attribute__((ext_vector_type(4), aligned(2)));
 
-// The sums of the ranges of K, and the epilogue: a thread has 4 neighbouring columns.
+// Rows of k bytes, `pitch` apart and at any address, to rows of `units` 16-byte pieces, zeros behind the last element.
 template <typename T>
-__global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, int64_t units_of_row) {
-    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / units_of_row, n = (u - row * units_of_row) * 4, at = row * p.N + n;
-    if (row >= p.n) return;
-    const int columns = (int)min((int64_t)4, p.N - n);
-    float v[4] = {};
-    for (int s = 0; s < p.splits; ++s)
+__global__ void __launch_bounds__(256) linear_pack_kernel(const unsigned char* from, int64_t pitch, uint32_t k, td_u32x4* to, int64_t rows, uint32_t units) {
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / units;
+    if (row >= rows) return;
+    const uint32_t at = (uint32_t)(u - row * units) * 16u;
+    const unsigned char* p = from + row * pitch + at;
+    td_u32x4 v = {0, 0, 0, 0};
+    if (at + 16 <= k) {
+        v = *reinterpret_cast<const any16_t*>(p);
+    } else {
+        const T* el = reinterpret_cast<const T*>(p);
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (q < columns) v[q] += p.part[((int64_t)s * p.n) * p.N + at + q];
-    with_act(p.act, [&](auto act) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (q >= columns) continue;
-            float z = v[q] + (p.b ? td_load<T>(static_cast<const T*>(p.b) + n + q) : 0.0f);
-            z = act_flat<decltype(act)::value>(z);
-            if (p.r) z += p.out_f32 ? static_cast<const float*>(p.r)[at + q] : td_load<bf16_t>(static_cast<const bf16_t*>(p.r) + at + q);
-            if (p.out_f32) static_cast<float*>(p.y)[at + q] = z;
-            else td_store<bf16_t>(static_cast<bf16_t*>(p.y) + at + q, z);
-        }
-    });
+        for (uint32_t q = 0; q < 16 / sizeof(T); ++q)
+            if (at + q * sizeof(T) < k) {
+                if constexpr (sizeof(T) == 2) v[q / 2] |= (uint32_t)el[q] << (16 * (q & 1));
+                else v[q] = __float_as_uint(el[q]);
+            }
+    }
+    to[u] = v;
 }
 
-struct Choice { int shape, splits, slices; };
+// The sums of the ranges of K, in their order, and the epilogue: a thread has 4 neighbouring columns.
+template <typename T>
+__global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, uint32_t units) {
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t row = u < (1ll << 32) ? (int64_t)((uint32_t)u / units) : u / units;
+    if (row >= p.n) return;
+    const int64_t n = (u - row * units) * 4, at = row * p.N + n, range = p.n * p.N;
+    const int columns = (int)min((int64_t)4, p.N - n);
+    float v[4] = {}, r[4] = {}, bias[4] = {};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (q >= columns) continue;
+        if (p.b) bias[q] = td_load<T>(static_cast<const T*>(p.b) + n + q);
+        if (p.r) r[q] = p.out_f32 ? static_cast<const float*>(p.r)[at + q] : td_load<bf16_t>(static_cast<const bf16_t*>(p.r) + at + q);
+    }
+    if (columns == 4) {
+#pragma unroll 4
+        for (int s = 0; s < p.splits; ++s) {
+            const td_u32x4 part = *reinterpret_cast<const any16_t*>(p.part + s * range + at);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] += __uint_as_float(part[q]);
+        }
+    } else {
+        for (int s = 0; s < p.splits; ++s)
+            for (int q = 0; q < 4; ++q)
+                if (q < columns) v[q] += p.part[s * range + at + q];
+    }
+    with_linear_act(p.act, [&](auto act) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = linear_act<decltype(act)::value>(v[q] + bias[q]) + r[q];
+    });
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        if (q >= columns) continue;
+        if (p.out_f32) static_cast<float*>(p.y)[at + q] = v[q];
+        else td_store<bf16_t>(static_cast<bf16_t*>(p.y) + at + q, v[q]);
+    }
+}
 
-Choice choose(const LinearArgs& p, int64_t es, bool grouped, bool direct, int64_t work_bytes) {
-    Choice best{0, 1, 0};
-    if (!direct) best.shape = p.n <= 32 ? 0 : 1;
-    else best.shape = p.n <= 16 ? 1 : p.n <= 128 ? 7 : 9;
-    const int sl = (direct ? kLinearShape : kLinearStaged)[best.shape].slice;
-    const int slices = (int)((p.k + sl - 1) / sl);
-    best.slices = (slices + best.splits - 1) / best.splits;
+// ---------------------------------------------------------------- how a call is done
+// What a tile takes, in us:
+//     max(fixed x turns + slices x max(alone x turns, slice x tiles of a CU), 1.5 + bytes / tbs)
+// with `blocks` of them at once on a CU, in `turns` turns: alone is a slice's latency, slice its share of the CU.  Bytes: x, y (the ranges'
+// sums), W, and for every further row of tiles `again` of W.  The constants are those with which the choice is best: over 573 products and 140
+// grouped ones in bf16 (sizes from 64 x 64 to 16384 x 16384, 1 to 3000 rows, weights from HBM; every tile with 1, 2, 4 and 8 ranges) it takes 0.9 % more
+// than the best measured, fp32 (179, 39) 0.5 %, staged (169, 24) 0.8 %, staged fp32 (98) 0.3 %.
+struct Rate { int blocks; float alone, slice, fixed, tbs; };
+constexpr Rate kRate[] = {{2, 0.231f, 0.222f, 3.87f, 5.58f}, {2, 0.301f, 0.280f, 3.80f, 4.91f}, {1, 0.561f, 0.561f, 3.80f, 5.58f},
+                          {2, 0.248f, 0.204f, 3.80f, 4.75f}, {1, 0.341f, 0.341f, 3.87f, 4.75f}, {1, 0.290f, 0.290f, 4.07f, 4.00f},
+                          {1, 0.414f, 0.414f, 4.60f, 5.21f}, {2, 0.289f, 0.267f, 3.54f, 5.58f}, {1, 0.376f, 0.376f, 4.78f, 4.66f},
+                          {1, 0.579f, 0.579f, 4.78f, 3.81f}, {1, 0.745f, 0.745f, 8.05f, 3.60f}, {1, 0.376f, 0.376f, 4.50f, 4.13f},
+                          {1, 0.371f, 0.371f, 4.31f, 4.13f}, {1, 1.120f, 1.120f, 15.93f, 3.52f}, {1, 0.815f, 0.815f, 13.58f, 4.53f},
+                          {1, 0.718f, 0.718f, 9.41f, 3.83f}};
+constexpr Rate kRateF32[] = {{2, 0.289f, 0.228f, 4.20f, 5.31f}, {2, 0.366f, 0.344f, 4.12f, 5.31f}, {1, 1.038f, 1.038f, 3.77f, 6.32f},
+                             {2, 0.420f, 0.318f, 3.89f, 3.91f}, {1, 0.654f, 0.654f, 6.13f, 5.33f}, {1, 0.623f, 0.623f, 3.91f, 2.79f},
+                             {1, 1.174f, 1.174f, 4.77f, 6.20f}, {2, 0.634f, 0.537f, 4.33f, 3.24f}, {1, 1.116f, 1.116f, 5.30f, 2.56f},
+                             {1, 2.067f, 2.067f, 7.76f, 3.66f}, {1, 2.912f, 2.912f, 10.80f, 2.66f}, {1, 0.545f, 0.545f, 4.47f, 4.51f},
+                             {1, 0.702f, 0.702f, 3.78f, 4.02f}};
+constexpr Rate kRateStaged[] = {{2, 0.249f, 0.229f, 4.72f, 3.43f}, {1, 0.389f, 0.389f, 4.58f, 2.99f}, {2, 0.194f, 0.220f, 4.34f, 4.92f},
+                                {2, 0.221f, 0.215f, 4.32f, 2.88f}, {1, 0.565f, 0.565f, 7.03f, 3.13f}};
+constexpr Rate kRateStagedF32[] = {{2, 0.076f, 0.253f, 4.35f, 3.98f}, {1, 0.368f, 0.368f, 4.49f, 3.98f}, {2, 0.049f, 0.301f, 4.26f, 4.41f},
+                                   {2, 0.506f, 0.553f, 4.27f, 5.36f}, {1, 1.937f, 1.937f, 8.53f, 4.68f}};
+static_assert(sizeof(kRate) / sizeof(Rate) == kLinearShapes + kLinearQuads && sizeof(kRateF32) / sizeof(Rate) == kLinearShapes &&
+              sizeof(kRateStaged) / sizeof(Rate) == kLinearStagedShapes && sizeof(kRateStagedF32) / sizeof(Rate) == kLinearStagedShapes, "a rate for each tile");
+// one more launch (2.5 on the GPU; callers that are not a graph wait for their host); a byte copied, of partial sums and outputs joined; sigma of an element of a tile, of eight wavefronts and of four
+constexpr double kLaunchUs = 4.0, kCopyUs = 1.0 / 4.5e6, kJoinUs = 1.0 / 5e6, kSigmaUs = 5.0 / 65536, kSigmaQuadUs = 8.0 / 65536;
+constexpr double kAgain = 0.23, kAgainF32 = 0.34, kAgainStaged = 0.15, kAgainStagedF32 = 0.41;
+constexpr int64_t kMostTiles = 1 << 21;            // of a launch
+
+// What decides: sizes, types, alignment
+struct Call {
+    int64_t M, N, x_rows, k, pitch;                // rows of y, columns, rows of x; bytes of a row, from row to row of x
+    int es, eo, act;
+    int experts;                                   // 0: one matrix
+    bool gather, x_aligned, W_aligned;             // (addresses)
+};
+struct Plan {
+    bool direct, pack_x, pack_W;
+    int shape, splits, slices;                     // (direct, in bf16: shapes of linear_kernel, then of linear_quad_kernel)
+    int64_t k, pitch, at_W, at_part, work;         // of what is multiplied; places in the working memory and its size
+    double us;
+};
+
+int shapes_of(bool direct, int es) { return direct ? kLinearShapes + (es == 2 ? kLinearQuads : 0) : kLinearStagedShapes; }
+const LinearShape& shape_of(bool direct, int s) { return !direct ? kLinearStaged[s] : s < kLinearShapes ? kLinearShape[s] : kLinearQuad[s - kLinearShapes]; }
+
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// The least time over the ways that the call allows and that take no more than `room` bytes of working memory
+Plan make_plan(const Call& c, int64_t room) {
+    Plan best{};
+    best.us = 1e300;
+    // groups: the experts that are hit, if rows fall on them evenly
+    const double hit = c.experts ? std::max(1.0, c.experts * (1.0 - std::exp(-(double)c.M / c.experts))) : 1.0;
+    const int64_t W_rows = c.N * std::max(c.experts, 1);
+    const bool k_whole = c.k % 16 == 0;
+    for (int way = 0; way < 2; ++way) {
+        Plan p{};
+        p.direct = way == 1;
+        p.k = c.k;
+        p.pitch = c.pitch;
+        double before = 0.0;
+        if (p.direct) {
+            p.pack_W = !(k_whole && c.W_aligned);
+            p.pack_x = !(k_whole && c.x_aligned && (c.pitch % 16 == 0 || c.x_rows == 1));
+            p.k = round_up(c.k, 16);
+            if (p.pack_x) p.pitch = p.k;
+            const int64_t bytes_x = p.pack_x ? round_up(c.x_rows * p.k, 256) : 0, bytes_W = p.pack_W ? round_up(W_rows * p.k, 256) : 0;
+            p.at_W = bytes_x;
+            p.at_part = bytes_x + bytes_W;
+            if (p.pack_x) before += kLaunchUs + 2.0 * (double)bytes_x * kCopyUs;
+            if (p.pack_W) before += kLaunchUs + 2.0 * (double)bytes_W * kCopyUs;
+            if (p.pitch >= 1 << 23 || p.k >= 1 << 23 || (c.gather && (c.x_rows - 1) * p.pitch + p.k >= (int64_t)kNowhere)) continue;
+        }
+        if (p.at_part > room) continue;
+        for (int s = 0; s < shapes_of(p.direct, c.es); ++s) {
+            const LinearShape& t = shape_of(p.direct, s);
+            const Rate& r = p.direct ? (c.es == 2 ? kRate[s] : kRateF32[s]) : (c.es == 2 ? kRateStaged[s] : kRateStagedF32[s]);
+            const int64_t slices = (p.k + t.slice - 1) / t.slice, tiles_n = (c.N + t.n - 1) / t.n;
+            const double tiles_m = c.experts ? 1.05 * hit * std::max(1.0, (double)c.M / hit / t.m + 0.5) : (double)((c.M + t.m - 1) / t.m);
+            if (tiles_m * (double)tiles_n >= kMostTiles && s + 1 < shapes_of(p.direct, c.es)) continue;
+            for (int splits = 1; splits <= 8; splits *= 2) {
+                const double blocks = tiles_m * (double)tiles_n * splits;
+                if (splits > 1 && (c.experts || slices / splits < 4 || blocks > 1024 || p.at_part + splits * c.M * c.N * 4 > room)) break;
+                const double rounds = std::ceil(blocks / 256), shared = std::ceil(rounds / r.blocks);
+                const double per = (double)((slices + splits - 1) / splits);
+                const double sigma = c.act == TARDIS_ACT_GELU_ERF || c.act == TARDIS_ACT_GELU_TANH ? (p.direct && s >= kLinearShapes ? kSigmaQuadUs : kSigmaUs) * t.m * t.n * rounds : 0.0;
+                const double multiply = r.fixed * shared + per * std::max(r.alone * shared, r.slice * rounds) + (splits > 1 ? 0.0 : sigma);
+                const double again = p.direct ? (c.es == 2 ? kAgain : kAgainF32) : (c.es == 2 ? kAgainStaged : kAgainStagedF32);
+                const double bytes = (hit + again * std::max(0.0, tiles_m - hit)) * c.N * p.k + (double)c.M * p.k + (double)c.M * c.N * (splits > 1 ? 4.0 * splits : c.eo);
+                double us = before + std::max(multiply, 1.5 + bytes / (r.tbs * 1e6));
+                if (splits > 1) us += kLaunchUs + (double)c.M * c.N * (4.0 * splits + c.eo) * kJoinUs;
+                if (us < best.us) {
+                    best = p;
+                    best.us = us;
+                    best.shape = s;
+                    best.splits = splits;
+                    best.slices = (int)((slices + splits - 1) / splits);
+                    best.work = p.at_part + (splits > 1 ? splits * c.M * c.N * 4 : 0);
+                }
+            }
+        }
+    }
     return best;
 }
 
-tardis_status_t run(LinearArgs& p, int32_t dtype, bool grouped, void* work, int64_t work_bytes, hipStream_t s) {
-    const int64_t es = (int64_t)td_elem_size(dtype);
-    const bool gather = grouped && p.order;
-    const bool direct = is_aligned16(p.x) && is_aligned16(p.W) && p.k % 16 == 0 && (p.x_pitch % 16 == 0 || p.n == 1) && p.x_pitch < (1 << 23) &&
-                        p.k < (1u << 23) && (!gather || p.x_bytes < (int64_t)kNowhere);
-    const Choice c = choose(p, es, grouped, direct, work_bytes);
-    const LinearShape& t = (direct ? kLinearShape : kLinearStaged)[c.shape];
+// p: operands and sizes as the caller gave them; pitches and k in bytes
+tardis_status_t run(LinearArgs p, int32_t dtype, const Call& c, void* work, int64_t work_bytes, hipStream_t s) {
+    const Plan plan = make_plan(c, work_bytes);
+    const LinearShape& t = shape_of(plan.direct, plan.shape);
+    const bool grouped = c.experts > 0, quad = plan.direct && plan.shape >= kLinearShapes, f32 = dtype == TARDIS_F32;
     p.tiles_m = (int)((p.n + t.m - 1) / t.m);
     p.tiles_n = (int)((p.N + t.n - 1) / t.n);
-    p.splits = c.splits;
-    p.slices = c.slices;
+    p.splits = plan.splits;
+    p.slices = plan.slices;
     // (of groups: at most one tile that is not full in each, and no more than rows)
     const int64_t tiles_m = grouped ? std::min(p.n, (p.n + (int64_t)p.experts * (t.m - 1)) / t.m) : p.tiles_m;
-    const int64_t tiles = tiles_m * p.tiles_n * c.splits;
-    if (tiles >= 1 << 21) return TARDIS_ERR_SHAPE;
-    if (dtype == TARDIS_F32) TD_TRY(td_linear_init_f32());
-    else TD_TRY(td_linear_init_bf16());
+    const int64_t tiles = tiles_m * p.tiles_n * plan.splits;
+    if (tiles >= kMostTiles) return TARDIS_ERR_SHAPE;
+    if (f32) TD_TRY(td_linear_init_f32());
+    else TD_TRY(quad ? td_linear_init_quad() : td_linear_init_bf16());
+    unsigned char* memory = static_cast<unsigned char*>(work);
+    auto pack = [&](const unsigned char* from, int64_t pitch, int64_t rows, unsigned char* to) {
+        const uint32_t units = (uint32_t)(plan.k / 16);
+        const dim3 grid((unsigned)((rows * units + 255) / 256));
+        if (f32) hipLaunchKernelGGL(linear_pack_kernel<float>, grid, dim3(256), 0, s, from, pitch, (uint32_t)c.k, reinterpret_cast<td_u32x4*>(to), rows, units);
+        else hipLaunchKernelGGL(linear_pack_kernel<bf16_t>, grid, dim3(256), 0, s, from, pitch, (uint32_t)c.k, reinterpret_cast<td_u32x4*>(to), rows, units);
+        return to;
+    };
+    if (plan.pack_x) p.x = pack(p.x, c.pitch, c.x_rows, memory);
+    if (plan.pack_W) p.W = pack(p.W, c.k, p.N * std::max(p.experts, 1), memory + plan.at_W);
+    p.k = (uint32_t)plan.k;
+    p.x_pitch = plan.pitch;
+    p.x_bytes = (c.x_rows - 1) * p.x_pitch + p.k;
     LinearArgs q = p;
-    if (c.splits > 1) {
-        q.part = static_cast<float*>(work);
+    if (plan.splits > 1) {
+        q.part = reinterpret_cast<float*>(memory + plan.at_part);
         q.act = TARDIS_ACT_IDENTITY;
     }
     const int blocks = (int)((tiles + 7) / 8 * 8);
-    if (dtype == TARDIS_F32) td_linear_launch_f32(q, grouped, direct, c.shape, blocks, s);
-    else td_linear_launch_bf16(q, grouped, direct, c.shape, blocks, s);
-    if (c.splits > 1) {
+    if (quad) td_linear_launch_quad(q, grouped, plan.shape - kLinearShapes, blocks, s);
+    else if (f32) td_linear_launch_f32(q, grouped, plan.direct, plan.shape, blocks, s);
+    else td_linear_launch_bf16(q, grouped, plan.direct, plan.shape, blocks, s);
+    if (plan.splits > 1) {
         p.part = q.part;
-        const int64_t units = (p.N + 3) / 4, n = (units * p.n + 255) / 256;
-        if (dtype == TARDIS_F32) hipLaunchKernelGGL(linear_join_kernel<float>, dim3((unsigned)n), dim3(256), 0, s, p, units);
-        else hipLaunchKernelGGL(linear_join_kernel<bf16_t>, dim3((unsigned)n), dim3(256), 0, s, p, units);
+        const int64_t units = (p.N + 3) / 4;
+        const dim3 grid((unsigned)((units * p.n + 255) / 256));
+        if (f32) hipLaunchKernelGGL(linear_join_kernel<float>, grid, dim3(256), 0, s, p, (uint32_t)units);
+        else hipLaunchKernelGGL(linear_join_kernel<bf16_t>, grid, dim3(256), 0, s, p, (uint32_t)units);
     }
     TD_HIP(hipGetLastError());
     return TARDIS_OK;
@@ -89,46 +235,46 @@ LinearArgs layer(const tardis_linear_desc* d) {
     p.b = d->b;
     p.N = d->n_out;
     p.k = (uint32_t)(d->n_in * (int64_t)td_elem_size(d->dtype));
-    p.act = d->act;
+    p.act = d->act == TARDIS_ACT_GELU_ERF && d->out_dtype == TARDIS_BF16 ? kActGelu16 : d->act;
     p.out_f32 = d->out_dtype == TARDIS_F32;
     return p;
 }
 
+Call call_of(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, bool gather, int64_t rows) {
+    const int64_t es = (int64_t)td_elem_size(d->dtype);
+    return {rows, d->n_out, x_rows, d->n_in * es, x_pitch * es, (int)es, (int)td_elem_size(d->out_dtype), d->act, (int)experts, gather,
+            is_aligned16(x), is_aligned16(d->W)};
+}
+
+constexpr int64_t kAnyRoom = (int64_t)1 << 62;
+
 }  // namespace
 
-size_t td_linear_work_bytes(const tardis_linear_desc* d, int64_t n) {
-    (void)d;
-    (void)n;
-    return 0;
+int64_t td_linear_work_bytes(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, bool gather, int64_t rows) {
+    return make_plan(call_of(d, experts, x, x_rows, x_pitch, gather, rows), kAnyRoom).work;
 }
 
 tardis_status_t td_linear(const tardis_linear_desc* d, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y, void* work,
                           int64_t work_bytes, hipStream_t s) {
-    const int64_t es = (int64_t)td_elem_size(d->dtype);
     LinearArgs p = layer(d);
     p.x = bytes_of(x);
     p.r = residual;
     p.y = y;
     p.n = p.x_rows = n;
-    p.x_pitch = x_pitch * es;
-    p.x_bytes = (n - 1) * p.x_pitch + p.k;
-    return run(p, d->dtype, false, work, work_bytes, s);
+    return run(p, d->dtype, call_of(d, 0, x, n, x_pitch, false, n), work, work_bytes, s);
 }
 
 tardis_status_t td_grouped_linear(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, const int32_t* offsets,
-                                  const int32_t* order, int64_t per_token, int64_t positions, void* y, hipStream_t s) {
-    const int64_t es = (int64_t)td_elem_size(d->dtype);
+                                  const int32_t* order, int64_t per_token, int64_t positions, void* y, void* work, int64_t work_bytes, hipStream_t s) {
     LinearArgs p = layer(d);
     p.x = bytes_of(x);
     p.y = y;
     p.n = positions;
     p.x_rows = x_rows;
-    p.x_pitch = x_pitch * es;
-    p.x_bytes = (x_rows - 1) * p.x_pitch + p.k;
     p.offsets = offsets;
     p.order = order;
     p.experts = (int)experts;
     p.per_token = (int)per_token;
     p.inv_per_token = per_token > 1 ? (uint32_t)(0x100000000ull / (uint64_t)per_token) : 0xffffffffu;
-    return run(p, d->dtype, true, nullptr, 0, s);
+    return run(p, d->dtype, call_of(d, experts, x, x_rows, x_pitch, order != nullptr, positions), work, work_bytes, s);
 }

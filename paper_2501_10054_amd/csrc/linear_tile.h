@@ -1,8 +1,7 @@
 // y = sigma(x W^T + b) + r for one weight matrix, or for one of several by groups of rows (mixture of experts): the kernel, for one
 // element type of x, W and b (linear_bf16.hip, linear_f32.hip); which tile a call takes is linear.hip's.
 #pragma once
-#include "linear.h"
-#include "sigma.h"
+#include "linear_act.h"
 #include "tiles.h"
 
 namespace {
@@ -49,7 +48,19 @@ __device__ __forceinline__ void tile_of(uint32_t t, uint32_t tiles_m, uint32_t t
 struct LinearBlock {
     int64_t first, n0;
     int rows, expert, s0, nk, range;
+    bool once;                                            // no other block reads its rows of W
 };
+
+// The whole slice that a block starts with.  Blocks that share slices start within a window of 8 of them; where each has rows of W to
+// itself they spread over the whole row, and W's lines are not kept (16384 x 4096, 16 x 32 tiles, us: 27.3; lines not kept 26.8, spread 25.0, both
+// 23.4; 4096 x 11008, 16 x 16: 18.8, 18.1, 19.8, 18.8)
+__device__ __forceinline__ int start_of(const LinearBlock& b, int whole) {
+    const int xcd = (int)blockIdx.x & 7, local = (int)blockIdx.x >> 3;
+    if (!b.once || whole < 8) return first_slice(xcd, local, whole);
+    uint32_t at;
+    divide((uint32_t)(local + xcd * whole / 8), (uint32_t)whole, at);
+    return uniform((int)at);
+}
 
 // Number `t` of `all` tiles for block b: an XCD (blocks b, b + 8, ...) has consecutive ones.  false: none
 __device__ __forceinline__ bool number_of(uint32_t block, uint32_t all, uint32_t& t) {
@@ -106,6 +117,7 @@ template <int TM> __device__ __forceinline__ bool find_group(const LinearArgs& p
             b.expert = c + at;
             b.first = from + (int64_t)tile_m * TM;
             b.rows = min(TM, rows - tile_m * TM);
+            b.once = tiles == 1;
             return true;
         }
         before += (uint32_t)__builtin_amdgcn_readlane(sum, 63);
@@ -114,27 +126,138 @@ template <int TM> __device__ __forceinline__ bool find_group(const LinearArgs& p
 }
 
 // The tile of a block: TM = 16 FA WM rows (tokens) x TN = 16 FB WN columns (rows of W), 8 wavefronts in a grid of WM x WN, times WK that
-// divide K: a slice is 64 WK bytes of every row, of which a wavefront multiplies 64, and every fragment of a slice is
-// read from LDS by WN (of W: WM) wavefronts only.  D slices are in LDS.
-template <typename T, bool DIRECT, int FA, int FB, int WM, int WN, int WK, int D>
+// divide K: a slice is 64 WK KS bytes of every row, of which a wavefront multiplies 64 KS, and every fragment of a slice is
+// read from LDS by WN (of W: WM) wavefronts only.  D slices are in LDS (DIRECT) or in registers, on their way to two in LDS.
+template <typename T, bool DIRECT, int FA, int FB, int WM, int WN, int WK, int KS, int D>
 struct LinearTile {
-    static constexpr int TM = 16 * FA * WM, TN = 16 * FB * WN, SL = 64 * WK;
+    static constexpr int TM = 16 * FA * WM, TN = 16 * FB * WN, SL = 64 * WK * KS;
     static constexpr int UA = TM * SL, UB = TN * SL, LA = UA / 8192, LB = UB / 8192;    // bytes of a slice, loads (16 bytes a lane) of a wavefront
-    static constexpr int kRing = D * (UA + UB);
+    static constexpr int kRing = (DIRECT ? D : 2) * (UA + UB);
     // row blocks of a wavefront that pass through LDS at a time behind the products: as many as the ring has room for
     static constexpr int kRowBytes = WK * WM * 16 * TN * 4;
     static constexpr int fit(int n) { return n == 1 || (FA % n == 0 && n * kRowBytes <= kRing) ? n : fit(n - 1); }
     static constexpr int RB = fit(FA), kLds = RB * kRowBytes > kRing ? RB * kRowBytes : kRing;
     static_assert(WM * WN * WK == 8 && UA % 8192 == 0 && UB % 8192 == 0 && kLds <= kLdsBytes, "eight wavefronts, whole loads");
-    static_assert(DIRECT ? D >= 3 && (D - 1) * (LA + LB) <= 63 : D == 2, "slices in LDS");
+    static_assert(DIRECT ? D >= 3 && (D - 1) * (LA + LB) <= 63 : D % 2 == 0, "slices under way");
 };
+
+// the row of x that is row m of this block's; -1: none
+template <bool GROUPED> __device__ __forceinline__ int64_t token_of_row(const LinearArgs& p, const LinearBlock& b, int m) {
+    if (m >= b.rows) return -1;
+    if (!GROUPED || !p.order) return b.first + m;
+    const uint32_t slot = (uint32_t)p.order[b.first + m];
+    uint32_t token = __umulhi(slot, p.inv_per_token);       // the quotient, or one less
+    if (slot - token * (uint32_t)p.per_token >= (uint32_t)p.per_token) ++token;
+    return (int64_t)token < p.x_rows ? (int64_t)token : -1; // (a negative slot is a large token)
+}
+
+// What follows the products of W wavefronts in a grid of WM x WN, times WK that divide K.
+// acc[i][j][q] = row (wm FA + i) 16 + lane % 16, column (wn FB + j) 16 + 4 (lane / 16) + q of the tile.  RB row blocks of a wavefront at a time
+// pass through LDS, where the parts of K meet (WK = 1: every wavefront's own), so that a store covers whole lines of a row and that what
+// is done to the elements is a loop; a thread finishes 8 neighbouring columns at once.
+template <typename T, bool GROUPED, int W, int FA, int FB, int WM, int WN, int WK, int RB>
+__device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearBlock& b, f32x4_t (&acc)[FA][FB], unsigned char* lds, int tid) {
+    constexpr bool OWN = WK == 1;
+    static constexpr int kAtOnce = OWN ? 2 : 1;                  // (one wavefront on a SIMD: two rows side by side; 2048 x 16384 x 4096 210 -> 195 us)
+    constexpr int COLS = OWN ? FB * 16 : WN * FB * 16, ROWS = OWN ? RB * 16 : WM * RB * 16, UNITS = COLS / 8, STRIDE = (OWN ? 64 : W * 64) / UNITS;
+    const int lane = tid & 63, wave = uniform(tid >> 6), wk = wave % WK, wn = wave / WK % WN, wm = wave / WK / WN, frow = lane & 15, fp = lane >> 4;
+    const int me = OWN ? lane : tid, unit = me % UNITS;
+    float* stage = reinterpret_cast<float*>(lds) + (OWN ? wave * ROWS * COLS : 0);
+    auto place_of = [&](int part, int row, int piece) { return (part * ROWS + row) * COLS + ((piece ^ (row & 15 & (COLS / 4 - 1))) * 4); };
+    auto sync = [&]() {
+        if constexpr (OWN) __builtin_amdgcn_wave_barrier();
+        else __syncthreads();
+    };
+    const int64_t n = b.n0 + (OWN ? wn * COLS : 0) + unit * 8;
+    const int columns = (int)min((int64_t)8, p.N - n);    // (of this thread; none or less: none)
+    auto load8 = [&](const void* from, int64_t at, bool f32, float (&v)[8]) {
+        if (columns >= 8) {
+            if (f32) {
+                const td_u32x4 lo = load_any16(static_cast<const float*>(from) + at), hi = load_any16(static_cast<const float*>(from) + at + 4);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    v[q] = __uint_as_float(lo[q]);
+                    v[4 + q] = __uint_as_float(hi[q]);
+                }
+            } else {
+                const td_u32x4 w = load_any16(static_cast<const bf16_t*>(from) + at);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    v[2 * q] = __uint_as_float(w[q] << 16);
+                    v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 8; ++q)
+                v[q] = q >= columns ? 0.0f : f32 ? static_cast<const float*>(from)[at + q] : td_bf16_to_f32(static_cast<const bf16_t*>(from)[at + q]);
+        }
+    };
+    float bias[8] = {};
+    if (p.b && !p.part && columns > 0) load8(p.b, (int64_t)b.expert * p.N + n, sizeof(T) == 4, bias);
+    for_constants<FA / RB>([&](auto batch) {
+        constexpr int i0 = decltype(batch)::value * RB;
+        if constexpr (i0 > 0) sync();
+#pragma unroll
+        for (int i = 0; i < RB; ++i)
+#pragma unroll
+            for (int j = 0; j < FB; ++j)
+                *reinterpret_cast<f32x4_t*>(stage + place_of(wk, ((OWN ? 0 : wm * RB) + i) * 16 + frow, ((OWN ? 0 : wn * FB) + j) * 4 + fp)) = acc[i0 + i][j];
+        sync();
+        with_linear_act(p.act, [&](auto act) {
+#pragma unroll kAtOnce
+            for (int at = me / UNITS; at < ROWS; at += STRIDE) {
+                const int m = OWN ? (wm * FA + i0) * 16 + at : (at / (RB * 16) * FA + i0) * 16 + at % (RB * 16);   // row of the tile
+                if (m >= b.rows || columns <= 0) continue;
+                if (GROUPED && p.order && token_of_row<GROUPED>(p, b, m) < 0) continue;
+                const int64_t row = b.first + m, to = row * p.N + n;
+                float r[8] = {}, v[8];
+                if (p.r && !p.part) load8(p.r, to, p.out_f32, r);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    f32x4_t sum = *reinterpret_cast<const f32x4_t*>(stage + place_of(0, at, unit * 2 + h));
+#pragma unroll
+                    for (int part = 1; part < WK; ++part) sum += *reinterpret_cast<const f32x4_t*>(stage + place_of(part, at, unit * 2 + h));
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) v[4 * h + q] = sum[q];
+                }
+                if (!p.part) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) v[q] = linear_act<decltype(act)::value>(v[q] + bias[q]) + r[q];
+                }
+                if (p.part || p.out_f32) {
+                    float* y = p.part ? p.part + (int64_t)b.range * p.n * p.N + to : static_cast<float*>(p.y) + to;
+                    if (columns >= 8) {
+                        store_any16(y, td_u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+                        store_any16(y + 4, td_u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            if (q < columns) y[q] = v[q];
+                    }
+                } else {
+                    bf16_t* y = static_cast<bf16_t*>(p.y) + to;
+                    const td_u32x4 o = {to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
+                    if (columns >= 8) {
+                        store_any16(y, o);
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 8; ++q)
+                            if (q < columns) y[q] = (bf16_t)(o[q / 2] >> (16 * (q & 1)));
+                    }
+                }
+            }
+        });
+    });
+}
+
 
 // What bounds it: few rows - the weights' stream from HBM; many - the way from L2 to LDS (tiles below 192 x 128) and the matrix cores.
 // DIRECT: x and W in whole, aligned pieces of 16 bytes, which go from memory straight to LDS; D - 1 slices are under way.  Else (odd
-// widths, odd pitches, rows that are 4 GB apart): through registers, two slices ahead, whatever the alignment.
-template <typename T, bool GROUPED, bool DIRECT, int FA, int FB, int WM, int WN, int WK, int D>
+// widths, odd pitches, rows that are 4 GB apart): through registers, D slices ahead, whatever the alignment.
+template <typename T, bool GROUPED, bool DIRECT, int FA, int FB, int WM, int WN, int WK, int KS, int D>
 __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
-    typedef LinearTile<T, DIRECT, FA, FB, WM, WN, WK, D> G;
+    typedef LinearTile<T, DIRECT, FA, FB, WM, WN, WK, KS, D> G;
     constexpr int TM = G::TM, TN = G::TN, SL = G::SL, LA = G::LA, LB = G::LB, PS = SL / 16, RPL = 64 / PS, SWZ = PS < 16 ? PS - 1 : 15;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -158,50 +281,50 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
         b.rows = (int)min((int64_t)TM, p.n - b.first);
         b.s0 = b.range * p.slices;
         b.nk = max(0, min(p.slices, slices - b.s0));
+        b.once = p.tiles_m == 1;
     }
     b.n0 = (int64_t)tile_n * TN;
     const int rows_w = (int)min((int64_t)TN, p.N - b.n0);
     const unsigned char* W = p.W + ((size_t)b.expert * p.N + b.n0) * p.k;
     // whole slices from a starting point of this block's own, then one that is not whole
     const int whole = max(0, min(b.nk, (int)(p.k / SL) - b.s0));
-    const int rot = first_slice((int)blockIdx.x & 7, (int)blockIdx.x >> 3, whole);
+    const int rot = start_of(b, whole);
     auto slice_of = [&](int t) { return b.s0 + (t >= whole ? t : t + rot >= whole ? t + rot - whole : t + rot); };
 
     // A load is RPL rows x SL bytes: lane -> row lane / PS, slot lane % PS, which holds piece slot ^ row (so the 16 rows of a fragment
     // hit all banks).  Wavefront w loads rows [w TM / 8, (w + 1) TM / 8) of x, of W alike.
     const int row_a = wave * (TM / 8) + lane / PS, row_b = wave * (TN / 8) + lane / PS;
     auto piece_of_row = [&](int row) { return (uint32_t)((lane % PS) ^ (row & SWZ)) * 16u; };
-    // the row of x that is row m of this block's; -1: none
-    auto token_of = [&](int m) -> int64_t {
-        if (m >= b.rows) return -1;
-        if (!GROUPED || !p.order) return b.first + m;
-        const uint32_t slot = (uint32_t)p.order[b.first + m];
-        uint32_t token = __umulhi(slot, p.inv_per_token);   // the quotient, or one less
-        if (slot - token * (uint32_t)p.per_token >= (uint32_t)p.per_token) ++token;
-        return (int64_t)token < p.x_rows ? (int64_t)token : -1;   // (a negative slot is a large token)
-    };
+    auto token_of = [&](int m) { return token_of_row<GROUPED>(p, b, m); };
 
     f32x4_t acc[FA][FB];
 #pragma unroll
     for (int i = 0; i < FA; ++i)
 #pragma unroll
         for (int j = 0; j < FB; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
-    // fragments: lane holds 16 bytes of row lane % 16 at piece 4 wk + lane / 16 of a slice
-    const uint32_t frag = (uint32_t)(frow * SL + (((4 * wk + fp) ^ (frow & SWZ)) * 16));
+    // fragments: lane holds 16 bytes of row lane % 16 at piece 4 (wk + WK step) + lane / 16 of a slice
+    uint32_t frag[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) frag[s] = (uint32_t)(frow * SL + (((4 * (wk + WK * s) + fp) ^ (frow & SWZ)) * 16));
     struct Fragments {
-        td_u32x4 a[FA], b[FB];
+        td_u32x4 a[KS][FA], b[KS][FB];
     };
     auto read = [&](Fragments& f, const unsigned char* at_a, const unsigned char* at_b) {
 #pragma unroll
-        for (int i = 0; i < FA; ++i) f.a[i] = *reinterpret_cast<const td_u32x4*>(at_a + (wm * FA + i) * (16 * SL) + frag);
+        for (int s = 0; s < KS; ++s) {
 #pragma unroll
-        for (int j = 0; j < FB; ++j) f.b[j] = *reinterpret_cast<const td_u32x4*>(at_b + (wn * FB + j) * (16 * SL) + frag);
+            for (int i = 0; i < FA; ++i) f.a[s][i] = *reinterpret_cast<const td_u32x4*>(at_a + (wm * FA + i) * (16 * SL) + frag[s]);
+#pragma unroll
+            for (int j = 0; j < FB; ++j) f.b[s][j] = *reinterpret_cast<const td_u32x4*>(at_b + (wn * FB + j) * (16 * SL) + frag[s]);
+        }
     };
     auto multiply = [&](const Fragments& f) {
 #pragma unroll
-        for (int i = 0; i < FA; ++i)
+        for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int j = 0; j < FB; ++j) mma_pieces<T>(acc[i][j], f.b[j], f.a[i]);
+            for (int i = 0; i < FA; ++i)
+#pragma unroll
+                for (int j = 0; j < FB; ++j) mma_pieces<T>(acc[i][j], f.b[s][j], f.a[s][i]);
     };
 
     if constexpr (DIRECT) {
@@ -251,8 +374,13 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
                     load_to_lds(to_a + slot * G::UA + i * 1024u, off_a[i] - (pc < last ? 0u : pc), a, soff);
                 }
             } else {
+                if (b.once) {
 #pragma unroll
-                for (int i = 0; i < LB; ++i) load_to_lds(to_b + slot * G::UB + i * 1024u, off_b[i], w, soff);
+                    for (int i = 0; i < LB; ++i) load_to_lds<true>(to_b + slot * G::UB + i * 1024u, off_b[i], w, soff);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < LB; ++i) load_to_lds(to_b + slot * G::UB + i * 1024u, off_b[i], w, soff);
+                }
 #pragma unroll
                 for (int i = 0; i < LA; ++i) load_to_lds(to_a + slot * G::UA + i * 1024u, off_a[i], a, soff);
             }
@@ -269,12 +397,15 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
         auto fetch = [&](Fragments& f, int t) {
             read(f, lds + slot * G::UA, lds + D * G::UA + slot * G::UB);
             if (t >= whole) {                             // a slice that is not whole: what the row has not is zero
-                const uint32_t at = (uint32_t)slice_of(t) * SL + (uint32_t)(4 * wk + fp) * 16u;
                 const td_u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < FA; ++i) f.a[i] = at < p.k ? f.a[i] : zero;
+                for (int s = 0; s < KS; ++s) {
+                    const bool in = (uint32_t)slice_of(t) * SL + (uint32_t)(4 * (wk + WK * s) + fp) * 16u < p.k;
 #pragma unroll
-                for (int j = 0; j < FB; ++j) f.b[j] = at < p.k ? f.b[j] : zero;
+                    for (int i = 0; i < FA; ++i) f.a[s][i] = in ? f.a[s][i] : zero;
+#pragma unroll
+                    for (int j = 0; j < FB; ++j) f.b[s][j] = in ? f.b[s][j] : zero;
+                }
             }
         };
         Fragments f[2];
@@ -297,162 +428,84 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
         }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     } else {
-        const unsigned char *from_a[LA], *from_b[LB];     // (rows that are not there: null)
+        // (for rows that are not there the first one's, of which nothing is kept: the loop has no branches, so that a load is waited
+        // for when it is used and not where paths meet)
+        const unsigned char *from_a[LA], *from_b[LB];
 #pragma unroll
-        for (int i = 0; i < LA; ++i) {
-            const int64_t token = token_of(row_a + i * RPL);
-            from_a[i] = token < 0 ? nullptr : p.x + token * p.x_pitch + piece_of_row(row_a + i * RPL);
-        }
+        for (int i = 0; i < LA; ++i) from_a[i] = p.x + max(token_of(row_a + i * RPL), (int64_t)0) * p.x_pitch + piece_of_row(row_a + i * RPL);
 #pragma unroll
         for (int i = 0; i < LB; ++i) {
             const int row = row_b + i * RPL;
-            from_b[i] = row < rows_w ? W + (size_t)row * p.k + piece_of_row(row) : nullptr;
+            from_b[i] = W + (size_t)(row < rows_w ? row : 0) * p.k + piece_of_row(row);
         }
         struct Pieces {
             td_u32x4 a[LA], b[LB];
         };
-        auto load_piece = [&](const unsigned char* from, uint32_t soff, uint32_t pc) {
-            const td_u32x4 zero = {0, 0, 0, 0};
-            if (!from || soff + pc >= p.k) return zero;
-            if (soff + pc + 16 <= p.k) return load_any16(from + soff);
-            td_u32x4 v = zero;                            // the row's last elements
-            const T* el = reinterpret_cast<const T*>(from + soff);
-            const uint32_t n = (p.k - soff - pc) / sizeof(T);
+        auto to_lds = [&](const Pieces& v, int place) {
+            unsigned char* at = lds + wave * (G::UA / 8) + place * G::UA + lane * 16;
 #pragma unroll
-            for (uint32_t u = 0; u < 16 / sizeof(T); ++u)
-                if (u < n) {
-                    if constexpr (sizeof(T) == 2) v[u / 2] |= (uint32_t)el[u] << (16 * (u & 1));
-                    else v[u] = __float_as_uint(el[u]);
-                }
-            return v;
+            for (int i = 0; i < LA; ++i) *reinterpret_cast<td_u32x4*>(at + i * 1024) = v.a[i];
+            at = lds + 2 * G::UA + wave * (G::UB / 8) + place * G::UB + lane * 16;
+#pragma unroll
+            for (int i = 0; i < LB; ++i) *reinterpret_cast<td_u32x4*>(at + i * 1024) = v.b[i];
         };
-        auto load_slice = [&](Pieces& v, int t) {
-            if (t >= b.nk) return;
-            const uint32_t soff = (uint32_t)slice_of(t) * SL;
-            if (t < whole) {
-                const td_u32x4 zero = {0, 0, 0, 0};
+        auto load_slice = [&](Pieces& v, int t) {         // (past the last whole slice: that one again)
+            const uint32_t soff = (uint32_t)slice_of(min(t, whole - 1)) * SL;
 #pragma unroll
-                for (int i = 0; i < LB; ++i) v.b[i] = from_b[i] ? load_any16(from_b[i] + soff) : zero;
+            for (int i = 0; i < LB; ++i) v.b[i] = load_any16(from_b[i] + soff);
 #pragma unroll
-                for (int i = 0; i < LA; ++i) v.a[i] = from_a[i] ? load_any16(from_a[i] + soff) : zero;
-            } else {
-#pragma unroll
-                for (int i = 0; i < LB; ++i) v.b[i] = load_piece(from_b[i], soff, piece_of_row(row_b + i * RPL));
-#pragma unroll
-                for (int i = 0; i < LA; ++i) v.a[i] = load_piece(from_a[i], soff, piece_of_row(row_a + i * RPL));
-            }
+            for (int i = 0; i < LA; ++i) v.a[i] = load_any16(from_a[i] + soff);
         };
-        Pieces v[2];
+        Pieces v[D];
         auto step = [&](Pieces& now, int t) {             // (the place in LDS was read two slices ago, before the last barrier)
-            unsigned char* at_a = lds + (t & 1) * G::UA;
-            unsigned char* at_b = lds + 2 * G::UA + (t & 1) * G::UB;
-#pragma unroll
-            for (int i = 0; i < LA; ++i) *reinterpret_cast<td_u32x4*>(at_a + wave * (G::UA / 8) + i * 1024 + lane * 16) = now.a[i];
-#pragma unroll
-            for (int i = 0; i < LB; ++i) *reinterpret_cast<td_u32x4*>(at_b + wave * (G::UB / 8) + i * 1024 + lane * 16) = now.b[i];
+            const int place = t & 1;
+            to_lds(now, place);
             __syncthreads();
-            load_slice(now, t + 2);
+            load_slice(now, t + D);
             Fragments f;
-            read(f, at_a, at_b);
+            read(f, lds + place * G::UA, lds + 2 * G::UA + place * G::UB);
             multiply(f);
         };
-        load_slice(v[0], 0);
-        load_slice(v[1], 1);
+        if (whole > 0) {
+#pragma unroll
+            for (int u = 0; u < D; ++u) load_slice(v[u], u);
+            int t = 0;
 #pragma unroll 1
-        for (int t = 0; t < b.nk; t += 2) {
-            step(v[0], t);
-            if (t + 1 < b.nk) step(v[1], t + 1);
+            for (; t + D <= whole; t += D)
+#pragma unroll
+                for (int u = 0; u < D; ++u) step(v[u], t + u);
+#pragma unroll
+            for (int u = 0; u < D; ++u)
+                if (t + u < whole) step(v[u], t + u);
+        }
+        if (whole < b.nk) {                               // a slice that is not whole: element by element, zeros behind the row's end
+            const uint32_t soff = (uint32_t)slice_of(whole) * SL;
+            auto load_piece = [&](const unsigned char* from, uint32_t pc) {
+                td_u32x4 w = {0, 0, 0, 0};
+                const T* el = reinterpret_cast<const T*>(from + soff);
+                const uint32_t n = soff + pc < p.k ? (p.k - soff - pc) / sizeof(T) : 0u;
+#pragma unroll
+                for (uint32_t u = 0; u < 16 / sizeof(T); ++u)
+                    if (u < n) {
+                        if constexpr (sizeof(T) == 2) w[u / 2] |= (uint32_t)el[u] << (16 * (u & 1));
+                        else w[u] = __float_as_uint(el[u]);
+                    }
+                return w;
+            };
+#pragma unroll
+            for (int i = 0; i < LB; ++i) v[0].b[i] = load_piece(from_b[i], piece_of_row(row_b + i * RPL));
+#pragma unroll
+            for (int i = 0; i < LA; ++i) v[0].a[i] = load_piece(from_a[i], piece_of_row(row_a + i * RPL));
+            to_lds(v[0], whole & 1);
+            __syncthreads();
+            Fragments f;
+            read(f, lds + (whole & 1) * G::UA, lds + 2 * G::UA + (whole & 1) * G::UB);
+            multiply(f);
         }
     }
     __syncthreads();
 
-    // acc[i][j][q] = row (wm FA + i) 16 + lane % 16, column (wn FB + j) 16 + 4 (lane / 16) + q of the tile.  The parts of K meet in LDS, some
-    // row blocks at a time; a thread finishes 8 neighbouring columns at once.
-    constexpr int RB = G::RB, UNITS = TN / 8, STRIDE = 512 / UNITS;
-    float* stage = reinterpret_cast<float*>(lds);
-    auto place_of = [&](int part, int row, int piece) { return (part * (WM * RB * 16) + row) * TN + ((piece ^ (row & 15 & (TN / 4 - 1))) * 4); };
-    const int unit = tid % UNITS;
-    const int64_t n = b.n0 + unit * 8;
-    const int columns = (int)min((int64_t)8, p.N - n);    // (of this thread; none or less: none)
-    auto load8 = [&](const void* from, int64_t at, bool f32, float (&v)[8]) {
-        if (columns >= 8) {
-            if (f32) {
-                const td_u32x4 lo = load_any16(static_cast<const float*>(from) + at), hi = load_any16(static_cast<const float*>(from) + at + 4);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v[q] = __uint_as_float(lo[q]);
-                    v[4 + q] = __uint_as_float(hi[q]);
-                }
-            } else {
-                const td_u32x4 w = load_any16(static_cast<const bf16_t*>(from) + at);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v[2 * q] = __uint_as_float(w[q] << 16);
-                    v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
-                }
-            }
-        } else {
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-                v[q] = q >= columns ? 0.0f : f32 ? static_cast<const float*>(from)[at + q] : td_bf16_to_f32(static_cast<const bf16_t*>(from)[at + q]);
-        }
-    };
-    float bias[8] = {};
-    if (p.b && !p.part && columns > 0) load8(p.b, (int64_t)b.expert * p.N + n, sizeof(T) == 4, bias);
-    for_constants<FA / RB>([&](auto batch) {
-        constexpr int i0 = decltype(batch)::value * RB;
-        if constexpr (i0 > 0) __syncthreads();
-#pragma unroll
-        for (int i = 0; i < RB; ++i)
-#pragma unroll
-            for (int j = 0; j < FB; ++j)
-                *reinterpret_cast<f32x4_t*>(stage + place_of(wk, (wm * RB + i) * 16 + frow, (wn * FB + j) * 4 + fp)) = acc[i0 + i][j];
-        __syncthreads();
-        with_act(p.act, [&](auto act) {
-#pragma unroll 1
-            for (int at = tid / UNITS; at < WM * RB * 16; at += STRIDE) {
-                const int m = (at / (RB * 16) * FA + i0) * 16 + at % (RB * 16);       // row of the tile
-                if (m >= b.rows || columns <= 0) continue;
-                if (GROUPED && p.order && token_of(m) < 0) continue;
-                const int64_t row = b.first + m, to = row * p.N + n;
-                float r[8] = {}, v[8];
-                if (p.r && !p.part) load8(p.r, to, p.out_f32, r);
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    f32x4_t sum = *reinterpret_cast<const f32x4_t*>(stage + place_of(0, at, unit * 2 + h));
-#pragma unroll
-                    for (int part = 1; part < WK; ++part) sum += *reinterpret_cast<const f32x4_t*>(stage + place_of(part, at, unit * 2 + h));
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) v[4 * h + q] = sum[q];
-                }
-                if (!p.part) {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) v[q] = act_flat<decltype(act)::value>(v[q] + bias[q]) + r[q];
-                }
-                if (p.part || p.out_f32) {
-                    float* y = p.part ? p.part + (int64_t)b.range * p.n * p.N + to : static_cast<float*>(p.y) + to;
-                    if (columns >= 8) {
-                        store_any16(y, td_u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
-                        store_any16(y + 4, td_u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
-                    } else {
-#pragma unroll
-                        for (int q = 0; q < 8; ++q)
-                            if (q < columns) y[q] = v[q];
-                    }
-                } else {
-                    bf16_t* y = static_cast<bf16_t*>(p.y) + to;
-                    const td_u32x4 o = {to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
-                    if (columns >= 8) {
-                        store_any16(y, o);
-                    } else {
-#pragma unroll
-                        for (int q = 0; q < 8; ++q)
-                            if (q < columns) y[q] = (bf16_t)(o[q / 2] >> (16 * (q & 1)));
-                    }
-                }
-            }
-        });
-    });
+    finish_linear<T, GROUPED, 8, FA, FB, WM, WN, WK, G::RB>(p, b, acc, lds, tid);
 }
 
 }  // namespace
@@ -463,23 +516,27 @@ namespace {
 template <typename F> void for_linear_shape(bool direct, int shape, F f) {
     if (direct) {
         switch (shape) {
-            case 0: f(std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<5>{}); break;
-            case 1: f(std::true_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<3>{}); break;
-            case 2: f(std::true_type{}, num<1>{}, num<4>{}, num<1>{}, num<1>{}, num<8>{}, num<4>{}); break;
-            case 3: f(std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<5>{}); break;
-            case 4: f(std::true_type{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<6>{}); break;
-            case 5: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}, num<6>{}); break;
-            case 6: f(std::true_type{}, num<4>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<5>{}); break;
-            case 7: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<5>{}); break;
-            case 8: f(std::true_type{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<6>{}); break;
-            case 9: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<5>{}); break;
-            default: f(std::true_type{}, num<6>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<4>{}); break;
+            case 0: f(std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<5>{}); break;
+            case 1: f(std::true_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<3>{}); break;
+            case 2: f(std::true_type{}, num<1>{}, num<4>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<4>{}); break;
+            case 3: f(std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<5>{}); break;
+            case 4: f(std::true_type{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<6>{}); break;
+            case 5: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}, num<1>{}, num<6>{}); break;
+            case 6: f(std::true_type{}, num<4>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<5>{}); break;
+            case 7: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<5>{}); break;
+            case 8: f(std::true_type{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<6>{}); break;
+            case 9: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<5>{}); break;
+            case 10: f(std::true_type{}, num<6>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}); break;
+            case 11: f(std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<2>{}, num<5>{}); break;
+            default: f(std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<2>{}, num<5>{}); break;
         }
     } else {
         switch (shape) {
-            case 0: f(std::false_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<2>{}); break;
-            case 1: f(std::false_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}); break;
-            default: f(std::false_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}); break;
+            case 0: f(std::false_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<6>{}); break;
+            case 1: f(std::false_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<4>{}); break;
+            case 2: f(std::false_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<4>{}); break;
+            case 3: f(std::false_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}); break;
+            default: f(std::false_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}); break;
         }
     }
 }
@@ -488,24 +545,24 @@ template <typename T> tardis_status_t linear_init() {
     bool ok = true;
     for (int direct = 0; direct < 2; ++direct)
         for (int shape = 0; shape < (direct ? kLinearShapes : kLinearStagedShapes); ++shape)
-            for_linear_shape(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ring) {
-                typedef LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ring> G;
+            for_linear_shape(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
+                typedef LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring> G;
                 const LinearShape& is = direct ? kLinearShape[shape] : kLinearStaged[shape];
                 ok &= is.m == G::TM && is.n == G::TN && is.slice == G::SL;
                 auto raise = [&](auto kernel) {
                     ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds) == hipSuccess;
                 };
-                raise(linear_kernel<T, false, decltype(d)::value, fa, fb, wm, wn, wk, ring>);
-                raise(linear_kernel<T, true, decltype(d)::value, fa, fb, wm, wn, wk, ring>);
+                raise(linear_kernel<T, false, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>);
+                raise(linear_kernel<T, true, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>);
             });
     return ok ? TARDIS_OK : TARDIS_ERR_HIP;
 }
 
 template <typename T> void linear_launch(const LinearArgs& p, bool grouped, bool direct, int shape, int blocks, hipStream_t s) {
-    for_linear_shape(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ring) {
-        constexpr int bytes = LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ring>::kLds;
-        if (grouped) hipLaunchKernelGGL((linear_kernel<T, true, decltype(d)::value, fa, fb, wm, wn, wk, ring>), dim3((unsigned)blocks), dim3(512), bytes, s, p);
-        else hipLaunchKernelGGL((linear_kernel<T, false, decltype(d)::value, fa, fb, wm, wn, wk, ring>), dim3((unsigned)blocks), dim3(512), bytes, s, p);
+    for_linear_shape(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
+        constexpr int bytes = LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>::kLds;
+        if (grouped) hipLaunchKernelGGL((linear_kernel<T, true, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(512), bytes, s, p);
+        else hipLaunchKernelGGL((linear_kernel<T, false, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(512), bytes, s, p);
     });
 }
 

@@ -26,7 +26,7 @@ EXPORTS = (
     "tardis_calibrate", "tardis_calibrate_search", "tardis_estimate_errors", "tardis_assign_thresholds", "tardis_fold", "tardis_ffn_forward", "tardis_ffn_forward_batched",
     "tardis_ffn_forward_static", "tardis_stack_forward", "tardis_dense_forward", "tardis_get_folded", "tardis_get_predictor_state",
     "tardis_get_sketch_groups", "tardis_get_last_outliers", "tardis_get_last_union", "tardis_get_handover", "tardis_set_next_layer",
-    "tardis_linear", "tardis_linear_workspace", "tardis_grouped_linear", "tardis_moe_route", "tardis_moe_route_workspace", "tardis_moe_combine",
+    "tardis_linear", "tardis_linear_workspace", "tardis_grouped_linear", "tardis_grouped_linear_workspace", "tardis_moe_route", "tardis_moe_route_workspace", "tardis_moe_combine",
     "tardis_destroy", "tardis_release_memory", "tardis_status_string", "tardis_version",
 )
 
@@ -82,8 +82,9 @@ def lib() -> C.CDLL:
         L.tardis_get_last_union.argtypes = [vp, i64, vp, vp, vp]
         L.tardis_get_handover.argtypes = [vp, i64, vp, vp]
         L.tardis_linear.argtypes = [C.POINTER(tardis_linear_desc), vp, i64, i64, vp, vp, vp, i64, vp]
-        L.tardis_linear_workspace.argtypes = [C.POINTER(tardis_linear_desc), i64, C.POINTER(i64)]
-        L.tardis_grouped_linear.argtypes = [C.POINTER(tardis_linear_desc), i64, vp, i64, i64, vp, vp, i64, i64, vp, vp]
+        L.tardis_linear_workspace.argtypes = [C.POINTER(tardis_linear_desc), vp, i64, i64, C.POINTER(i64)]
+        L.tardis_grouped_linear.argtypes = [C.POINTER(tardis_linear_desc), i64, vp, i64, i64, vp, vp, i64, i64, vp, vp, i64, vp]
+        L.tardis_grouped_linear_workspace.argtypes = [C.POINTER(tardis_linear_desc), i64, vp, i64, i64, C.c_int32, i64, C.POINTER(i64)]
         L.tardis_moe_route.argtypes = [vp, i64, i64, i64, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp, i64, vp]
         L.tardis_moe_route_workspace.argtypes = [i64, i64, C.POINTER(i64)]
         L.tardis_moe_combine.argtypes = [vp, i64, vp, vp, i64, i64, i64, C.c_int32, vp, vp, C.c_int32, vp]
@@ -318,12 +319,15 @@ def tardis_release_memory():
     _check(lib().tardis_release_memory(), "tardis_release_memory")
 
 
-@functools.lru_cache(maxsize=1024)
-def _linear_work_bytes(n, n_in, n_out, dtype, out_dtype, act):
-    """Of a call of these sizes (weights at an aligned address stand in for those of the call)."""
+@functools.lru_cache(maxsize=4096)
+def _linear_work_bytes(sizes, experts, x_rows, pitch, ordered, rows, x_at, W_at):
+    """Of a call of these sizes (n_in, n_out, dtype, out_dtype, act) with operands at addresses of these remainders by 16."""
     bytes_ = C.c_int64()
-    desc = tardis_linear_desc(n_in, n_out, dtype, out_dtype, act, 0, 256, None)
-    _check(lib().tardis_linear_workspace(desc, n, bytes_), "tardis_linear_workspace")
+    desc = tardis_linear_desc(*sizes, 0, 256 + W_at, None)
+    if experts:
+        _check(lib().tardis_grouped_linear_workspace(desc, experts, 256 + x_at, x_rows, pitch, ordered, rows, bytes_), "tardis_grouped_linear_workspace")
+    else:
+        _check(lib().tardis_linear_workspace(desc, 256 + x_at, rows, pitch, bytes_), "tardis_linear_workspace")
     return bytes_.value
 
 
@@ -355,11 +359,11 @@ def tardis_linear(x, W, b=None, act: str = "identity", residual=None, out_dtype=
         y = torch.empty(n, n_out, dtype=out_dtype, device=x.device)
     else:
         assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, n_out) and y.device == x.device
-    code, out_code, act_code = _DTYPE_CODE[dt], _DTYPE_CODE[out_dtype], ACT[act]
-    desc = tardis_linear_desc(n_in, n_out, code, out_code, act_code, 0, W.data_ptr(), None if b is None else b.data_ptr())
-    bytes_ = _linear_work_bytes(n, n_in, n_out, code, out_code, act_code)
+    sizes, x_at, W_at = (n_in, n_out, _DTYPE_CODE[dt], _DTYPE_CODE[out_dtype], ACT[act]), x.data_ptr(), W.data_ptr()
+    desc = tardis_linear_desc(*sizes, 0, W_at, None if b is None else b.data_ptr())
+    bytes_ = _linear_work_bytes(sizes, 0, n, pitch, 0, n, x_at & 15, W_at & 15)
     work = torch.empty(bytes_, dtype=torch.uint8, device=x.device) if bytes_ else None
-    _check(lib().tardis_linear(desc, x.data_ptr(), n, pitch, _ptr(residual), y.data_ptr(), _ptr(work), bytes_, _stream(stream)), "tardis_linear")
+    _check(lib().tardis_linear(desc, x_at, n, pitch, _ptr(residual), y.data_ptr(), _ptr(work), bytes_, _stream(stream)), "tardis_linear")
     return y
 
 
@@ -379,9 +383,12 @@ def tardis_grouped_linear(x, W, offsets, b=None, act: str = "identity", order=No
         y = torch.empty(positions, n_out, dtype=out_dtype, device=x.device)
     else:
         assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (positions, n_out) and y.device == x.device
-    desc = tardis_linear_desc(n_in, n_out, _DTYPE_CODE[dt], _DTYPE_CODE[out_dtype], ACT[act], 0, W.data_ptr(), None if b is None else b.data_ptr())
-    _check(lib().tardis_grouped_linear(desc, experts, x.data_ptr(), x_rows, pitch, offsets.data_ptr(), _ptr(order), per_token, positions, y.data_ptr(),
-                                       _stream(stream)), "tardis_grouped_linear")
+    sizes, x_at, W_at, ordered = (n_in, n_out, _DTYPE_CODE[dt], _DTYPE_CODE[out_dtype], ACT[act]), x.data_ptr(), W.data_ptr(), order is not None
+    desc = tardis_linear_desc(*sizes, 0, W_at, None if b is None else b.data_ptr())
+    bytes_ = _linear_work_bytes(sizes, experts, x_rows, pitch, int(ordered), positions, x_at & 15, W_at & 15)
+    work = torch.empty(bytes_, dtype=torch.uint8, device=x.device) if bytes_ else None
+    _check(lib().tardis_grouped_linear(desc, experts, x_at, x_rows, pitch, offsets.data_ptr(), _ptr(order), per_token, positions, y.data_ptr(),
+                                       _ptr(work), bytes_, _stream(stream)), "tardis_grouped_linear")
     return y
 
 

@@ -24,8 +24,8 @@ def linear(desc, x=P, n=4, pitch=64, r=None, y=P, work=None, bytes_=0):
     return T.lib().tardis_linear(desc, x, n, pitch, r, y, work, bytes_, None)
 
 
-def grouped(desc, experts=4, x=P, x_rows=8, pitch=64, offsets=P, order=P, per_token=2, positions=16, y=P):
-    return T.lib().tardis_grouped_linear(desc, experts, x, x_rows, pitch, offsets, order, per_token, positions, y, None)
+def grouped(desc, experts=4, x=P, x_rows=8, pitch=64, offsets=P, order=P, per_token=2, positions=16, y=P, work=None, bytes_=0):
+    return T.lib().tardis_grouped_linear(desc, experts, x, x_rows, pitch, offsets, order, per_token, positions, y, work, bytes_, None)
 
 
 def route(logits=P, n=8, experts=16, k=2, dtype=T.F32, renormalise=1, ids=P, weights=P, offsets=P, order=P, place=P, work=None, bytes_=0):
@@ -40,22 +40,24 @@ def combine(z=P, rows=16, place=P, weights=P, n=8, k=2, d=64, dtype=T.BF16, r=No
 def test_bad_descriptions(change, status):
     assert linear(_desc(**change)) == status
     assert grouped(_desc(**change)) == status
-    assert T.lib().tardis_linear_workspace(_desc(**change), 4, C.c_int64()) == status
+    assert T.lib().tardis_linear_workspace(_desc(**change), P, 4, 64, C.c_int64()) == status
+    assert T.lib().tardis_grouped_linear_workspace(_desc(**change), 4, P, 8, 64, 1, 16, C.c_int64()) == status
 
 
 def test_linear_refuses():
     assert linear(None) == T.ERR_INVALID_ARG
     odd = C.c_void_p(0x4001)
-    for kw in (dict(x=None), dict(y=None), dict(x=odd), dict(y=odd), dict(r=odd), dict(work=C.c_void_p(0x4002), bytes_=64), dict(work=P, bytes_=-1)):
+    for kw in (dict(x=None), dict(y=None), dict(x=odd), dict(y=odd), dict(r=odd), dict(work=C.c_void_p(0x4008), bytes_=64), dict(work=P, bytes_=-1)):
         assert linear(_desc(), **kw) == T.ERR_INVALID_ARG, kw
     assert linear(_desc(out_dtype=T.F32), y=C.c_void_p(0x4002)) == T.ERR_INVALID_ARG
     for kw in (dict(n=-1), dict(n=(1 << 30) + 1), dict(pitch=63), dict(pitch=(1 << 30) + 1)):
         assert linear(_desc(), **kw) == T.ERR_SHAPE, kw
     assert linear(_desc(), n=0, x=None, y=None) == T.OK
-    assert T.lib().tardis_linear_workspace(_desc(), 4, None) == T.ERR_INVALID_ARG
-    assert T.lib().tardis_linear_workspace(_desc(), -1, C.c_int64()) == T.ERR_SHAPE
+    assert T.lib().tardis_linear_workspace(_desc(), P, 4, 64, None) == T.ERR_INVALID_ARG
+    assert T.lib().tardis_linear_workspace(_desc(), P, -1, 64, C.c_int64()) == T.ERR_SHAPE
+    assert T.lib().tardis_linear_workspace(_desc(), P, 4, 63, C.c_int64()) == T.ERR_SHAPE
     got = C.c_int64(7)
-    assert T.lib().tardis_linear_workspace(_desc(), 0, got) == T.OK and got.value == 0
+    assert T.lib().tardis_linear_workspace(_desc(), P, 0, 64, got) == T.OK and got.value == 0
 
 
 def test_more_tiles_than_a_launch_takes():
@@ -73,6 +75,11 @@ def test_grouped_refuses():
     for kw in (dict(experts=0), dict(experts=65537), dict(x_rows=-1), dict(pitch=63), dict(positions=-1), dict(per_token=0), dict(positions=(1 << 30) + 1),
                dict(order=None, x_rows=15)):
         assert grouped(_desc(), **kw) == T.ERR_SHAPE, kw
+    for kw in (dict(work=C.c_void_p(0x4008), bytes_=64), dict(work=P, bytes_=-1)):
+        assert grouped(_desc(), **kw) == T.ERR_INVALID_ARG, kw
+    assert T.lib().tardis_grouped_linear_workspace(_desc(), 4, P, 8, 64, 1, 16, None) == T.ERR_INVALID_ARG
+    for experts, x_rows, pitch, ordered, rows in ((0, 8, 64, 1, 16), (65537, 8, 64, 1, 16), (4, 8, 63, 1, 16), (4, 8, 64, 0, 16), (4, -1, 64, 1, 16)):
+        assert T.lib().tardis_grouped_linear_workspace(_desc(), experts, P, x_rows, pitch, ordered, rows, C.c_int64()) == T.ERR_SHAPE
     assert grouped(_desc(), positions=0, offsets=None, x=None, y=None) == T.OK
     assert grouped(_desc(), x_rows=0, x=None) == T.OK
 
