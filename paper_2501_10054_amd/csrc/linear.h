@@ -13,6 +13,7 @@ struct LinearArgs {
     uint32_t k;
     int act, out_f32;
     int tiles_m, tiles_n, splits, slices;   // of the whole product; ranges of K, slices in one.  (groups: tiles_n alone)
+    int tile_rows;                 // linear_quad_kernel: rows of a tile
     // rows by groups: those of group e are offsets[e] .. offsets[e + 1], with weights W + e N k; row m is row order[m] / per_token of x
     const int32_t *offsets, *order;
     int experts, per_token;

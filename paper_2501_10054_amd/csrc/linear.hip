@@ -77,29 +77,29 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, uint32_t
 //     max(fixed x turns + slices x max(alone x turns, slice x tiles of a CU), 1.5 + bytes / tbs)
 // with `blocks` of them at once on a CU, in `turns` turns: alone is a slice's latency, slice its share of the CU.  Bytes: x, y (the ranges'
 // sums), W, and for every further row of tiles `again` of W.  The constants are those with which the choice is best: over 573 products and 140
-// grouped ones in bf16 (sizes from 64 x 64 to 16384 x 16384, 1 to 3000 rows, weights from HBM; every tile with 1, 2, 4 and 8 ranges) it takes 0.9 % more
-// than the best measured, fp32 (179, 39) 0.5 %, staged (169, 24) 0.8 %, staged fp32 (98) 0.3 %.
+// grouped ones in bf16 (sizes from 64 x 64 to 16384 x 16384, 1 to 3000 rows, weights from HBM; every tile with 1, 2, 4 and 8 ranges) it takes 0.8 % more
+// than the best measured, fp32 (179, 39) 0.6 %, staged (169, 24) 0.6 %, staged fp32 (98) 0.3 %.
 struct Rate { int blocks; float alone, slice, fixed, tbs; };
-constexpr Rate kRate[] = {{2, 0.231f, 0.222f, 3.87f, 5.58f}, {2, 0.301f, 0.280f, 3.80f, 4.91f}, {1, 0.561f, 0.561f, 3.80f, 5.58f},
-                          {2, 0.248f, 0.204f, 3.80f, 4.75f}, {1, 0.341f, 0.341f, 3.87f, 4.75f}, {1, 0.290f, 0.290f, 4.07f, 4.00f},
-                          {1, 0.414f, 0.414f, 4.60f, 5.21f}, {2, 0.289f, 0.267f, 3.54f, 5.58f}, {1, 0.376f, 0.376f, 4.78f, 4.66f},
-                          {1, 0.579f, 0.579f, 4.78f, 3.81f}, {1, 0.745f, 0.745f, 8.05f, 3.60f}, {1, 0.376f, 0.376f, 4.50f, 4.13f},
-                          {1, 0.371f, 0.371f, 4.31f, 4.13f}, {1, 1.120f, 1.120f, 15.93f, 3.52f}, {1, 0.815f, 0.815f, 13.58f, 4.53f},
-                          {1, 0.718f, 0.718f, 9.41f, 3.83f}};
-constexpr Rate kRateF32[] = {{2, 0.289f, 0.228f, 4.20f, 5.31f}, {2, 0.366f, 0.344f, 4.12f, 5.31f}, {1, 1.038f, 1.038f, 3.77f, 6.32f},
-                             {2, 0.420f, 0.318f, 3.89f, 3.91f}, {1, 0.654f, 0.654f, 6.13f, 5.33f}, {1, 0.623f, 0.623f, 3.91f, 2.79f},
-                             {1, 1.174f, 1.174f, 4.77f, 6.20f}, {2, 0.634f, 0.537f, 4.33f, 3.24f}, {1, 1.116f, 1.116f, 5.30f, 2.56f},
-                             {1, 2.067f, 2.067f, 7.76f, 3.66f}, {1, 2.912f, 2.912f, 10.80f, 2.66f}, {1, 0.545f, 0.545f, 4.47f, 4.51f},
-                             {1, 0.702f, 0.702f, 3.78f, 4.02f}};
-constexpr Rate kRateStaged[] = {{2, 0.249f, 0.229f, 4.72f, 3.43f}, {1, 0.389f, 0.389f, 4.58f, 2.99f}, {2, 0.194f, 0.220f, 4.34f, 4.92f},
-                                {2, 0.221f, 0.215f, 4.32f, 2.88f}, {1, 0.565f, 0.565f, 7.03f, 3.13f}};
+constexpr Rate kRate[] = {{2, 0.225f, 0.210f, 3.95f, 5.37f}, {2, 0.326f, 0.301f, 3.80f, 4.67f}, {1, 0.615f, 0.615f, 3.76f, 5.50f},
+                          {2, 0.235f, 0.204f, 3.83f, 4.78f}, {1, 0.331f, 0.331f, 3.90f, 5.23f}, {1, 0.270f, 0.270f, 4.13f, 3.95f},
+                          {1, 0.424f, 0.424f, 4.60f, 5.18f}, {2, 0.318f, 0.284f, 3.54f, 5.56f}, {1, 0.369f, 0.369f, 5.00f, 4.13f},
+                          {1, 0.573f, 0.573f, 5.64f, 5.07f}, {1, 0.693f, 0.693f, 7.39f, 3.63f}, {1, 0.373f, 0.373f, 4.50f, 4.87f},
+                          {1, 0.365f, 0.365f, 4.31f, 4.30f}, {1, 0.990f, 0.990f, 16.86f, 3.35f}, {1, 0.904f, 0.904f, 13.11f, 4.43f},
+                          {1, 0.753f, 0.753f, 9.74f, 4.69f}};
+constexpr Rate kRateF32[] = {{2, 0.289f, 0.237f, 4.20f, 5.49f}, {2, 0.369f, 0.344f, 4.12f, 6.19f}, {1, 0.947f, 0.947f, 3.86f, 6.19f},
+                             {2, 0.412f, 0.320f, 3.73f, 4.91f}, {1, 0.651f, 0.651f, 4.39f, 4.50f}, {1, 0.628f, 0.628f, 3.72f, 2.98f},
+                             {1, 1.174f, 1.174f, 4.69f, 6.50f}, {2, 0.635f, 0.537f, 4.23f, 3.39f}, {1, 1.116f, 1.116f, 5.30f, 2.64f},
+                             {1, 2.082f, 2.082f, 6.96f, 2.65f}, {1, 2.961f, 2.961f, 9.52f, 2.50f}, {1, 0.509f, 0.509f, 4.75f, 4.84f},
+                             {1, 0.699f, 0.699f, 3.88f, 4.42f}};
+constexpr Rate kRateStaged[] = {{2, 0.221f, 0.229f, 4.77f, 3.42f}, {1, 0.388f, 0.388f, 4.64f, 3.31f}, {2, 0.190f, 0.220f, 4.35f, 4.90f},
+                                {2, 0.221f, 0.216f, 4.33f, 2.86f}, {1, 0.570f, 0.570f, 6.95f, 2.84f}};
 constexpr Rate kRateStagedF32[] = {{2, 0.076f, 0.253f, 4.35f, 3.98f}, {1, 0.368f, 0.368f, 4.49f, 3.98f}, {2, 0.049f, 0.301f, 4.26f, 4.41f},
                                    {2, 0.506f, 0.553f, 4.27f, 5.36f}, {1, 1.937f, 1.937f, 8.53f, 4.68f}};
 static_assert(sizeof(kRate) / sizeof(Rate) == kLinearShapes + kLinearQuads && sizeof(kRateF32) / sizeof(Rate) == kLinearShapes &&
               sizeof(kRateStaged) / sizeof(Rate) == kLinearStagedShapes && sizeof(kRateStagedF32) / sizeof(Rate) == kLinearStagedShapes, "a rate for each tile");
 // one more launch (2.5 on the GPU; callers that are not a graph wait for their host); a byte copied, of partial sums and outputs joined; sigma of an element of a tile, of eight wavefronts and of four
 constexpr double kLaunchUs = 4.0, kCopyUs = 1.0 / 4.5e6, kJoinUs = 1.0 / 5e6, kSigmaUs = 5.0 / 65536, kSigmaQuadUs = 8.0 / 65536;
-constexpr double kAgain = 0.23, kAgainF32 = 0.34, kAgainStaged = 0.15, kAgainStagedF32 = 0.41;
+constexpr double kAgain = 0.31, kAgainF32 = 0.42, kAgainStaged = 0.23, kAgainStagedF32 = 0.41;
 constexpr int64_t kMostTiles = 1 << 21;            // of a launch
 
 // What decides: sizes, types, alignment
@@ -152,15 +152,17 @@ Plan make_plan(const Call& c, int64_t room) {
             const LinearShape& t = shape_of(p.direct, s);
             const Rate& r = p.direct ? (c.es == 2 ? kRate[s] : kRateF32[s]) : (c.es == 2 ? kRateStaged[s] : kRateStagedF32[s]);
             const int64_t slices = (p.k + t.slice - 1) / t.slice, tiles_n = (c.N + t.n - 1) / t.n;
-            const double tiles_m = c.experts ? 1.05 * hit * std::max(1.0, (double)c.M / hit / t.m + 0.5) : (double)((c.M + t.m - 1) / t.m);
+            const double tiles_m = c.experts ? hit * std::max(1.0, (double)c.M / hit / t.m + 0.5) : (double)((c.M + t.m - 1) / t.m);
             if (tiles_m * (double)tiles_n >= kMostTiles && s + 1 < shapes_of(p.direct, c.es)) continue;
             for (int splits = 1; splits <= 8; splits *= 2) {
                 const double blocks = tiles_m * (double)tiles_n * splits;
                 if (splits > 1 && (c.experts || slices / splits < 4 || blocks > 1024 || p.at_part + splits * c.M * c.N * 4 > room)) break;
-                const double rounds = std::ceil(blocks / 256), shared = std::ceil(rounds / r.blocks);
+                // (how many tiles groups have is an estimate)
+                const double rounds = c.experts ? std::max(1.0, blocks / 256 + 0.5) : std::ceil(blocks / 256);
+                const double turns = c.experts ? std::max(1.0, rounds / r.blocks) : std::ceil(rounds / r.blocks);
                 const double per = (double)((slices + splits - 1) / splits);
                 const double sigma = c.act == TARDIS_ACT_GELU_ERF || c.act == TARDIS_ACT_GELU_TANH ? (p.direct && s >= kLinearShapes ? kSigmaQuadUs : kSigmaUs) * t.m * t.n * rounds : 0.0;
-                const double multiply = r.fixed * shared + per * std::max(r.alone * shared, r.slice * rounds) + (splits > 1 ? 0.0 : sigma);
+                const double multiply = r.fixed * turns + per * std::max(r.alone * turns, r.slice * rounds) + (splits > 1 ? 0.0 : sigma);
                 const double again = p.direct ? (c.es == 2 ? kAgain : kAgainF32) : (c.es == 2 ? kAgainStaged : kAgainStagedF32);
                 const double bytes = (hit + again * std::max(0.0, tiles_m - hit)) * c.N * p.k + (double)c.M * p.k + (double)c.M * c.N * (splits > 1 ? 4.0 * splits : c.eo);
                 double us = before + std::max(multiply, 1.5 + bytes / (r.tbs * 1e6));
@@ -186,6 +188,7 @@ tardis_status_t run(LinearArgs p, int32_t dtype, const Call& c, void* work, int6
     const bool grouped = c.experts > 0, quad = plan.direct && plan.shape >= kLinearShapes, f32 = dtype == TARDIS_F32;
     p.tiles_m = (int)((p.n + t.m - 1) / t.m);
     p.tiles_n = (int)((p.N + t.n - 1) / t.n);
+    p.tile_rows = (int)std::min<int64_t>(t.m, round_up((p.n + p.tiles_m - 1) / p.tiles_m, 32));
     p.splits = plan.splits;
     p.slices = plan.slices;
     // (of groups: at most one tile that is not full in each, and no more than rows)

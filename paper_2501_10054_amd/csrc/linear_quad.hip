@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(256, 1) linear_quad_kernel(LinearArgs p) {
     int tile_n;
     const int whole = (int)(p.k / SL);
     if constexpr (GROUPED) {
-        if (!find_group<TM>(p, lane, b, tile_n)) return;
+        if (!find_group<TM, true>(p, lane, b, tile_n) || b.rows == 0) return;
         b.s0 = b.range = 0;
         b.nk = whole;
     } else {
@@ -53,8 +53,9 @@ __global__ void __launch_bounds__(256, 1) linear_quad_kernel(LinearArgs p) {
         b.range = uniform((int)divide(t, (uint32_t)(p.tiles_m * p.tiles_n), in_range));
         tile_of(in_range, (uint32_t)p.tiles_m, (uint32_t)p.tiles_n, tile_m, tile_n);
         b.expert = 0;
-        b.first = (int64_t)tile_m * TM;
-        b.rows = (int)min((int64_t)TM, p.n - b.first);
+        b.first = (int64_t)tile_m * p.tile_rows;
+        b.rows = (int)min((int64_t)p.tile_rows, p.n - b.first);
+        if (b.rows <= 0) return;
         b.s0 = b.range * p.slices;
         b.nk = max(0, min(p.slices, whole - b.s0));
     }
@@ -141,145 +142,162 @@ __global__ void __launch_bounds__(256, 1) linear_quad_kernel(LinearArgs p) {
         for_constants<NA>([&](auto i) { if constexpr (NB + decltype(i)::value < most) load(i, oa, off_a[decltype(i)::value]); });
     });
 
-    f32x4_t acc[NA][NB];
+    // The products and what follows, of NR row blocks of a wavefront
+    auto products = [&](auto rows) {
+        constexpr int NR = decltype(rows)::value;
+        f32x4_t acc[NR][NB];
 #pragma unroll
-    for (int i = 0; i < NA; ++i)
+        for (int i = 0; i < NR; ++i)
 #pragma unroll
-        for (int j = 0; j < NB; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
-    // fragments: lane holds 16 bytes of row lane % 16 at piece 4 step + lane / 16
-    const int frow = lane & 15, fp = lane >> 4;
-    uint32_t frag_a[2], frag_b[2];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const uint32_t sw = (uint32_t)(frow * SL + (((s * 4 + fp) ^ (frow & 7)) * 16));
-        frag_a[s] = (uint32_t)(wm * NA * 16 * SL) + sw;
-        frag_b[s] = (uint32_t)(SA * G::UA + wn * NB * 16 * SL) + sw;
-    }
-    td_u32x4 fa[2][NA], fb[2][NB];
-    uint32_t xa = frag_a[0], xb = frag_b[0];          // where the next half slice's fragments lie
-    auto read_one = [&](int buf, int t) {             // fa[0], all of fb, the rest of fa
-        if (t == 0) fa[buf][0] = *reinterpret_cast<const td_u32x4*>(lds + xa);
-        else if (t <= NB) fb[buf][t - 1] = *reinterpret_cast<const td_u32x4*>(lds + xb + (t - 1) * (16 * SL));
-        else fa[buf][t - NB] = *reinterpret_cast<const td_u32x4*>(lds + xa + (t - NB) * (16 * SL));
-    };
-    auto mma = [&](f32x4_t& c, const td_u32x4& w, const td_u32x4& x) { asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x)); };
-    auto hold = [&]() {
-        // The compiler does not know how long the products take: every use of the accumulators from here on comes behind the statements
-        // before this, a wait among them
-#pragma unroll
-        for (int i = 0; i < NA; ++i)
-#pragma unroll
-            for (int j = 0; j < NB; ++j) asm volatile("" : "+a"(acc[i][j])::"memory");
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(G::kStart) : "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-#pragma unroll
-    for (int t = 0; t < G::kPer; ++t) read_one(0, t);
-    xa = frag_a[1];
-    xb = frag_b[1];
-    uint32_t ring_a = 0, ring_b = 0;                  // of the slice that is multiplied
-    auto turn = [&](uint32_t o, uint32_t unit, uint32_t ring) { return o + unit == ring ? 0u : o + unit; };
-    hold();
-    asm volatile("s_nop 7" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    // (a wait that the compiler knows of: what it believes to be under way here it waits for in every turn of the loop)
-    __builtin_amdgcn_s_waitcnt(kNoLds);
-    __builtin_amdgcn_sched_barrier(0);
-    // One slice: the MFMAs of its first half while the fragments of the second are read, the barrier behind which slice kt+1
-    // has arrived and this slice's buffers are free, the MFMAs of the second half while slice kt+1's first are read.
-    for (int kt = 0; kt < b.nk; ++kt) {
-        for_constants<TOT>([&](auto gap) {
-            constexpr int q = decltype(gap)::value, half = q / NM, h = q % NM;
-            constexpr int since = (q + NM) % TOT;                                     // gaps since the barrier
-            constexpr int until_b = NM - 1 - h, until_a = (G::kEvery * NB < NM ? G::kEvery * NB : NM) - 1 - h;
-            if constexpr (q == NM) {
-                __builtin_amdgcn_s_waitcnt(kNoLds);
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(G::kWait) : "memory");
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
-                oa.to = lds_a + ring_a;
-                ob.to = lds_b + ring_b;
-            }
-            if constexpr (h % 2 == 0 && h / 2 < G::kPer) read_one(1 - half, h / 2);
-            // the loads of this period: m0, the load
-            constexpr int n = since / G::kEvery, in = since % G::kEvery;
-            if constexpr (n < NB) {
-                if constexpr (in == 0) target(ob.to, num<n>{});
-                if constexpr (in == 1) fetch(ob, off_b[n]);
-            } else if constexpr (n < G::kPer) {
-                if constexpr (in == 0) target(oa.to, num<n - NB>{});
-                if constexpr (in == 1) fetch(oa, off_a[n - NB]);
-            }
-            // the slices of the next period's loads: W's before the barrier, x's while W's are issued
-            if constexpr (half == 0 && until_b < 10 && until_b % 2 == 0) find(ob, rb, 4 - until_b / 2);
-            if constexpr (half == 1 && until_a >= 0 && until_a < 10 && until_a % 2 == 0) find(oa, ra, 4 - until_a / 2);
-            // ring offsets and addresses of the next fragments, once this half's are under way
-            if constexpr (half == 0 && h == G::kTurnA) xa = frag_a[0] + turn(ring_a, G::UA, SA * G::UA);
-            if constexpr (half == 0 && h == G::kTurnB) xb = frag_b[0] + turn(ring_b, G::UB, SB * G::UB);
-            if constexpr (half == 1 && h == G::kTurnA) {
-                ring_a = turn(ring_a, G::UA, SA * G::UA);
-                xa = frag_a[1] + ring_a;
-            }
-            if constexpr (half == 1 && h == G::kTurnB) {
-                ring_b = turn(ring_b, G::UB, SB * G::UB);
-                xb = frag_b[1] + ring_b;
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            mma(acc[h / NB][h % NB], fb[half][h % NB], fa[half][h / NB]);
-            __builtin_amdgcn_sched_barrier(0);
-        });
-    }
-    // the rest of the row, alone: pieces past its end are loaded from its start (in bounds) and zeroed as they are read
-    const uint32_t from = (uint32_t)whole * SL, rest = p.k - from;
-    if (rest > 0 && b.range == p.splits - 1) {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        oa.rs = ra;
-        ob.rs = rb;
-        oa.soff = ob.soff = from;
-        oa.to = lds_a;
-        ob.to = lds_b;
-        const uint32_t back = piece < rest ? 0u : piece;
-        asm volatile("s_nop 4" : "+s"(oa.rs), "+s"(ob.rs));
-        for_constants<NA>([&](auto i) { load(i, oa, off_a[decltype(i)::value] - back); });
-        for_constants<NB>([&](auto i) { load(i, ob, off_b[decltype(i)::value] - back); });
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
+            for (int j = 0; j < NB; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
+        // fragments: lane holds 16 bytes of row lane % 16 at piece 4 step + lane / 16
+        const int frow = lane & 15, fp = lane >> 4;
+        uint32_t frag_a[2], frag_b[2];
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            xa = frag_a[s];
-            xb = frag_b[s];
-            const bool in = (uint32_t)(s * 4 + fp) * 16u < rest;
-            const td_u32x4 zero = {0, 0, 0, 0};
-#pragma unroll
-            for (int t = 0; t < G::kPer; ++t) read_one(s, t);
-#pragma unroll
-            for (int i = 0; i < NA; ++i) {
-                fa[s][i] = in ? fa[s][i] : zero;
-                asm volatile("" : "+v"(fa[s][i]));
-            }
-#pragma unroll
-            for (int j = 0; j < NB; ++j) {
-                fb[s][j] = in ? fb[s][j] : zero;
-                asm volatile("" : "+v"(fb[s][j]));
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            asm volatile("s_nop 7" ::: "memory");
-            __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-            for (int h = 0; h < NM; ++h) mma(acc[h / NB][h % NB], fb[s][h % NB], fa[s][h / NB]);
-            __builtin_amdgcn_sched_barrier(0);
+            const uint32_t sw = (uint32_t)(frow * SL + (((s * 4 + fp) ^ (frow & 7)) * 16));
+            frag_a[s] = (uint32_t)(wm * 16 * SL) + sw;
+            frag_b[s] = (uint32_t)(SA * G::UA + wn * NB * 16 * SL) + sw;
         }
+        td_u32x4 fa[2][NR], fb[2][NB];
+        uint32_t xa = frag_a[0], xb = frag_b[0];          // where the next half slice's fragments lie
+        auto read_one = [&](int buf, int t) {             // fa[0], all of fb, the rest of fa
+            if (t - NB >= NR) return;
+            if (t == 0) fa[buf][0] = *reinterpret_cast<const td_u32x4*>(lds + xa);
+            else if (t <= NB) fb[buf][t - 1] = *reinterpret_cast<const td_u32x4*>(lds + xb + (t - 1) * (16 * SL));
+            else fa[buf][t - NB] = *reinterpret_cast<const td_u32x4*>(lds + xa + (t - NB) * (2 * 16 * SL));
+        };
+        auto mma = [&](f32x4_t& c, const td_u32x4& w, const td_u32x4& x) { asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(c) : "v"(w), "v"(x)); };
+        auto hold = [&]() {
+            // The compiler does not know how long the products take: every use of the accumulators from here on comes behind the statements
+            // before this, a wait among them
+#pragma unroll
+            for (int i = 0; i < NR; ++i)
+#pragma unroll
+                for (int j = 0; j < NB; ++j) asm volatile("" : "+a"(acc[i][j])::"memory");
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(G::kStart) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int t = 0; t < G::kPer; ++t) read_one(0, t);
+        xa = frag_a[1];
+        xb = frag_b[1];
+        uint32_t ring_a = 0, ring_b = 0;                  // of the slice that is multiplied
+        auto turn = [&](uint32_t o, uint32_t unit, uint32_t ring) { return o + unit == ring ? 0u : o + unit; };
+        hold();
+        asm volatile("s_nop 7" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        // (a wait that the compiler knows of: what it believes to be under way here it waits for in every turn of the loop)
+        __builtin_amdgcn_s_waitcnt(kNoLds);
+        __builtin_amdgcn_sched_barrier(0);
+        // One slice: the MFMAs of its first half while the fragments of the second are read, the barrier behind which slice kt+1
+        // has arrived and this slice's buffers are free, the MFMAs of the second half while slice kt+1's first are read.
+        for (int kt = 0; kt < b.nk; ++kt) {
+            for_constants<TOT>([&](auto gap) {
+                constexpr int q = decltype(gap)::value, half = q / NM, h = q % NM;
+                constexpr int since = (q + NM) % TOT;                                     // gaps since the barrier
+                constexpr int until_b = NM - 1 - h, until_a = (G::kEvery * NB < NM ? G::kEvery * NB : NM) - 1 - h;
+                if constexpr (q == NM) {
+                    __builtin_amdgcn_s_waitcnt(kNoLds);
+                    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(G::kWait) : "memory");
+                    __builtin_amdgcn_s_barrier();
+                    asm volatile("" ::: "memory");
+                    oa.to = lds_a + ring_a;
+                    ob.to = lds_b + ring_b;
+                }
+                if constexpr (h % 2 == 0 && h / 2 < G::kPer) read_one(1 - half, h / 2);
+                // the loads of this period: m0, the load
+                constexpr int n = since / G::kEvery, in = since % G::kEvery;
+                if constexpr (n < NB) {
+                    if constexpr (in == 0) target(ob.to, num<n>{});
+                    if constexpr (in == 1) fetch(ob, off_b[n]);
+                } else if constexpr (n < G::kPer) {
+                    if constexpr (in == 0) target(oa.to, num<n - NB>{});
+                    if constexpr (in == 1) fetch(oa, off_a[n - NB]);
+                }
+                // the slices of the next period's loads: W's before the barrier, x's while W's are issued
+                if constexpr (half == 0 && until_b < 10 && until_b % 2 == 0) find(ob, rb, 4 - until_b / 2);
+                if constexpr (half == 1 && until_a >= 0 && until_a < 10 && until_a % 2 == 0) find(oa, ra, 4 - until_a / 2);
+                // ring offsets and addresses of the next fragments, once this half's are under way
+                if constexpr (half == 0 && h == G::kTurnA) xa = frag_a[0] + turn(ring_a, G::UA, SA * G::UA);
+                if constexpr (half == 0 && h == G::kTurnB) xb = frag_b[0] + turn(ring_b, G::UB, SB * G::UB);
+                if constexpr (half == 1 && h == G::kTurnA) {
+                    ring_a = turn(ring_a, G::UA, SA * G::UA);
+                    xa = frag_a[1] + ring_a;
+                }
+                if constexpr (half == 1 && h == G::kTurnB) {
+                    ring_b = turn(ring_b, G::UB, SB * G::UB);
+                    xb = frag_b[1] + ring_b;
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if constexpr (h / NB < NR) mma(acc[h / NB][h % NB], fb[half][h % NB], fa[half][h / NB]);
+                else asm volatile("s_nop 0");             // (the wait state between m0 and a load)
+                __builtin_amdgcn_sched_barrier(0);
+            });
+        }
+        // the rest of the row, alone: pieces past its end are loaded from its start (in bounds) and zeroed as they are read
+        const uint32_t from = (uint32_t)whole * SL, rest = p.k - from;
+        if (rest > 0 && b.range == p.splits - 1) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            oa.rs = ra;
+            ob.rs = rb;
+            oa.soff = ob.soff = from;
+            oa.to = lds_a;
+            ob.to = lds_b;
+            const uint32_t back = piece < rest ? 0u : piece;
+            asm volatile("s_nop 4" : "+s"(oa.rs), "+s"(ob.rs));
+            for_constants<NA>([&](auto i) { load(i, oa, off_a[decltype(i)::value] - back); });
+            for_constants<NB>([&](auto i) { load(i, ob, off_b[decltype(i)::value] - back); });
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                xa = frag_a[s];
+                xb = frag_b[s];
+                const bool in = (uint32_t)(s * 4 + fp) * 16u < rest;
+                const td_u32x4 zero = {0, 0, 0, 0};
+#pragma unroll
+                for (int t = 0; t < G::kPer; ++t) read_one(s, t);
+#pragma unroll
+                for (int i = 0; i < NR; ++i) {
+                    fa[s][i] = in ? fa[s][i] : zero;
+                    asm volatile("" : "+v"(fa[s][i]));
+                }
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    fb[s][j] = in ? fb[s][j] : zero;
+                    asm volatile("" : "+v"(fb[s][j]));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                asm volatile("s_nop 7" ::: "memory");
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int h = 0; h < NR * NB; ++h) mma(acc[h / NB][h % NB], fb[s][h % NB], fa[s][h / NB]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+        // (the products are in inline assembly: their results are waited for here)
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        hold();
+        finish_linear<bf16_t, GROUPED, 4, NR, NB, 2, 2, 1, G::fit(NR)>(p, b, acc, lds, tid);
+    };
+    // The rows of a product or group are divided evenly between its tiles, and the row blocks of a tile are dealt out to the wavefronts in turns, so
+    // that a tile which is not full takes fewer MFMAs.  (Each number of row blocks with its own accumulators and epilogue: where loops share them the
+    // compiler copies 256 registers from one to the other.)
+    if constexpr (NA == 8) {
+        if (b.rows <= 128) products(num<4>{});
+        else if (b.rows <= 192) products(num<6>{});
+        else products(num<8>{});
+    } else {
+        if (b.rows <= 16 * NA) products(num<NA / 2>{});
+        else products(num<NA>{});
     }
-    // (the products are in inline assembly: their results are waited for here)
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    hold();
-    finish_linear<bf16_t, GROUPED, 4, NA, NB, 2, 2, 1, G::RB>(p, b, acc, lds, tid);
 }
 
 template <typename F> void for_quad_shape(int shape, F f) {

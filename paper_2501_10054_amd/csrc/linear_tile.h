@@ -81,7 +81,8 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {
 
 // Which group's tile this block has: the rows of a group are known on the device alone, so every wavefront adds up the groups' tiles
 // (a lane has a group) and looks for its own number.  Offsets outside of 0 .. n count as the nearest of the two.
-template <int TM> __device__ __forceinline__ bool find_group(const LinearArgs& p, int lane, LinearBlock& b, int& tile_n) {
+// EVEN: the tiles of a group have as many rows each, to the next 32.
+template <int TM, bool EVEN> __device__ __forceinline__ bool find_group(const LinearArgs& p, int lane, LinearBlock& b, int& tile_n) {
     const int positions = (int)p.n;
     auto group = [&](int e, int& from) {
         from = e < p.experts ? min(max(p.offsets[e], 0), positions) : 0;
@@ -115,8 +116,14 @@ template <int TM> __device__ __forceinline__ bool find_group(const LinearArgs& p
             int tile_m;
             tile_of(t - mine * (uint32_t)p.tiles_n, (uint32_t)tiles, (uint32_t)p.tiles_n, tile_m, tile_n);
             b.expert = c + at;
-            b.first = from + (int64_t)tile_m * TM;
-            b.rows = min(TM, rows - tile_m * TM);
+            int step = TM;
+            if constexpr (EVEN) {
+                uint32_t rest;
+                step = uniform((int)divide((uint32_t)rows, (uint32_t)tiles, rest));   // (rows < 2^21 in one group: else the tiles are full)
+                step = rows < 1 << 21 ? min((step + (rest > 0) + 31) & ~31, TM) : TM;
+            }
+            b.first = from + (int64_t)tile_m * step;
+            b.rows = max(0, min(step, rows - tile_m * step));
             b.once = tiles == 1;
             return true;
         }
@@ -152,7 +159,7 @@ template <bool GROUPED> __device__ __forceinline__ int64_t token_of_row(const Li
 }
 
 // What follows the products of W wavefronts in a grid of WM x WN, times WK that divide K.
-// acc[i][j][q] = row (wm FA + i) 16 + lane % 16, column (wn FB + j) 16 + 4 (lane / 16) + q of the tile.  RB row blocks of a wavefront at a time
+// acc[i][j][q] = row (WM i + wm) 16 + lane % 16, column (wn FB + j) 16 + 4 (lane / 16) + q of the tile.  RB row blocks of a wavefront at a time
 // pass through LDS, where the parts of K meet (WK = 1: every wavefront's own), so that a store covers whole lines of a row and that what
 // is done to the elements is a loop; a thread finishes 8 neighbouring columns at once.
 template <typename T, bool GROUPED, int W, int FA, int FB, int WM, int WN, int WK, int RB>
@@ -207,7 +214,7 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
         with_linear_act(p.act, [&](auto act) {
 #pragma unroll kAtOnce
             for (int at = me / UNITS; at < ROWS; at += STRIDE) {
-                const int m = OWN ? (wm * FA + i0) * 16 + at : (at / (RB * 16) * FA + i0) * 16 + at % (RB * 16);   // row of the tile
+                const int block = OWN ? wm + WM * (at / 16) : at / (RB * 16) + WM * (at / 16 % RB), m = (i0 * WM + block) * 16 + at % 16;   // row of the tile
                 if (m >= b.rows || columns <= 0) continue;
                 if (GROUPED && p.order && token_of_row<GROUPED>(p, b, m) < 0) continue;
                 const int64_t row = b.first + m, to = row * p.N + n;
@@ -267,7 +274,7 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
     int tile_n;
     const int slices = (int)((p.k + SL - 1) / SL);
     if constexpr (GROUPED) {
-        if (!find_group<TM>(p, lane, b, tile_n)) return;
+        if (!find_group<TM, false>(p, lane, b, tile_n)) return;
         b.s0 = b.range = 0;
         b.nk = slices;
     } else {
@@ -309,20 +316,21 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
     struct Fragments {
         td_u32x4 a[KS][FA], b[KS][FB];
     };
-    auto read = [&](Fragments& f, const unsigned char* at_a, const unsigned char* at_b) {
+    // (rows: the row blocks of a wavefront that are there, see below)
+    auto read = [&](auto rows, Fragments& f, const unsigned char* at_a, const unsigned char* at_b) {
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
 #pragma unroll
-            for (int i = 0; i < FA; ++i) f.a[s][i] = *reinterpret_cast<const td_u32x4*>(at_a + (wm * FA + i) * (16 * SL) + frag[s]);
+            for (int i = 0; i < decltype(rows)::value; ++i) f.a[s][i] = *reinterpret_cast<const td_u32x4*>(at_a + (WM * i + wm) * (16 * SL) + frag[s]);
 #pragma unroll
             for (int j = 0; j < FB; ++j) f.b[s][j] = *reinterpret_cast<const td_u32x4*>(at_b + (wn * FB + j) * (16 * SL) + frag[s]);
         }
     };
-    auto multiply = [&](const Fragments& f) {
+    auto multiply = [&](auto rows, const Fragments& f) {
 #pragma unroll
         for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int i = 0; i < FA; ++i)
+            for (int i = 0; i < decltype(rows)::value; ++i)
 #pragma unroll
                 for (int j = 0; j < FB; ++j) mma_pieces<T>(acc[i][j], f.b[s][j], f.a[s][i]);
     };
@@ -393,39 +401,44 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
         };
 #pragma unroll 1
         for (int s = 0; s < D; ++s) load_slice(s, (uint32_t)s);
-        uint32_t slot = 0;                                // of the slice that is read next
-        auto fetch = [&](Fragments& f, int t) {
-            read(f, lds + slot * G::UA, lds + D * G::UA + slot * G::UB);
-            if (t >= whole) {                             // a slice that is not whole: what the row has not is zero
-                const td_u32x4 zero = {0, 0, 0, 0};
+        auto products = [&](auto rows) {
+            uint32_t slot = 0;                            // of the slice that is read next
+            auto fetch = [&](Fragments& f, int t) {
+                read(rows, f, lds + slot * G::UA, lds + D * G::UA + slot * G::UB);
+                if (t >= whole) {                         // a slice that is not whole: what the row has not is zero
+                    const td_u32x4 zero = {0, 0, 0, 0};
 #pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const bool in = (uint32_t)slice_of(t) * SL + (uint32_t)(4 * (wk + WK * s) + fp) * 16u < p.k;
+                    for (int s = 0; s < KS; ++s) {
+                        const bool in = (uint32_t)slice_of(t) * SL + (uint32_t)(4 * (wk + WK * s) + fp) * 16u < p.k;
 #pragma unroll
-                    for (int i = 0; i < FA; ++i) f.a[s][i] = in ? f.a[s][i] : zero;
+                        for (int i = 0; i < decltype(rows)::value; ++i) f.a[s][i] = in ? f.a[s][i] : zero;
 #pragma unroll
-                    for (int j = 0; j < FB; ++j) f.b[s][j] = in ? f.b[s][j] : zero;
+                        for (int j = 0; j < FB; ++j) f.b[s][j] = in ? f.b[s][j] : zero;
+                    }
                 }
+            };
+            Fragments f[2];
+            auto step = [&](const Fragments& now, Fragments& next, int t) {
+                arrived(num<2>{});                        // slice t + 1 is here, and slice t's place is free
+                const uint32_t free = slot;
+                slot = slot + 1 == D ? 0 : slot + 1;
+                load_slice(t + D, free);
+                if (t + 1 < b.nk) fetch(next, t + 1);
+                multiply(rows, now);
+            };
+            if (b.nk > 0) {
+                arrived(num<1>{});
+                fetch(f[0], 0);
+            }
+#pragma unroll 1
+            for (int t = 0; t < b.nk; t += 2) {
+                step(f[0], f[1], t);
+                if (t + 1 < b.nk) step(f[1], f[0], t + 1);
             }
         };
-        Fragments f[2];
-        auto step = [&](const Fragments& now, Fragments& next, int t) {
-            arrived(num<2>{});                            // slice t + 1 is here, and slice t's place is free
-            const uint32_t free = slot;
-            slot = slot + 1 == D ? 0 : slot + 1;
-            load_slice(t + D, free);
-            if (t + 1 < b.nk) fetch(next, t + 1);
-            multiply(now);
-        };
-        if (b.nk > 0) {
-            arrived(num<1>{});
-            fetch(f[0], 0);
-        }
-#pragma unroll 1
-        for (int t = 0; t < b.nk; t += 2) {
-            step(f[0], f[1], t);
-            if (t + 1 < b.nk) step(f[1], f[0], t + 1);
-        }
+        // (a tile that is at most half full: its row blocks are dealt out to the wavefronts in turns, so each has half of them)
+        if (FA >= 4 && b.rows <= TM / 2) products(num<(FA >= 4 ? FA / 2 : FA)>{});
+        else products(num<FA>{});
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     } else {
         // (for rows that are not there the first one's, of which nothing is kept: the loop has no branches, so that a load is waited
@@ -463,8 +476,8 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
             __syncthreads();
             load_slice(now, t + D);
             Fragments f;
-            read(f, lds + place * G::UA, lds + 2 * G::UA + place * G::UB);
-            multiply(f);
+            read(num<FA>{}, f, lds + place * G::UA, lds + 2 * G::UA + place * G::UB);
+            multiply(num<FA>{}, f);
         };
         if (whole > 0) {
 #pragma unroll
@@ -499,8 +512,8 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
             to_lds(v[0], whole & 1);
             __syncthreads();
             Fragments f;
-            read(f, lds + (whole & 1) * G::UA, lds + 2 * G::UA + (whole & 1) * G::UB);
-            multiply(f);
+            read(num<FA>{}, f, lds + (whole & 1) * G::UA, lds + 2 * G::UA + (whole & 1) * G::UB);
+            multiply(num<FA>{}, f);
         }
     }
     __syncthreads();

@@ -96,3 +96,24 @@ def test_nothing_spills(listings):
             assert int(re.search(r"\.vgpr_spill_count:\s+(\d+)", part)[1]) == 0, name
             assert int(re.search(r"\.private_segment_fixed_size:\s+(\d+)", part)[1]) == 0, name
     assert seen == 2 * 36 + 2 * 6
+
+
+@pytest.mark.parametrize("source,kernel", [("linear_quad", "linear_quad_kernel"), ("linear_bf16", "linear_kernel"), ("linear_f32", "linear_kernel")])
+def test_scalars_written_by_vector_instructions_are_waited_for(listings, source, kernel):
+    """5 wait states between a vector instruction that writes a scalar register and a load that reads it: the loads are inline assembly, whose
+    operands the compiler takes for ready."""
+    def scalars(text):
+        regs = set()
+        for m in re.finditer(r"\bs(?:\[(\d+):(\d+)\]|(\d+)\b)", text):
+            lo, hi = (int(m[1]), int(m[2])) if m[1] else (int(m[3]), int(m[3]))
+            regs.update(range(lo, hi + 1))
+        return regs
+
+    for name, (code, labels) in _kernels(listings[source, False], kernel).items():
+        for i, (op, rest) in enumerate(code):
+            if not op.startswith(("v_readlane", "v_readfirstlane", "v_cmp")):
+                continue
+            written = scalars(rest.split(",")[0])
+            for k in _walk(code, labels, i, 5):
+                if code[k][0].startswith("buffer_load"):
+                    assert not written & scalars(code[k][1]), (name, op, rest, code[k])
