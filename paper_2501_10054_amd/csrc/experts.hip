@@ -12,10 +12,11 @@ namespace {
 // slots (token, place in its choice) in the order of their experts, which is a counting sort: its counts and its ranks are sums of whole numbers
 // in a fixed order, so the result is the same in every run.
 //
-// What bounds it: round trips.  One block does all of a call of few tokens (kRounds tokens for each of its groups of lanes); more take two
-// launches, the choice with the counts of every block, then the placement, for which every block adds up the counts of those before it (at
-// most kMostBlocks), which costs less than a launch of its own for that.
-constexpr int kRouteThreads = 1024, kRounds = 4, kMostBlocks = 256, kRouteWaves = kRouteThreads / 64;
+// What bounds it: round trips and, for many tokens, the vector instructions of the choice (16384 tokens, 128 experts, 8 chosen, in 64 blocks 25 us,
+// in 256 @CHOOSE).  One block does all of a call of up to kRounds tokens for each of its groups of lanes; more take two launches, the choice with
+// the counts of every block, then the placement, for which every block adds up the counts of those before it (at most kMostBlocks), which
+// costs less than a launch of its own for that.
+constexpr int kRouteThreads = 1024, kRounds = 2, kMostBlocks = 256, kRouteWaves = kRouteThreads / 64;
 
 struct RouteArgs {
     const void* logits;
@@ -23,8 +24,11 @@ struct RouteArgs {
     int experts, k, renormalise, tokens;           // tokens of a block
     int32_t *ids, *offsets, *order, *place;
     float* weights;
-    int32_t* counts;                               // [block][expert]
+    int32_t* counts;                               // [block][counts_of_row(experts)]
 };
+
+// (rows of whole, aligned pieces of 16 bytes)
+__host__ __device__ __forceinline__ int counts_of_row(int experts) { return (experts + 3) & ~3; }
 
 template <int CTRL> __device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false); }
 template <int CTRL> __device__ __forceinline__ float dpp(float v) { return __int_as_float(dpp<CTRL>(__float_as_int(v))); }
@@ -69,8 +73,8 @@ __device__ __forceinline__ void choose_experts(const RouteArgs& p, int64_t first
             for (int i = 0; i < V; ++i) total += weight(v[i]);
             total = over_lanes<G>(total, add);
         }
-        int my_id = -1;
-        float my_weight = 0.0f;
+        int my_id = -1;                                       // lane j has the choice number j
+        float my_logit = -INFINITY;
 #pragma unroll 1
         for (int j = 0; j < p.k; ++j) {
             float best = v[0];
@@ -84,17 +88,15 @@ __device__ __forceinline__ void choose_experts(const RouteArgs& p, int64_t first
             const int id = over_lanes<G>(best == top && top > -INFINITY ? lane + G * at : INT32_MAX, smaller);
 #pragma unroll
             for (int i = 0; i < V; ++i) v[i] = lane + G * i == id ? -INFINITY : v[i];
-            const float w = weight(top);
-            if (p.renormalise) total += w;
-            if (lane == j) {
-                my_id = id == INT32_MAX ? -1 : id;
-                my_weight = w;
-            }
+            my_id = lane == j && id != INT32_MAX ? id : my_id;
+            my_logit = lane == j ? top : my_logit;
         }
+        const float mine = weight(my_logit);
+        if (p.renormalise) total = over_lanes<G>(mine, add);
         if (lane < p.k) {
             const int64_t slot = (first + t) * p.k + lane;
             p.ids[slot] = my_id;
-            p.weights[slot] = my_id < 0 ? 0.0f : my_weight / total;
+            p.weights[slot] = my_id < 0 ? 0.0f : mine / total;
             if (my_id >= 0) atomicAdd(counts + my_id, 1);
         }
     }
@@ -183,7 +185,7 @@ template <typename T, int G, int V, bool ALONE> __global__ void __launch_bounds_
     choose_experts<T, G, V>(p, first, tokens, counts);
     __syncthreads();
     if constexpr (ALONE) place_slots(p, first, tokens, counts, zeros, from, sums);
-    else if (tid < p.experts) p.counts[(int64_t)blockIdx.x * p.experts + tid] = counts[tid];
+    else if (tid < counts_of_row(p.experts)) p.counts[(int64_t)blockIdx.x * counts_of_row(p.experts) + tid] = tid < p.experts ? counts[tid] : 0;
 }
 
 __global__ void __launch_bounds__(kRouteThreads) route_place_kernel(RouteArgs p) {
@@ -193,18 +195,24 @@ __global__ void __launch_bounds__(kRouteThreads) route_place_kernel(RouteArgs p)
     const int tid = threadIdx.x, blocks = (int)gridDim.x, mine = (int)blockIdx.x;
     if (tid < p.experts) all[tid] = before[tid] = 0;
     __syncthreads();
-    // parts of the blocks for every expert
-    const int parts = kRouteThreads / p.experts, part = tid / p.experts, e = tid % p.experts;
+    // four neighbouring experts for a thread, of every `parts`-th block
+    const int pieces = counts_of_row(p.experts) / 4, parts = kRouteThreads / pieces, part = tid / pieces, piece = tid % pieces;
     if (part < parts) {
-        int a = 0, b = 0;
+        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        const i32x4* rows = reinterpret_cast<const i32x4*>(p.counts) + piece;
+        i32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
 #pragma unroll 8
         for (int i = part; i < blocks; i += parts) {
-            const int c = p.counts[(int64_t)i * p.experts + e];
+            const i32x4 c = rows[(int64_t)i * pieces];
             a += c;
-            b += i < mine ? c : 0;
+            b += i < mine ? c : i32x4{0, 0, 0, 0};
         }
-        atomicAdd(all + e, a);
-        atomicAdd(before + e, b);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            if (piece * 4 + q < p.experts) {
+                atomicAdd(all + piece * 4 + q, a[q]);
+                atomicAdd(before + piece * 4 + q, b[q]);
+            }
     }
     __syncthreads();
     const int64_t first = (int64_t)mine * p.tokens;
@@ -222,9 +230,11 @@ template <typename F> void for_experts(int64_t experts, F f) {
     else f(num<64>{}, num<16>{});
 }
 
+// Tokens of a block: all of them where one block does the call, else one for each of its groups of lanes, or so many that the blocks are no more
+// than kMostBlocks
 int64_t tokens_of_block(int64_t n, int64_t experts) {
-    const int64_t few = kRounds * kRouteThreads / (experts <= 128 ? 16 : 64);
-    return std::max(few, (n + kMostBlocks - 1) / kMostBlocks);
+    const int64_t groups = kRouteThreads / (experts <= 128 ? 16 : 64);
+    return n <= kRounds * groups ? kRounds * groups : std::max(groups, (n + kMostBlocks - 1) / kMostBlocks);
 }
 
 template <typename T> void launch_route(RouteArgs& p, hipStream_t s) {
@@ -239,7 +249,8 @@ template <typename T> void launch_route(RouteArgs& p, hipStream_t s) {
 
 // ---------------------------------------------------------------- the sum of the experts' outputs
 // y[t] = r[t] + sum_j w[t, j] z[place[t, j]], in this order, in fp32.  A thread has the columns of 16 bytes of a row; the rows of up to 8
-// slots are asked for at once.  Bound: the rows' bytes, each read once.
+// slots are asked for at once.  Bound: the rows' bytes, each read once (so their lines are not kept).  ALIKE: all threads of a wavefront have the same
+// token, whose places and weights are scalar loads.
 struct CombineArgs {
     const unsigned char* z;
     const int32_t* place;
@@ -252,11 +263,12 @@ struct CombineArgs {
 
 typedef uint32_t any16_t __attribute__((ext_vector_type(4), aligned(2)));
 
-template <typename T> __global__ void __launch_bounds__(256) combine_kernel(CombineArgs p) {
+template <typename T, bool ALIKE> __global__ void __launch_bounds__(256) combine_kernel(CombineArgs p) {
     constexpr int C = 16 / (int)sizeof(T);         // columns of a thread
     const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t t = u < (1ll << 32) ? (int64_t)((uint32_t)u / (uint32_t)p.units) : u / p.units;
+    int64_t t = u < (1ll << 32) ? (int64_t)((uint32_t)u / (uint32_t)p.units) : u / p.units;
     if (t >= p.n) return;
+    if constexpr (ALIKE) t = __builtin_amdgcn_readfirstlane((int)t);
     const int64_t c = (u - t * p.units) * C;
     const int columns = (int)min((int64_t)C, p.d - c);
     float v[C] = {};
@@ -273,7 +285,7 @@ template <typename T> __global__ void __launch_bounds__(256) combine_kernel(Comb
         td_u32x4 x[8];
         if (columns == C) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = *reinterpret_cast<const any16_t*>(reinterpret_cast<const T*>(p.z) + (int64_t)max(at[j], 0) * p.d + c);
+            for (int j = 0; j < 8; ++j) x[j] = __builtin_nontemporal_load(reinterpret_cast<const any16_t*>(reinterpret_cast<const T*>(p.z) + (int64_t)max(at[j], 0) * p.d + c));
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -298,12 +310,36 @@ template <typename T> __global__ void __launch_bounds__(256) combine_kernel(Comb
             }
     }
     const int64_t to = t * p.d + c;
+    if (columns < C) {                             // the end of a row
 #pragma unroll
-    for (int q = 0; q < C; ++q) {
-        if (q >= columns) continue;
-        if (p.r) v[q] += p.out_f32 ? static_cast<const float*>(p.r)[to + q] : td_load<bf16_t>(static_cast<const bf16_t*>(p.r) + to + q);
-        if (p.out_f32) static_cast<float*>(p.y)[to + q] = v[q];
-        else td_store<bf16_t>(static_cast<bf16_t*>(p.y) + to + q, v[q]);
+        for (int q = 0; q < C; ++q) {
+            if (q >= columns) continue;
+            if (p.r) v[q] += p.out_f32 ? static_cast<const float*>(p.r)[to + q] : td_load<bf16_t>(static_cast<const bf16_t*>(p.r) + to + q);
+            if (p.out_f32) static_cast<float*>(p.y)[to + q] = v[q];
+            else td_store<bf16_t>(static_cast<bf16_t*>(p.y) + to + q, v[q]);
+        }
+    } else if (p.out_f32) {
+#pragma unroll
+        for (int h = 0; h < C; h += 4) {
+            if (p.r) {
+                const td_u32x4 r = *reinterpret_cast<const any16_t*>(static_cast<const float*>(p.r) + to + h);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) v[h + q] += __uint_as_float(r[q]);
+            }
+            *reinterpret_cast<any16_t*>(static_cast<float*>(p.y) + to + h) =
+                any16_t{__float_as_uint(v[h]), __float_as_uint(v[h + 1]), __float_as_uint(v[h + 2]), __float_as_uint(v[h + 3])};
+        }
+    } else {
+        typedef uint32_t any_t __attribute__((ext_vector_type(C / 2), aligned(2)));
+        if (p.r) {
+            const any_t r = *reinterpret_cast<const any_t*>(static_cast<const bf16_t*>(p.r) + to);
+#pragma unroll
+            for (int q = 0; q < C; ++q) v[q] += __uint_as_float(q & 1 ? r[q / 2] & 0xffff0000u : r[q / 2] << 16);
+        }
+        any_t o;
+#pragma unroll
+        for (int q = 0; q < C / 2; ++q) o[q] = to_bf16x2(v[2 * q], v[2 * q + 1]);
+        *reinterpret_cast<any_t*>(static_cast<bf16_t*>(p.y) + to) = o;
     }
 }
 
@@ -311,7 +347,7 @@ template <typename T> __global__ void __launch_bounds__(256) combine_kernel(Comb
 
 size_t td_route_work_bytes(int64_t n, int64_t experts) {
     const int64_t tokens = tokens_of_block(n, experts), blocks = (n + tokens - 1) / tokens;
-    return blocks > 1 ? (size_t)(blocks * experts) * 4 : 0;
+    return blocks > 1 ? (size_t)blocks * counts_of_row((int)experts) * 4 : 0;
 }
 
 tardis_status_t td_moe_route(const void* logits, int64_t n, int64_t experts, int64_t k, int32_t dtype, int renormalise, int32_t* ids, float* weights,
@@ -352,8 +388,10 @@ tardis_status_t td_moe_combine(const void* z, int64_t rows, const int32_t* place
     p.units = (d + columns - 1) / columns;
     const int64_t blocks = (p.units * n + 255) / 256;
     if (blocks > 0x7fffffff) return TARDIS_ERR_SHAPE;
-    if (dtype == TARDIS_F32) hipLaunchKernelGGL(combine_kernel<float>, dim3((unsigned)blocks), dim3(256), 0, s, p);
-    else hipLaunchKernelGGL(combine_kernel<bf16_t>, dim3((unsigned)blocks), dim3(256), 0, s, p);
+    const bool alike = p.units % 64 == 0;
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, p); };
+    if (dtype == TARDIS_F32) launch(alike ? combine_kernel<float, true> : combine_kernel<float, false>);
+    else launch(alike ? combine_kernel<bf16_t, true> : combine_kernel<bf16_t, false>);
     TD_HIP(hipGetLastError());
     return TARDIS_OK;
 }

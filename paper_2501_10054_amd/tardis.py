@@ -338,6 +338,10 @@ def _route_work_bytes(n, experts):
     return bytes_.value
 
 
+def _empty(n, width, dtype, device):
+    return torch.empty_strided((n, width), (width, 1), dtype=dtype, device=device)   # (half the host time of torch.empty)
+
+
 def _rows(x, n_in):
     """Rows that may lie further apart than they are long -> their number and distance."""
     assert x.is_cuda and x.dim() == 2 and x.shape[1] == n_in
@@ -350,15 +354,15 @@ def tardis_linear(x, W, b=None, act: str = "identity", residual=None, out_dtype=
     """-> n x n_out: act(x W^T + b) + residual.  Rows of x may have a pitch; out_dtype: of residual and y (default: x's)."""
     n_out, n_in = W.shape
     n, pitch = _rows(x, n_in)
-    dt = x.dtype
+    dt, dev = x.dtype, x.get_device()
     out_dtype = out_dtype or dt
-    assert W.is_contiguous() and W.dtype == dt and W.device == x.device
-    assert b is None or (b.is_contiguous() and b.dtype == dt and b.numel() == n_out and b.device == x.device)
-    assert residual is None or (residual.is_contiguous() and residual.dtype == out_dtype and residual.shape == (n, n_out) and residual.device == x.device)
+    assert W.is_contiguous() and W.dtype == dt and W.get_device() == dev
+    assert b is None or (b.is_contiguous() and b.dtype == dt and b.numel() == n_out and b.get_device() == dev)
+    assert residual is None or (residual.is_contiguous() and residual.dtype == out_dtype and residual.shape == (n, n_out) and residual.get_device() == dev)
     if y is None:
-        y = torch.empty(n, n_out, dtype=out_dtype, device=x.device)
+        y = _empty(n, n_out, out_dtype, x.device)
     else:
-        assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, n_out) and y.device == x.device
+        assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, n_out) and y.get_device() == dev
     sizes, x_at, W_at = (n_in, n_out, _DTYPE_CODE[dt], _DTYPE_CODE[out_dtype], ACT[act]), x.data_ptr(), W.data_ptr()
     desc = tardis_linear_desc(*sizes, 0, W_at, None if b is None else b.data_ptr())
     bytes_ = _linear_work_bytes(sizes, 0, n, pitch, 0, n, x_at & 15, W_at & 15)
@@ -372,17 +376,17 @@ def tardis_grouped_linear(x, W, offsets, b=None, act: str = "identity", order=No
     an order x[p].  W: experts x n_out x n_in.  Rows of y in no group are not written."""
     experts, n_out, n_in = W.shape
     x_rows, pitch = _rows(x, n_in)
-    dt = x.dtype
+    dt, dev = x.dtype, x.get_device()
     out_dtype = out_dtype or dt
-    assert W.is_contiguous() and W.dtype == dt and W.device == x.device
-    assert b is None or (b.is_contiguous() and b.dtype == dt and b.numel() == experts * n_out and b.device == x.device)
-    assert offsets.is_contiguous() and offsets.dtype == torch.int32 and offsets.numel() == experts + 1 and offsets.device == x.device
-    assert order is None or (order.is_contiguous() and order.dtype == torch.int32 and order.device == x.device)
+    assert W.is_contiguous() and W.dtype == dt and W.get_device() == dev
+    assert b is None or (b.is_contiguous() and b.dtype == dt and b.numel() == experts * n_out and b.get_device() == dev)
+    assert offsets.is_contiguous() and offsets.dtype == torch.int32 and offsets.numel() == experts + 1 and offsets.get_device() == dev
+    assert order is None or (order.is_contiguous() and order.dtype == torch.int32 and order.get_device() == dev)
     positions = x_rows if order is None else order.numel()
     if y is None:
-        y = torch.empty(positions, n_out, dtype=out_dtype, device=x.device)
+        y = _empty(positions, n_out, out_dtype, x.device)
     else:
-        assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (positions, n_out) and y.device == x.device
+        assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (positions, n_out) and y.get_device() == dev
     sizes, x_at, W_at, ordered = (n_in, n_out, _DTYPE_CODE[dt], _DTYPE_CODE[out_dtype], ACT[act]), x.data_ptr(), W.data_ptr(), order is not None
     desc = tardis_linear_desc(*sizes, 0, W_at, None if b is None else b.data_ptr())
     bytes_ = _linear_work_bytes(sizes, experts, x_rows, pitch, int(ordered), positions, x_at & 15, W_at & 15)
@@ -397,9 +401,9 @@ def tardis_moe_route(logits, k: int, renormalise: bool = True, stream=None):
     n, experts = logits.shape
     assert logits.is_cuda and logits.is_contiguous()
     dev = logits.device
-    words = torch.empty(3 * n * k + experts + 1, dtype=torch.int32, device=dev)
-    ids, order, place, offsets = words[:n * k].view(n, k), words[n * k:2 * n * k], words[2 * n * k:3 * n * k].view(n, k), words[3 * n * k:]
-    weights = torch.empty(n, k, dtype=torch.float32, device=dev)
+    ids, place, weights = _empty(n, k, torch.int32, dev), _empty(n, k, torch.int32, dev), _empty(n, k, torch.float32, dev)
+    order = torch.empty_strided((n * k,), (1,), dtype=torch.int32, device=dev)
+    offsets = torch.empty_strided((experts + 1,), (1,), dtype=torch.int32, device=dev)
     bytes_ = _route_work_bytes(n, experts)
     work = torch.empty(bytes_, dtype=torch.uint8, device=dev) if bytes_ else None
     _check(lib().tardis_moe_route(logits.data_ptr(), n, experts, k, _DTYPE_CODE[logits.dtype], 1 if renormalise else 0, ids.data_ptr(), weights.data_ptr(),
@@ -409,15 +413,15 @@ def tardis_moe_route(logits, k: int, renormalise: bool = True, stream=None):
 
 def tardis_moe_combine(z, place, weights, residual=None, out_dtype=None, y=None, stream=None):
     """-> n x d: residual[t] + sum_j weights[t, j] z[place[t, j]]; a place below 0 is a dropped slot.  out_dtype: of residual and y (default: z's)."""
-    (rows, d), (n, k) = z.shape, place.shape
+    (rows, d), (n, k), dev = z.shape, place.shape, z.get_device()
     out_dtype = out_dtype or z.dtype
-    assert z.is_cuda and z.is_contiguous() and place.is_contiguous() and place.dtype == torch.int32 and place.device == z.device
-    assert weights.is_contiguous() and weights.dtype == torch.float32 and weights.shape == (n, k) and weights.device == z.device
-    assert residual is None or (residual.is_contiguous() and residual.dtype == out_dtype and residual.shape == (n, d) and residual.device == z.device)
+    assert z.is_cuda and z.is_contiguous() and place.is_contiguous() and place.dtype == torch.int32 and place.get_device() == dev
+    assert weights.is_contiguous() and weights.dtype == torch.float32 and weights.shape == (n, k) and weights.get_device() == dev
+    assert residual is None or (residual.is_contiguous() and residual.dtype == out_dtype and residual.shape == (n, d) and residual.get_device() == dev)
     if y is None:
-        y = torch.empty(n, d, dtype=out_dtype, device=z.device)
+        y = _empty(n, d, out_dtype, z.device)
     else:
-        assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, d) and y.device == z.device
+        assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, d) and y.get_device() == dev
     _check(lib().tardis_moe_combine(z.data_ptr(), rows, place.data_ptr(), weights.data_ptr(), n, k, d, _DTYPE_CODE[z.dtype], _ptr(residual), y.data_ptr(),
                                     _DTYPE_CODE[out_dtype], _stream(stream)), "tardis_moe_combine")
     return y
