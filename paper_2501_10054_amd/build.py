@@ -15,6 +15,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libtardis.so")
 SIGMA_PROBE = os.path.join(OBJ, "sigma_probe.so")
+LINEAR_PROBE = os.path.join(OBJ, "linear_probe.so")
 
 SOURCES = ["api.hip", "decode.hip", "experts.hip", "forward.hip", "gemm.hip", "linear.hip", "linear_bf16.hip", "linear_f32.hip", "linear_quad.hip", "offline.hip", "prefill.hip", "stack.hip", "stream.hip"]
 
@@ -55,6 +56,7 @@ def build(verbose: bool = True) -> str:
     if verbose:
         print(f"built {LIB}")
     build_sigma_probe()
+    build_linear_probe()
     build_c_demo(verbose)
     return LIB
 
@@ -66,6 +68,16 @@ def build_sigma_probe() -> str:
     if os.path.exists(src):
         _run([_hipcc(), *FLAGS, "-I" + CSRC, "-shared", src, "-o", SIGMA_PROBE])
     return SIGMA_PROBE
+
+
+def build_linear_probe() -> str:
+    """tests/linear_probe.hip: the linear layer's kernels by their numbers (links what build() has compiled)."""
+    src = os.path.join(os.path.dirname(HERE), "tests", "linear_probe.hip")
+    if os.path.exists(src):
+        objs = [os.path.join(OBJ, f"linear_{part}.o") for part in ("bf16", "f32", "quad")]
+        _run([_hipcc(), *FLAGS, "-I" + CSRC, "-c", src, "-o", LINEAR_PROBE + ".o"])
+        _run([_hipcc(), "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LINEAR_PROBE, LINEAR_PROBE + ".o", *objs])
+    return LINEAR_PROBE
 
 
 def build_c_demo(verbose: bool = True) -> str | None:

@@ -32,6 +32,8 @@ constexpr LinearShape kLinearShape[] = {{16, 16, 512}, {16, 32, 512}, {16, 64, 5
 constexpr int kLinearShapes = sizeof(kLinearShape) / sizeof(LinearShape);
 constexpr LinearShape kLinearStaged[] = {{16, 16, 512}, {16, 32, 512}, {32, 32, 256}, {64, 64, 128}, {128, 128, 128}};
 constexpr int kLinearStagedShapes = sizeof(kLinearStaged) / sizeof(LinearShape);
+// (fp32 has no use for three of them: the matrix cores are the limit, and smaller tiles fill the CUs)
+constexpr bool linear_has(int es, bool direct, int shape) { return !(es == 4 && direct && (shape == 4 || shape == 6 || shape == 8)); }
 // of linear_quad_kernel (bf16, rows in whole pieces)
 constexpr LinearShape kLinearQuad[] = {{256, 256, 128}, {192, 256, 128}, {256, 128, 128}};
 constexpr int kLinearQuads = sizeof(kLinearQuad) / sizeof(LinearShape);

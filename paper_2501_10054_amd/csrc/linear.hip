@@ -149,6 +149,7 @@ Plan make_plan(const Call& c, int64_t room) {
         }
         if (p.at_part > room) continue;
         for (int s = 0; s < shapes_of(p.direct, c.es); ++s) {
+            if (!(p.direct && s >= kLinearShapes) && !linear_has(c.es, p.direct, s)) continue;
             const LinearShape& t = shape_of(p.direct, s);
             const Rate& r = p.direct ? (c.es == 2 ? kRate[s] : kRateF32[s]) : (c.es == 2 ? kRateStaged[s] : kRateStagedF32[s]);
             const int64_t slices = (p.k + t.slice - 1) / t.slice, tiles_n = (c.N + t.n - 1) / t.n;

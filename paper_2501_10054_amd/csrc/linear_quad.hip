@@ -26,9 +26,11 @@ template <int NA, int NB> struct LinearQuad {
     static constexpr int kWaitB = NA + (SB - 2) * kPer, kWaitA = (SA - 2) * kPer, kWait = kWaitB < kWaitA ? kWaitB : kWaitA;
     static constexpr int kStart = (SA > SB ? NA : 0) + (SB - 2) * kPer + kFirst;   // loads behind those of slice 0 in the prologue
     static constexpr int kRowBytes = 4 * 16 * NB * 16 * 4;
-    static constexpr int fit(int n) { return n == 1 || (NA % n == 0 && n * kRowBytes <= kLdsBytes) ? n : fit(n - 1); }
-    static constexpr int RB = fit(NA), kRing = SA * UA + SB * UB, kLds = kRing > RB * kRowBytes ? kRing : RB * kRowBytes;
-    static_assert(SB >= 2 && kWait <= 63 && kStart <= 63 && kLds <= kLdsBytes, "slice buffers");
+    static constexpr int kRing = SA * UA + SB * UB;
+    // of `rows` row blocks of a wavefront so many at a time behind the products: a part of them that the ring has room for
+    static constexpr int fit(int rows, int n) { return n == 1 || (rows % n == 0 && n * kRowBytes <= kRing) ? n : fit(rows, n - 1); }
+    static constexpr int kLds = kRing;
+    static_assert(kRowBytes <= kRing && SB >= 2 && kWait <= 63 && kStart <= 63 && kLds <= kLdsBytes, "slice buffers");
     static_assert(2 * kPer <= NM - 4 && kFirst * kEvery >= NM && (kPer - 1) * kEvery + 1 < TOT && kEvery * NB > 12, "places of reads and loads");
 };
 
@@ -285,7 +287,7 @@ __global__ void __launch_bounds__(256, 1) linear_quad_kernel(LinearArgs p) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
         __builtin_amdgcn_s_barrier();
         hold();
-        finish_linear<bf16_t, GROUPED, 4, NR, NB, 2, 2, 1, G::fit(NR)>(p, b, acc, lds, tid);
+        finish_linear<bf16_t, GROUPED, 4, NR, NB, 2, 2, 1, G::fit(NR, NR)>(p, b, acc, lds, tid);
     };
     // The rows of a product or group are divided evenly between its tiles, and the row blocks of a tile are dealt out to the wavefronts in turns, so
     // that a tile which is not full takes fewer MFMAs.  (Each number of row blocks with its own accumulators and epilogue: where loops share them the

@@ -164,6 +164,7 @@ template <bool GROUPED> __device__ __forceinline__ int64_t token_of_row(const Li
 // is done to the elements is a loop; a thread finishes 8 neighbouring columns at once.
 template <typename T, bool GROUPED, int W, int FA, int FB, int WM, int WN, int WK, int RB>
 __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearBlock& b, f32x4_t (&acc)[FA][FB], unsigned char* lds, int tid) {
+    static_assert(FA % RB == 0, "all row blocks");
     constexpr bool OWN = WK == 1;
     static constexpr int kAtOnce = OWN ? 2 : 1;                  // (one wavefront on a SIMD: two rows side by side; 2048 x 16384 x 4096 210 -> 195 us)
     constexpr int COLS = OWN ? FB * 16 : WN * FB * 16, ROWS = OWN ? RB * 16 : WM * RB * 16, UNITS = COLS / 8, STRIDE = (OWN ? 64 : W * 64) / UNITS;
@@ -526,18 +527,18 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
 // ---------------------------------------------------------------- launches, for one element type
 namespace {
 
-template <typename F> void for_linear_shape(bool direct, int shape, F f) {
+template <typename T, typename F> void for_linear_shape(bool direct, int shape, F f) {
     if (direct) {
         switch (shape) {
             case 0: f(std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<5>{}); break;
             case 1: f(std::true_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<3>{}); break;
             case 2: f(std::true_type{}, num<1>{}, num<4>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<4>{}); break;
             case 3: f(std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<5>{}); break;
-            case 4: f(std::true_type{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<6>{}); break;
+            case 4: if constexpr (linear_has(sizeof(T), true, 4)) f(std::true_type{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<6>{}); break;
             case 5: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}, num<1>{}, num<6>{}); break;
-            case 6: f(std::true_type{}, num<4>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<5>{}); break;
+            case 6: if constexpr (linear_has(sizeof(T), true, 6)) f(std::true_type{}, num<4>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<5>{}); break;
             case 7: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<5>{}); break;
-            case 8: f(std::true_type{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<6>{}); break;
+            case 8: if constexpr (linear_has(sizeof(T), true, 8)) f(std::true_type{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<6>{}); break;
             case 9: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<5>{}); break;
             case 10: f(std::true_type{}, num<6>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}); break;
             case 11: f(std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<2>{}, num<5>{}); break;
@@ -558,7 +559,7 @@ template <typename T> tardis_status_t linear_init() {
     bool ok = true;
     for (int direct = 0; direct < 2; ++direct)
         for (int shape = 0; shape < (direct ? kLinearShapes : kLinearStagedShapes); ++shape)
-            for_linear_shape(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
+            for_linear_shape<T>(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
                 typedef LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring> G;
                 const LinearShape& is = direct ? kLinearShape[shape] : kLinearStaged[shape];
                 ok &= is.m == G::TM && is.n == G::TN && is.slice == G::SL;
@@ -572,7 +573,7 @@ template <typename T> tardis_status_t linear_init() {
 }
 
 template <typename T> void linear_launch(const LinearArgs& p, bool grouped, bool direct, int shape, int blocks, hipStream_t s) {
-    for_linear_shape(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
+    for_linear_shape<T>(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
         constexpr int bytes = LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>::kLds;
         if (grouped) hipLaunchKernelGGL((linear_kernel<T, true, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(512), bytes, s, p);
         else hipLaunchKernelGGL((linear_kernel<T, false, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(512), bytes, s, p);
