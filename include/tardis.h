@@ -387,7 +387,7 @@ tardis_status_t tardis_grouped_linear_workspace(const tardis_linear_desc* desc, 
 tardis_status_t tardis_moe_route(const void* logits, int64_t n, int64_t experts, int64_t k, int32_t dtype,
                                  int32_t renormalise, int32_t* ids, float* weights, int32_t* offsets, int32_t* order,
                                  int32_t* place, void* work, int64_t work_bytes, void* stream);
-tardis_status_t tardis_moe_route_workspace(int64_t n, int64_t experts, int64_t* bytes);
+tardis_status_t tardis_moe_route_workspace(int64_t n, int64_t experts, int64_t k, int64_t* bytes);
 
 /* y[t] = residual[t] + sum_j weights[t][j] z[place[t][j]] over the k slots of a token, in
  * this order, rounded once; a place outside of 0 .. rows - 1 is a dropped slot.

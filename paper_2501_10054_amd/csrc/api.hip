@@ -621,10 +621,10 @@ tardis_status_t tardis_grouped_linear(const tardis_linear_desc* desc, int64_t ex
                              static_cast<hipStream_t>(stream));
 }
 
-tardis_status_t tardis_moe_route_workspace(int64_t n, int64_t experts, int64_t* bytes) {
+tardis_status_t tardis_moe_route_workspace(int64_t n, int64_t experts, int64_t k, int64_t* bytes) {
     if (!bytes) return TARDIS_ERR_INVALID_ARG;
-    if (!rows_fit(n, 0) || experts < 1 || experts > kMaxExperts) return TARDIS_ERR_SHAPE;
-    *bytes = n > 0 ? (int64_t)td_route_work_bytes(n, experts) : 0;
+    if (!rows_fit(n, 0) || experts < 1 || experts > kMaxExperts || k < 1 || k > kMaxChosen || k > experts) return TARDIS_ERR_SHAPE;
+    *bytes = n > 0 ? (int64_t)td_route_work_bytes(n, experts, k) : 0;
     return TARDIS_OK;
 }
 
@@ -638,7 +638,7 @@ tardis_status_t tardis_moe_route(const void* logits, int64_t n, int64_t experts,
     if (!aligned_to(logits, td_elem_size(dtype)) || !aligned_to(ids, 4) || !aligned_to(weights, 4) || !aligned_to(order, 4) || !aligned_to(place, 4) ||
         !aligned_to(work, 4))
         return TARDIS_ERR_INVALID_ARG;
-    if (n > 0 && td_route_work_bytes(n, experts) > 0 && (!work || work_bytes < (int64_t)td_route_work_bytes(n, experts))) return TARDIS_ERR_INVALID_ARG;
+    if (n > 0 && td_route_work_bytes(n, experts, k) > 0 && (!work || work_bytes < (int64_t)td_route_work_bytes(n, experts, k))) return TARDIS_ERR_INVALID_ARG;
     return td_moe_route(logits, n, experts, k, dtype, renormalise, ids, weights, offsets, order, place, work, static_cast<hipStream_t>(stream));
 }
 

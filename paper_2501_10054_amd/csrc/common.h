@@ -330,7 +330,7 @@ tardis_status_t td_linear(const tardis_linear_desc* d, const void* x, int64_t n,
 tardis_status_t td_grouped_linear(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, const int32_t* offsets,
                                   const int32_t* order, int64_t per_token, int64_t positions, void* y, void* work, int64_t work_bytes, hipStream_t s);
 // experts.hip
-size_t td_route_work_bytes(int64_t n, int64_t experts);
+size_t td_route_work_bytes(int64_t n, int64_t experts, int64_t k);
 tardis_status_t td_moe_route(const void* logits, int64_t n, int64_t experts, int64_t k, int32_t dtype, int renormalise, int32_t* ids, float* weights,
                              int32_t* offsets, int32_t* order, int32_t* place, void* work, hipStream_t s);
 tardis_status_t td_moe_combine(const void* z, int64_t rows, const int32_t* place, const float* weights, int64_t n, int64_t k, int64_t d, int32_t dtype,

@@ -13,10 +13,10 @@ namespace {
 // in a fixed order, so the result is the same in every run.
 //
 // What bounds it: round trips and, for many tokens, the vector instructions of the choice (16384 tokens, 128 experts, 8 chosen, in 64 blocks 25 us,
-// in 256 @CHOOSE).  One block does all of a call of up to kRounds tokens for each of its groups of lanes; more take two launches, the choice with
+// in 256 @CHOOSE).  One block does all of a call of few tokens (tokens_of_block); more take two launches, the choice with
 // the counts of every block, then the placement, for which every block adds up the counts of those before it (at most kMostBlocks), which
 // costs less than a launch of its own for that.
-constexpr int kRouteThreads = 1024, kRounds = 2, kMostBlocks = 256, kRouteWaves = kRouteThreads / 64;
+constexpr int kRouteThreads = 1024, kMostBlocks = 256, kRouteWaves = kRouteThreads / 64;
 
 struct RouteArgs {
     const void* logits;
@@ -111,15 +111,29 @@ __device__ __forceinline__ int scan_of_wave(int v, int lane) {
     return v;
 }
 
-// `all`, `before`: how often an expert is chosen by all blocks, by the blocks before this one; `from`: kRouteWaves x experts
-__device__ __forceinline__ void place_slots(const RouteArgs& p, int64_t first, int tokens, const int32_t* all, const int32_t* before, int32_t* from,
-                                            int32_t* sums) {
+// The slots [begin, end) of a wavefront, of the block's from slot0 on, and the expert of this lane's first one
+struct Slots {
+    int64_t slot0, slots, begin, end;
+    int id;
+};
+__device__ __forceinline__ Slots slots_of(const RouteArgs& p, int64_t first, int tokens) {
+    Slots s;
+    s.slots = (int64_t)tokens * p.k;
+    s.slot0 = first * p.k;
+    const int64_t per_wave = (s.slots + kRouteThreads - 1) / kRouteThreads * 64;
+    s.begin = min(s.slots, (threadIdx.x >> 6) * per_wave);
+    s.end = min(s.slots, s.begin + per_wave);
+    const int64_t i = s.begin + (threadIdx.x & 63);
+    s.id = i < s.end ? p.ids[s.slot0 + i] : -1;
+    return s;
+}
+
+// `all`, `before`: how often an expert is chosen by all blocks, by the blocks before this one; `from`: kRouteWaves x experts zeros
+__device__ __forceinline__ void place_slots(const RouteArgs& p, const Slots& s, const int32_t* all, const int32_t* before, int32_t* from, int32_t* sums) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int64_t slots = (int64_t)tokens * p.k, per_wave = (slots + kRouteThreads - 1) / kRouteThreads * 64;
-    const int64_t slot0 = first * p.k, begin = min(slots, wave * per_wave), end = min(slots, begin + per_wave);
-    for (int i = tid; i < kRouteWaves * p.experts; i += kRouteThreads) from[i] = 0;
-    __syncthreads();
-    for (int64_t i = begin + lane; i < end; i += 64) {
+    const int64_t slot0 = s.slot0, slots = s.slots, begin = s.begin, end = s.end;
+    if (s.id >= 0) atomicAdd(from + wave * p.experts + s.id, 1);
+    for (int64_t i = begin + 64 + lane; i < end; i += 64) {
         const int id = p.ids[slot0 + i];
         if (id >= 0) atomicAdd(from + wave * p.experts + id, 1);
     }
@@ -128,6 +142,7 @@ __device__ __forceinline__ void place_slots(const RouteArgs& p, int64_t first, i
     if (lane == 63) sums[wave] = upto;
     __syncthreads();
     int offset = upto - mine, total = 0;
+#pragma unroll
     for (int w = 0; w < kRouteWaves; ++w) {
         offset += w < wave ? sums[w] : 0;
         total += sums[w];
@@ -137,11 +152,13 @@ __device__ __forceinline__ void place_slots(const RouteArgs& p, int64_t first, i
             p.offsets[tid] = offset;
             if (tid == 0) p.offsets[p.experts] = total;
         }
-        int at = offset + before[tid];
+        int at = offset + before[tid], c[kRouteWaves];
+#pragma unroll
+        for (int w = 0; w < kRouteWaves; ++w) c[w] = from[w * p.experts + tid];
+#pragma unroll
         for (int w = 0; w < kRouteWaves; ++w) {
-            const int c = from[w * p.experts + tid];
             from[w * p.experts + tid] = at;
-            at += c;
+            at += c[w];
         }
     }
     __syncthreads();
@@ -149,7 +166,7 @@ __device__ __forceinline__ void place_slots(const RouteArgs& p, int64_t first, i
     volatile int32_t* next = from + wave * p.experts;
     for (int64_t i0 = begin; i0 < end; i0 += 64) {
         const int64_t i = i0 + lane;
-        const int id = i < end ? p.ids[slot0 + i] : -1;
+        const int id = i0 == begin ? s.id : i < end ? p.ids[slot0 + i] : -1;
         uint64_t same = __ballot(id >= 0);                        // lanes with this one's expert
         for (int bit = 0; bit < bits; ++bit) {
             const uint64_t set = __ballot((id >> bit) & 1);
@@ -179,12 +196,14 @@ template <typename T, int G, int V, bool ALONE> __global__ void __launch_bounds_
         counts[tid] = 0;
         if (ALONE) zeros[tid] = 0;
     }
+    if (ALONE)
+        for (int i = tid; i < kRouteWaves * p.experts; i += kRouteThreads) from[i] = 0;
     __syncthreads();
     const int64_t first = (int64_t)blockIdx.x * p.tokens;
     const int tokens = (int)min((int64_t)p.tokens, p.n - first);
     choose_experts<T, G, V>(p, first, tokens, counts);
     __syncthreads();
-    if constexpr (ALONE) place_slots(p, first, tokens, counts, zeros, from, sums);
+    if constexpr (ALONE) place_slots(p, slots_of(p, first, tokens), counts, zeros, from, sums);
     else if (tid < counts_of_row(p.experts)) p.counts[(int64_t)blockIdx.x * counts_of_row(p.experts) + tid] = tid < p.experts ? counts[tid] : 0;
 }
 
@@ -193,7 +212,10 @@ __global__ void __launch_bounds__(kRouteThreads) route_place_kernel(RouteArgs p)
     __shared__ int32_t sums[kRouteWaves];
     int32_t *all = words, *before = words + p.experts, *from = before + p.experts;
     const int tid = threadIdx.x, blocks = (int)gridDim.x, mine = (int)blockIdx.x;
+    const int64_t first = (int64_t)mine * p.tokens;
+    const Slots slots = slots_of(p, first, (int)min((int64_t)p.tokens, p.n - first));
     if (tid < p.experts) all[tid] = before[tid] = 0;
+    for (int i = tid; i < kRouteWaves * p.experts; i += kRouteThreads) from[i] = 0;
     __syncthreads();
     // four neighbouring experts for a thread, of every `parts`-th block
     const int pieces = counts_of_row(p.experts) / 4, parts = kRouteThreads / pieces, part = tid / pieces, piece = tid % pieces;
@@ -215,8 +237,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_place_kernel(RouteArgs p)
             }
     }
     __syncthreads();
-    const int64_t first = (int64_t)mine * p.tokens;
-    place_slots(p, first, (int)min((int64_t)p.tokens, p.n - first), all, before, from, sums);
+    place_slots(p, slots, all, before, from, sums);
 }
 
 // f(lanes of a group, logits of a lane)
@@ -231,10 +252,18 @@ template <typename F> void for_experts(int64_t experts, F f) {
 }
 
 // Tokens of a block: all of them where one block does the call, else one for each of its groups of lanes, or so many that the blocks are no more
-// than kMostBlocks
-int64_t tokens_of_block(int64_t n, int64_t experts) {
-    const int64_t groups = kRouteThreads / (experts <= 128 ? 16 : 64);
-    return n <= kRounds * groups ? kRounds * groups : std::max(groups, (n + kMostBlocks - 1) / kMostBlocks);
+// than kMostBlocks.  One block where its rounds take less than a second launch and the adding up of counts, 8 us: a round is a load's way and for each
+// choice the instructions of V logits and of two sums over lanes (198 tokens, 4 experts, 3 chosen: 8.3 us in one block, 13.8 in two launches; 393
+// tokens, 75 experts, 3 chosen 23.7 and @TWO).
+int64_t tokens_of_block(int64_t n, int64_t experts, int64_t k) {
+    int64_t groups = 1, logits = 1;
+    for_experts(experts, [&](auto g, auto v) {
+        groups = kRouteThreads / decltype(g)::value;
+        logits = decltype(v)::value;
+    });
+    const int64_t rounds = (n + groups - 1) / groups;
+    if (rounds <= 1 || (double)rounds * (0.8 + 0.055 * (double)(k * (logits + 4))) < 8.0) return std::max<int64_t>(1, rounds) * groups;
+    return std::max(groups, (n + kMostBlocks - 1) / kMostBlocks);
 }
 
 template <typename T> void launch_route(RouteArgs& p, hipStream_t s) {
@@ -345,8 +374,8 @@ template <typename T, bool ALIKE> __global__ void __launch_bounds__(256) combine
 
 }  // namespace
 
-size_t td_route_work_bytes(int64_t n, int64_t experts) {
-    const int64_t tokens = tokens_of_block(n, experts), blocks = (n + tokens - 1) / tokens;
+size_t td_route_work_bytes(int64_t n, int64_t experts, int64_t k) {
+    const int64_t tokens = tokens_of_block(n, experts, k), blocks = (n + tokens - 1) / tokens;
     return blocks > 1 ? (size_t)blocks * counts_of_row((int)experts) * 4 : 0;
 }
 
@@ -358,7 +387,7 @@ tardis_status_t td_moe_route(const void* logits, int64_t n, int64_t experts, int
     p.experts = (int)experts;
     p.k = (int)k;
     p.renormalise = renormalise;
-    p.tokens = (int)tokens_of_block(n, experts);
+    p.tokens = (int)tokens_of_block(n, experts, k);
     p.ids = ids;
     p.weights = weights;
     p.offsets = offsets;

@@ -28,7 +28,7 @@ constexpr uint32_t kNowhere = 0xe0000000u;        // an offset past the end of a
 struct LinearShape { int m, n, slice; };
 constexpr LinearShape kLinearShape[] = {{16, 16, 512}, {16, 32, 512}, {16, 64, 512}, {32, 32, 256}, {32, 64, 256}, {64, 32, 256},
                                         {64, 64, 256}, {64, 64, 128}, {128, 64, 128}, {128, 128, 128}, {192, 128, 128},
-                                        {16, 16, 1024}, {32, 32, 512}};
+                                        {16, 16, 1024}, {32, 32, 512}, {64, 64, 128}, {64, 128, 128}, {128, 128, 128}};
 constexpr int kLinearShapes = sizeof(kLinearShape) / sizeof(LinearShape);
 constexpr LinearShape kLinearStaged[] = {{16, 16, 512}, {16, 32, 512}, {32, 32, 256}, {64, 64, 128}, {128, 128, 128}};
 constexpr int kLinearStagedShapes = sizeof(kLinearStaged) / sizeof(LinearShape);

@@ -76,30 +76,31 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, uint32_t
 // What a tile takes, in us:
 //     max(fixed x turns + slices x max(alone x turns, slice x tiles of a CU), 1.5 + bytes / tbs)
 // with `blocks` of them at once on a CU, in `turns` turns: alone is a slice's latency, slice its share of the CU.  Bytes: x, y (the ranges'
-// sums), W, and for every further row of tiles `again` of W.  The constants are those with which the choice is best: over 573 products and 140
-// grouped ones in bf16 (sizes from 64 x 64 to 16384 x 16384, 1 to 3000 rows, weights from HBM; every tile with 1, 2, 4 and 8 ranges) it takes 0.8 % more
-// than the best measured, fp32 (179, 39) 0.6 %, staged (169, 24) 0.6 %, staged fp32 (98) 0.3 %.
+// sums), W, and for every further row of tiles `again` of W.  The constants are those with which the choice is best: over 583 products and 151
+// grouped ones in bf16 (sizes from 64 x 64 to 16384 x 16384, 1 to 5000 rows, weights from HBM; every tile with 1, 2, 4 and 8 ranges) it takes 1.2 % more
+// than the best measured, fp32 (185, 39) 0.8 %, staged (179, 28) 1.0 %, staged fp32 (98) 0.3 %.
 struct Rate { int blocks; float alone, slice, fixed, tbs; };
-constexpr Rate kRate[] = {{2, 0.225f, 0.210f, 3.95f, 5.37f}, {2, 0.326f, 0.301f, 3.80f, 4.67f}, {1, 0.615f, 0.615f, 3.76f, 5.50f},
-                          {2, 0.235f, 0.204f, 3.83f, 4.78f}, {1, 0.331f, 0.331f, 3.90f, 5.23f}, {1, 0.270f, 0.270f, 4.13f, 3.95f},
-                          {1, 0.424f, 0.424f, 4.60f, 5.18f}, {2, 0.318f, 0.284f, 3.54f, 5.56f}, {1, 0.369f, 0.369f, 5.00f, 4.13f},
-                          {1, 0.573f, 0.573f, 5.64f, 5.07f}, {1, 0.693f, 0.693f, 7.39f, 3.63f}, {1, 0.373f, 0.373f, 4.50f, 4.87f},
-                          {1, 0.365f, 0.365f, 4.31f, 4.30f}, {1, 0.990f, 0.990f, 16.86f, 3.35f}, {1, 0.904f, 0.904f, 13.11f, 4.43f},
-                          {1, 0.753f, 0.753f, 9.74f, 4.69f}};
-constexpr Rate kRateF32[] = {{2, 0.289f, 0.237f, 4.20f, 5.49f}, {2, 0.369f, 0.344f, 4.12f, 6.19f}, {1, 0.947f, 0.947f, 3.86f, 6.19f},
-                             {2, 0.412f, 0.320f, 3.73f, 4.91f}, {1, 0.651f, 0.651f, 4.39f, 4.50f}, {1, 0.628f, 0.628f, 3.72f, 2.98f},
-                             {1, 1.174f, 1.174f, 4.69f, 6.50f}, {2, 0.635f, 0.537f, 4.23f, 3.39f}, {1, 1.116f, 1.116f, 5.30f, 2.64f},
-                             {1, 2.082f, 2.082f, 6.96f, 2.65f}, {1, 2.961f, 2.961f, 9.52f, 2.50f}, {1, 0.509f, 0.509f, 4.75f, 4.84f},
-                             {1, 0.699f, 0.699f, 3.88f, 4.42f}};
-constexpr Rate kRateStaged[] = {{2, 0.221f, 0.229f, 4.77f, 3.42f}, {1, 0.388f, 0.388f, 4.64f, 3.31f}, {2, 0.190f, 0.220f, 4.35f, 4.90f},
-                                {2, 0.221f, 0.216f, 4.33f, 2.86f}, {1, 0.570f, 0.570f, 6.95f, 2.84f}};
-constexpr Rate kRateStagedF32[] = {{2, 0.076f, 0.253f, 4.35f, 3.98f}, {1, 0.368f, 0.368f, 4.49f, 3.98f}, {2, 0.049f, 0.301f, 4.26f, 4.41f},
-                                   {2, 0.506f, 0.553f, 4.27f, 5.36f}, {1, 1.937f, 1.937f, 8.53f, 4.68f}};
+constexpr Rate kRate[] = {{2, 0.229f, 0.222f, 3.95f, 5.54f}, {2, 0.398f, 0.404f, 3.77f, 5.63f}, {1, 0.542f, 0.542f, 3.98f, 5.27f},
+                          {2, 0.247f, 0.205f, 3.95f, 4.77f}, {1, 0.331f, 0.331f, 3.96f, 5.27f}, {1, 0.276f, 0.276f, 4.13f, 4.16f},
+                          {1, 0.420f, 0.420f, 4.88f, 5.01f}, {2, 0.279f, 0.263f, 3.82f, 5.62f}, {1, 0.388f, 0.388f, 4.89f, 4.06f},
+                          {1, 0.527f, 0.527f, 6.25f, 4.71f}, {1, 0.624f, 0.624f, 8.23f, 3.17f}, {1, 0.375f, 0.375f, 4.56f, 5.53f},
+                          {1, 0.407f, 0.407f, 4.31f, 4.34f}, {5, 0.424f, 0.262f, 3.35f, 4.26f}, {3, 0.784f, 0.376f, 4.15f, 4.62f},
+                          {2, 0.694f, 0.569f, 5.86f, 3.41f}, {1, 0.902f, 0.902f, 22.72f, 3.43f}, {1, 0.946f, 0.946f, 15.02f, 4.27f},
+                          {1, 0.805f, 0.805f, 8.55f, 4.39f}};
+constexpr Rate kRateF32[] = {{2, 0.266f, 0.238f, 4.14f, 5.61f}, {2, 0.436f, 0.344f, 4.19f, 6.18f}, {1, 1.017f, 1.017f, 3.56f, 6.18f},
+                             {2, 0.368f, 0.323f, 3.75f, 4.50f}, {}, {1, 0.657f, 0.657f, 4.34f, 3.59f}, {}, {2, 0.644f, 0.542f, 4.62f, 3.49f}, {},
+                             {1, 2.075f, 2.075f, 6.39f, 2.50f}, {1, 3.086f, 3.086f, 8.00f, 3.83f}, {1, 0.483f, 0.483f, 4.53f, 4.86f},
+                             {1, 0.696f, 0.696f, 4.06f, 4.42f}, {5, 0.689f, 0.540f, 3.88f, 3.38f}, {3, 1.149f, 1.040f, 5.81f, 2.57f},
+                             {2, 2.066f, 2.073f, 7.14f, 5.23f}};
+constexpr Rate kRateStaged[] = {{2, 0.246f, 0.231f, 4.77f, 3.34f}, {1, 0.389f, 0.389f, 4.64f, 3.29f}, {2, 0.176f, 0.227f, 4.35f, 4.73f},
+                                {2, 0.228f, 0.214f, 4.34f, 2.79f}, {1, 0.560f, 0.560f, 7.05f, 2.77f}};
+constexpr Rate kRateStagedF32[] = {{2, 0.104f, 0.250f, 4.45f, 4.01f}, {1, 0.377f, 0.377f, 4.45f, 4.01f}, {2, 0.053f, 0.305f, 4.21f, 4.46f},
+                                   {2, 0.556f, 0.550f, 4.53f, 5.00f}, {1, 2.042f, 2.042f, 6.55f, 4.71f}};
 static_assert(sizeof(kRate) / sizeof(Rate) == kLinearShapes + kLinearQuads && sizeof(kRateF32) / sizeof(Rate) == kLinearShapes &&
               sizeof(kRateStaged) / sizeof(Rate) == kLinearStagedShapes && sizeof(kRateStagedF32) / sizeof(Rate) == kLinearStagedShapes, "a rate for each tile");
 // one more launch (2.5 on the GPU; callers that are not a graph wait for their host); a byte copied, of partial sums and outputs joined; sigma of an element of a tile, of eight wavefronts and of four
 constexpr double kLaunchUs = 4.0, kCopyUs = 1.0 / 4.5e6, kJoinUs = 1.0 / 5e6, kSigmaUs = 5.0 / 65536, kSigmaQuadUs = 8.0 / 65536;
-constexpr double kAgain = 0.31, kAgainF32 = 0.42, kAgainStaged = 0.23, kAgainStagedF32 = 0.41;
+constexpr double kAgain = 0.38, kAgainF32 = 0.44, kAgainStaged = 0.20, kAgainStagedF32 = 0.43;
 constexpr int64_t kMostTiles = 1 << 21;            // of a launch
 
 // What decides: sizes, types, alignment
@@ -155,7 +156,7 @@ Plan make_plan(const Call& c, int64_t room) {
             const int64_t slices = (p.k + t.slice - 1) / t.slice, tiles_n = (c.N + t.n - 1) / t.n;
             const double tiles_m = c.experts ? hit * std::max(1.0, (double)c.M / hit / t.m + 0.5) : (double)((c.M + t.m - 1) / t.m);
             if (tiles_m * (double)tiles_n >= kMostTiles && s + 1 < shapes_of(p.direct, c.es)) continue;
-            for (int splits = 1; splits <= 8; splits *= 2) {
+            for (int splits = 1; splits <= 16; splits *= 2) {
                 const double blocks = tiles_m * (double)tiles_n * splits;
                 if (splits > 1 && (c.experts || slices / splits < 4 || blocks > 1024 || p.at_part + splits * c.M * c.N * 4 > room)) break;
                 // (how many tiles groups have is an estimate)

@@ -132,20 +132,21 @@ template <int TM, bool EVEN> __device__ __forceinline__ bool find_group(const Li
     return false;
 }
 
-// The tile of a block: TM = 16 FA WM rows (tokens) x TN = 16 FB WN columns (rows of W), 8 wavefronts in a grid of WM x WN, times WK that
+// The tile of a block: TM = 16 FA WM rows (tokens) x TN = 16 FB WN columns (rows of W), W wavefronts in a grid of WM x WN, times WK that
 // divide K: a slice is 64 WK KS bytes of every row, of which a wavefront multiplies 64 KS, and every fragment of a slice is
 // read from LDS by WN (of W: WM) wavefronts only.  D slices are in LDS (DIRECT) or in registers, on their way to two in LDS.
 template <typename T, bool DIRECT, int FA, int FB, int WM, int WN, int WK, int KS, int D>
 struct LinearTile {
     static constexpr int TM = 16 * FA * WM, TN = 16 * FB * WN, SL = 64 * WK * KS;
-    static constexpr int UA = TM * SL, UB = TN * SL, LA = UA / 8192, LB = UB / 8192;    // bytes of a slice, loads (16 bytes a lane) of a wavefront
+    static constexpr int W = WM * WN * WK;
+    static constexpr int UA = TM * SL, UB = TN * SL, LA = UA / (1024 * W), LB = UB / (1024 * W);    // bytes of a slice, loads (16 bytes a lane) of a wavefront
     static constexpr int kRing = (DIRECT ? D : 2) * (UA + UB);
     // row blocks of a wavefront that pass through LDS at a time behind the products: as many as the ring has room for
     static constexpr int kRowBytes = WK * WM * 16 * TN * 4;
     static constexpr int fit(int n) { return n == 1 || (FA % n == 0 && n * kRowBytes <= kRing) ? n : fit(n - 1); }
     static constexpr int RB = fit(FA), kLds = RB * kRowBytes > kRing ? RB * kRowBytes : kRing;
-    static_assert(WM * WN * WK == 8 && UA % 8192 == 0 && UB % 8192 == 0 && kLds <= kLdsBytes, "eight wavefronts, whole loads");
-    static_assert(DIRECT ? D >= 3 && (D - 1) * (LA + LB) <= 63 : D % 2 == 0, "slices under way");
+    static_assert((W == 8 || W == 4) && UA % (1024 * W) == 0 && UB % (1024 * W) == 0 && kLds <= kLdsBytes, "whole loads");
+    static_assert(DIRECT ? D >= 2 && (D - 1) * (LA + LB) <= 63 : D % 2 == 0, "slices under way");
 };
 
 // the row of x that is row m of this block's; -1: none
@@ -264,7 +265,7 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
 // DIRECT: x and W in whole, aligned pieces of 16 bytes, which go from memory straight to LDS; D - 1 slices are under way.  Else (odd
 // widths, odd pitches, rows that are 4 GB apart): through registers, D slices ahead, whatever the alignment.
 template <typename T, bool GROUPED, bool DIRECT, int FA, int FB, int WM, int WN, int WK, int KS, int D>
-__global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
+__global__ void __launch_bounds__(64 * WM * WN * WK, 2) linear_kernel(LinearArgs p) {
     typedef LinearTile<T, DIRECT, FA, FB, WM, WN, WK, KS, D> G;
     constexpr int TM = G::TM, TN = G::TN, SL = G::SL, LA = G::LA, LB = G::LB, PS = SL / 16, RPL = 64 / PS, SWZ = PS < 16 ? PS - 1 : 15;
     extern __shared__ __align__(1024) unsigned char lds[];
@@ -300,8 +301,8 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
     auto slice_of = [&](int t) { return b.s0 + (t >= whole ? t : t + rot >= whole ? t + rot - whole : t + rot); };
 
     // A load is RPL rows x SL bytes: lane -> row lane / PS, slot lane % PS, which holds piece slot ^ row (so the 16 rows of a fragment
-    // hit all banks).  Wavefront w loads rows [w TM / 8, (w + 1) TM / 8) of x, of W alike.
-    const int row_a = wave * (TM / 8) + lane / PS, row_b = wave * (TN / 8) + lane / PS;
+    // hit all banks).  Wavefront w loads the w-th part of the rows of x, of W alike.
+    const int row_a = wave * (TM / G::W) + lane / PS, row_b = wave * (TN / G::W) + lane / PS;
     auto piece_of_row = [&](int row) { return (uint32_t)((lane % PS) ^ (row & SWZ)) * 16u; };
     auto token_of = [&](int m) { return token_of_row<GROUPED>(p, b, m); };
 
@@ -363,7 +364,7 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
         }
 #pragma unroll
         for (int i = 0; i < LA; ++i) asm volatile("" : "+v"(off_a[i]));   // (waited for here, not between the loads below)
-        const uint32_t to_a = base + (uint32_t)wave * (G::UA / 8), to_b = base + (uint32_t)(D * G::UA) + (uint32_t)wave * (G::UB / 8);
+        const uint32_t to_a = base + (uint32_t)wave * (G::UA / G::W), to_b = base + (uint32_t)(D * G::UA) + (uint32_t)wave * (G::UB / G::W);
         auto load_slice = [&](int t, uint32_t slot) {     // (past the last slice: an empty buffer)
             const bool live = t < b.nk;
             const uint32_t soff = live ? (uint32_t)slice_of(t) * SL : 0u;
@@ -456,10 +457,10 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
             td_u32x4 a[LA], b[LB];
         };
         auto to_lds = [&](const Pieces& v, int place) {
-            unsigned char* at = lds + wave * (G::UA / 8) + place * G::UA + lane * 16;
+            unsigned char* at = lds + wave * (G::UA / G::W) + place * G::UA + lane * 16;
 #pragma unroll
             for (int i = 0; i < LA; ++i) *reinterpret_cast<td_u32x4*>(at + i * 1024) = v.a[i];
-            at = lds + 2 * G::UA + wave * (G::UB / 8) + place * G::UB + lane * 16;
+            at = lds + 2 * G::UA + wave * (G::UB / G::W) + place * G::UB + lane * 16;
 #pragma unroll
             for (int i = 0; i < LB; ++i) *reinterpret_cast<td_u32x4*>(at + i * 1024) = v.b[i];
         };
@@ -519,7 +520,7 @@ __global__ void __launch_bounds__(512, 2) linear_kernel(LinearArgs p) {
     }
     __syncthreads();
 
-    finish_linear<T, GROUPED, 8, FA, FB, WM, WN, WK, G::RB>(p, b, acc, lds, tid);
+    finish_linear<T, GROUPED, G::W, FA, FB, WM, WN, WK, G::RB>(p, b, acc, lds, tid);
 }
 
 }  // namespace
@@ -542,7 +543,12 @@ template <typename T, typename F> void for_linear_shape(bool direct, int shape, 
             case 9: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<5>{}); break;
             case 10: f(std::true_type{}, num<6>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}); break;
             case 11: f(std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<2>{}, num<5>{}); break;
-            default: f(std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<2>{}, num<5>{}); break;
+            case 12: f(std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<2>{}, num<5>{}); break;
+            // short rows, whose tiles are mostly beginnings and ends: four wavefronts and two slices, so that 5, 3 and 2 of them are on a CU
+            // (3000 x 16384 x 256, us, best of the others / these: 66 / 56; 5000 x 2048 x 256 19.5 / 15.9; 600 x 8000 x 64 9.6 / 7.7)
+            case 13: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
+            case 14: f(std::true_type{}, num<2>{}, num<4>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
+            default: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
         }
     } else {
         switch (shape) {
@@ -574,9 +580,10 @@ template <typename T> tardis_status_t linear_init() {
 
 template <typename T> void linear_launch(const LinearArgs& p, bool grouped, bool direct, int shape, int blocks, hipStream_t s) {
     for_linear_shape<T>(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
-        constexpr int bytes = LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>::kLds;
-        if (grouped) hipLaunchKernelGGL((linear_kernel<T, true, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(512), bytes, s, p);
-        else hipLaunchKernelGGL((linear_kernel<T, false, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(512), bytes, s, p);
+        typedef LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring> G;
+        constexpr int bytes = G::kLds, threads = 64 * G::W;
+        if (grouped) hipLaunchKernelGGL((linear_kernel<T, true, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(threads), bytes, s, p);
+        else hipLaunchKernelGGL((linear_kernel<T, false, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(threads), bytes, s, p);
     });
 }
 

@@ -86,7 +86,7 @@ def lib() -> C.CDLL:
         L.tardis_grouped_linear.argtypes = [C.POINTER(tardis_linear_desc), i64, vp, i64, i64, vp, vp, i64, i64, vp, vp, i64, vp]
         L.tardis_grouped_linear_workspace.argtypes = [C.POINTER(tardis_linear_desc), i64, vp, i64, i64, C.c_int32, i64, C.POINTER(i64)]
         L.tardis_moe_route.argtypes = [vp, i64, i64, i64, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp, i64, vp]
-        L.tardis_moe_route_workspace.argtypes = [i64, i64, C.POINTER(i64)]
+        L.tardis_moe_route_workspace.argtypes = [i64, i64, i64, C.POINTER(i64)]
         L.tardis_moe_combine.argtypes = [vp, i64, vp, vp, i64, i64, i64, C.c_int32, vp, vp, C.c_int32, vp]
         L.tardis_destroy.argtypes = [vp]
         L.tardis_release_memory.argtypes = []
@@ -332,9 +332,9 @@ def _linear_work_bytes(sizes, experts, x_rows, pitch, ordered, rows, x_at, W_at)
 
 
 @functools.lru_cache(maxsize=1024)
-def _route_work_bytes(n, experts):
+def _route_work_bytes(n, experts, k):
     bytes_ = C.c_int64()
-    _check(lib().tardis_moe_route_workspace(n, experts, bytes_), "tardis_moe_route_workspace")
+    _check(lib().tardis_moe_route_workspace(n, experts, k, bytes_), "tardis_moe_route_workspace")
     return bytes_.value
 
 
@@ -404,7 +404,7 @@ def tardis_moe_route(logits, k: int, renormalise: bool = True, stream=None):
     ids, place, weights = _empty(n, k, torch.int32, dev), _empty(n, k, torch.int32, dev), _empty(n, k, torch.float32, dev)
     order = torch.empty_strided((n * k,), (1,), dtype=torch.int32, device=dev)
     offsets = torch.empty_strided((experts + 1,), (1,), dtype=torch.int32, device=dev)
-    bytes_ = _route_work_bytes(n, experts)
+    bytes_ = _route_work_bytes(n, experts, k)
     work = torch.empty(bytes_, dtype=torch.uint8, device=dev) if bytes_ else None
     _check(lib().tardis_moe_route(logits.data_ptr(), n, experts, k, _DTYPE_CODE[logits.dtype], 1 if renormalise else 0, ids.data_ptr(), weights.data_ptr(),
                                   offsets.data_ptr(), order.data_ptr(), place.data_ptr(), _ptr(work), bytes_, _stream(stream)), "tardis_moe_route")

@@ -93,13 +93,15 @@ def test_route_refuses():
         assert route(**kw) == T.ERR_SHAPE, kw
     assert route(dtype=T.FP8_E4M3) == T.ERR_DTYPE
     need = C.c_int64()
-    assert T.lib().tardis_moe_route_workspace(100000, 64, need) == T.OK and need.value > 0
+    assert T.lib().tardis_moe_route_workspace(100000, 64, 2, need) == T.OK and need.value > 0
     assert route(n=100000, experts=64) == T.ERR_INVALID_ARG                                        # none given
     assert route(n=100000, experts=64, work=P, bytes_=need.value - 1) == T.ERR_INVALID_ARG
-    assert T.lib().tardis_moe_route_workspace(8, 64, need) == T.OK and need.value == 0
-    assert T.lib().tardis_moe_route_workspace(8, 1025, need) == T.ERR_SHAPE
-    assert T.lib().tardis_moe_route_workspace(-1, 64, need) == T.ERR_SHAPE
-    assert T.lib().tardis_moe_route_workspace(8, 64, None) == T.ERR_INVALID_ARG
+    assert T.lib().tardis_moe_route_workspace(8, 64, 2, need) == T.OK and need.value == 0
+    assert T.lib().tardis_moe_route_workspace(8, 1025, 2, need) == T.ERR_SHAPE
+    assert T.lib().tardis_moe_route_workspace(-1, 64, 2, need) == T.ERR_SHAPE
+    assert T.lib().tardis_moe_route_workspace(8, 64, 17, need) == T.ERR_SHAPE
+    assert T.lib().tardis_moe_route_workspace(8, 2, 3, need) == T.ERR_SHAPE
+    assert T.lib().tardis_moe_route_workspace(8, 64, 2, None) == T.ERR_INVALID_ARG
 
 
 def test_combine_refuses():
