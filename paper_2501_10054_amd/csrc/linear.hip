@@ -76,17 +76,17 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, uint32_t
 // What a tile takes, in us:
 //     max(fixed x turns + slices x max(alone x turns, slice x tiles of a CU), 1.5 + bytes / tbs)
 // with `blocks` of them at once on a CU, in `turns` turns: alone is a slice's latency, slice its share of the CU.  Bytes: x, y (the ranges'
-// sums), W, and for every further row of tiles `again` of W.  The constants are those with which the choice is best: over 583 products and 151
-// grouped ones in bf16 (sizes from 64 x 64 to 16384 x 16384, 1 to 5000 rows, weights from HBM; every tile with 1, 2, 4 and 8 ranges) it takes 1.2 % more
+// sums), W, and for every further row of tiles `again` of W.  The constants are those with which the choice is best: over 583 products and 154
+// grouped ones in bf16 (sizes from 64 x 64 to 16384 x 16384, 1 to 5000 rows, weights from HBM; every tile with 1, 2, 4 and 8 ranges) it takes 1.3 % more
 // than the best measured, fp32 (185, 39) 0.8 %, staged (179, 28) 1.0 %, staged fp32 (98) 0.3 %.
 struct Rate { int blocks; float alone, slice, fixed, tbs; };
-constexpr Rate kRate[] = {{2, 0.229f, 0.222f, 3.95f, 5.54f}, {2, 0.398f, 0.404f, 3.77f, 5.63f}, {1, 0.542f, 0.542f, 3.98f, 5.27f},
-                          {2, 0.247f, 0.205f, 3.95f, 4.77f}, {1, 0.331f, 0.331f, 3.96f, 5.27f}, {1, 0.276f, 0.276f, 4.13f, 4.16f},
-                          {1, 0.420f, 0.420f, 4.88f, 5.01f}, {2, 0.279f, 0.263f, 3.82f, 5.62f}, {1, 0.388f, 0.388f, 4.89f, 4.06f},
-                          {1, 0.527f, 0.527f, 6.25f, 4.71f}, {1, 0.624f, 0.624f, 8.23f, 3.17f}, {1, 0.375f, 0.375f, 4.56f, 5.53f},
-                          {1, 0.407f, 0.407f, 4.31f, 4.34f}, {5, 0.424f, 0.262f, 3.35f, 4.26f}, {3, 0.784f, 0.376f, 4.15f, 4.62f},
-                          {2, 0.694f, 0.569f, 5.86f, 3.41f}, {1, 0.902f, 0.902f, 22.72f, 3.43f}, {1, 0.946f, 0.946f, 15.02f, 4.27f},
-                          {1, 0.805f, 0.805f, 8.55f, 4.39f}};
+constexpr Rate kRate[] = {{2, 0.229f, 0.220f, 3.96f, 5.53f}, {2, 0.418f, 0.403f, 3.77f, 5.55f}, {1, 0.544f, 0.544f, 3.98f, 5.27f},
+                          {2, 0.238f, 0.205f, 4.00f, 4.81f}, {1, 0.324f, 0.324f, 4.01f, 5.27f}, {1, 0.276f, 0.276f, 4.15f, 4.16f},
+                          {1, 0.405f, 0.405f, 4.84f, 5.01f}, {2, 0.275f, 0.265f, 3.82f, 5.46f}, {1, 0.373f, 0.373f, 4.85f, 3.97f},
+                          {1, 0.526f, 0.526f, 6.26f, 4.70f}, {1, 0.624f, 0.624f, 8.23f, 3.18f}, {1, 0.375f, 0.375f, 4.56f, 5.52f},
+                          {1, 0.401f, 0.401f, 4.31f, 4.24f}, {5, 0.613f, 0.262f, 3.08f, 4.53f}, {3, 0.770f, 0.368f, 4.10f, 4.62f},
+                          {2, 0.697f, 0.566f, 5.89f, 3.76f}, {1, 1.101f, 1.101f, 16.43f, 3.46f}, {1, 0.930f, 0.930f, 15.57f, 4.28f},
+                          {1, 0.803f, 0.803f, 8.51f, 4.37f}};
 constexpr Rate kRateF32[] = {{2, 0.266f, 0.238f, 4.14f, 5.61f}, {2, 0.436f, 0.344f, 4.19f, 6.18f}, {1, 1.017f, 1.017f, 3.56f, 6.18f},
                              {2, 0.368f, 0.323f, 3.75f, 4.50f}, {}, {1, 0.657f, 0.657f, 4.34f, 3.59f}, {}, {2, 0.644f, 0.542f, 4.62f, 3.49f}, {},
                              {1, 2.075f, 2.075f, 6.39f, 2.50f}, {1, 3.086f, 3.086f, 8.00f, 3.83f}, {1, 0.483f, 0.483f, 4.53f, 4.86f},

@@ -160,3 +160,14 @@ def test_another_stream_and_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(y, want)
         assert torch.equal(experts_layer(t, *weights, k)[0], want)
+
+
+def test_the_example_runs():
+    """examples/expert_layer.py: two bf16 roundings on the way and one at the end, 2^-8 each at most in the norm."""
+    import importlib.util
+    import os
+    at = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "expert_layer.py")
+    spec = importlib.util.spec_from_file_location("expert_layer", at)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    assert example.main(tokens=40, width=256, hidden=136, experts=12, chosen=3) < 3 * 2.0 ** -8
