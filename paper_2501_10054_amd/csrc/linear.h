@@ -23,8 +23,7 @@ struct LinearArgs {
 constexpr int kActGelu16 = 4;                     // behind tardis_act_t's: GELU for outputs in bf16
 constexpr uint32_t kNowhere = 0xe0000000u;        // an offset past the end of any operand that is loaded by offsets
 
-// The tiles: rows, columns, wavefronts that divide K (a slice is 64 bytes of each).  f(row blocks, column blocks of a wavefront, grid of
-// wavefronts, wavefronts in K, slices in LDS)
+// The tiles: rows, columns and bytes of K in a slice (64 or 128 for each of the wavefronts that divide it)
 struct LinearShape { int m, n, slice; };
 constexpr LinearShape kLinearShape[] = {{16, 16, 512}, {16, 32, 512}, {16, 64, 512}, {32, 32, 256}, {32, 64, 256}, {64, 32, 256},
                                         {64, 64, 256}, {64, 64, 128}, {128, 64, 128}, {128, 128, 128}, {192, 128, 128},
@@ -32,8 +31,13 @@ constexpr LinearShape kLinearShape[] = {{16, 16, 512}, {16, 32, 512}, {16, 64, 5
 constexpr int kLinearShapes = sizeof(kLinearShape) / sizeof(LinearShape);
 constexpr LinearShape kLinearStaged[] = {{16, 16, 512}, {16, 32, 512}, {32, 32, 256}, {64, 64, 128}, {128, 128, 128}};
 constexpr int kLinearStagedShapes = sizeof(kLinearStaged) / sizeof(LinearShape);
-// (fp32 has no use for three of them: the matrix cores are the limit, and smaller tiles fill the CUs)
-constexpr bool linear_has(int es, bool direct, int shape) { return !(es == 4 && direct && (shape == 4 || shape == 6 || shape == 8)); }
+// The rule in linear.hip has no use for some of them: in fp32 the matrix cores are the limit, where few blocks with long slices gain nothing
+// and smaller tiles fill the CUs better; a group's rows are many only where the call has tiles enough for small ones.
+constexpr bool linear_has(int es, bool direct, bool grouped, int shape) {
+    if (!direct) return !(grouped && shape == 1);
+    if (es == 2) return !(grouped && shape == 8);
+    return !(shape == 2 || (shape >= 4 && shape <= 9) || shape == 12 || (grouped && (shape == 10 || shape == 15)));
+}
 // of linear_quad_kernel (bf16, rows in whole pieces)
 constexpr LinearShape kLinearQuad[] = {{256, 256, 128}, {192, 256, 128}, {256, 128, 128}};
 constexpr int kLinearQuads = sizeof(kLinearQuad) / sizeof(LinearShape);

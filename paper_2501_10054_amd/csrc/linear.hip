@@ -80,6 +80,7 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, uint32_t
 // grouped ones in bf16 (sizes from 64 x 64 to 16384 x 16384, 1 to 5000 rows, weights from HBM; every tile with 1, 2, 4 and 8 ranges) it takes 1.3 % more
 // than the best measured, fp32 (185, 39) 0.8 %, staged (179, 28) 1.0 %, staged fp32 (98) 0.3 %.
 struct Rate { int blocks; float alone, slice, fixed, tbs; };
+// ({}: a tile that is not there, linear_has)
 constexpr Rate kRate[] = {{2, 0.229f, 0.220f, 3.96f, 5.53f}, {2, 0.418f, 0.403f, 3.77f, 5.55f}, {1, 0.544f, 0.544f, 3.98f, 5.27f},
                           {2, 0.238f, 0.205f, 4.00f, 4.81f}, {1, 0.324f, 0.324f, 4.01f, 5.27f}, {1, 0.276f, 0.276f, 4.15f, 4.16f},
                           {1, 0.405f, 0.405f, 4.84f, 5.01f}, {2, 0.275f, 0.265f, 3.82f, 5.46f}, {1, 0.373f, 0.373f, 4.85f, 3.97f},
@@ -87,11 +88,9 @@ constexpr Rate kRate[] = {{2, 0.229f, 0.220f, 3.96f, 5.53f}, {2, 0.418f, 0.403f,
                           {1, 0.401f, 0.401f, 4.31f, 4.24f}, {5, 0.613f, 0.262f, 3.08f, 4.53f}, {3, 0.770f, 0.368f, 4.10f, 4.62f},
                           {2, 0.697f, 0.566f, 5.89f, 3.76f}, {1, 1.101f, 1.101f, 16.43f, 3.46f}, {1, 0.930f, 0.930f, 15.57f, 4.28f},
                           {1, 0.803f, 0.803f, 8.51f, 4.37f}};
-constexpr Rate kRateF32[] = {{2, 0.266f, 0.238f, 4.14f, 5.61f}, {2, 0.436f, 0.344f, 4.19f, 6.18f}, {1, 1.017f, 1.017f, 3.56f, 6.18f},
-                             {2, 0.368f, 0.323f, 3.75f, 4.50f}, {}, {1, 0.657f, 0.657f, 4.34f, 3.59f}, {}, {2, 0.644f, 0.542f, 4.62f, 3.49f}, {},
-                             {1, 2.075f, 2.075f, 6.39f, 2.50f}, {1, 3.086f, 3.086f, 8.00f, 3.83f}, {1, 0.483f, 0.483f, 4.53f, 4.86f},
-                             {1, 0.696f, 0.696f, 4.06f, 4.42f}, {5, 0.689f, 0.540f, 3.88f, 3.38f}, {3, 1.149f, 1.040f, 5.81f, 2.57f},
-                             {2, 2.066f, 2.073f, 7.14f, 5.23f}};
+constexpr Rate kRateF32[] = {{2, 0.266f, 0.238f, 4.14f, 5.61f}, {2, 0.436f, 0.344f, 4.19f, 6.18f}, {}, {2, 0.368f, 0.323f, 3.75f, 4.50f},
+                             {}, {}, {}, {}, {}, {}, {1, 3.086f, 3.086f, 8.00f, 3.83f}, {1, 0.483f, 0.483f, 4.53f, 4.86f},
+                             {}, {5, 0.689f, 0.540f, 3.88f, 3.38f}, {3, 1.149f, 1.040f, 5.81f, 2.57f}, {2, 2.066f, 2.073f, 7.14f, 5.23f}};
 constexpr Rate kRateStaged[] = {{2, 0.246f, 0.231f, 4.77f, 3.34f}, {1, 0.389f, 0.389f, 4.64f, 3.29f}, {2, 0.176f, 0.227f, 4.35f, 4.73f},
                                 {2, 0.228f, 0.214f, 4.34f, 2.79f}, {1, 0.560f, 0.560f, 7.05f, 2.77f}};
 constexpr Rate kRateStagedF32[] = {{2, 0.104f, 0.250f, 4.45f, 4.01f}, {1, 0.377f, 0.377f, 4.45f, 4.01f}, {2, 0.053f, 0.305f, 4.21f, 4.46f},
@@ -150,7 +149,7 @@ Plan make_plan(const Call& c, int64_t room) {
         }
         if (p.at_part > room) continue;
         for (int s = 0; s < shapes_of(p.direct, c.es); ++s) {
-            if (!(p.direct && s >= kLinearShapes) && !linear_has(c.es, p.direct, s)) continue;
+            if (!(p.direct && s >= kLinearShapes) && !linear_has(c.es, p.direct, c.experts > 0, s)) continue;
             const LinearShape& t = shape_of(p.direct, s);
             const Rate& r = p.direct ? (c.es == 2 ? kRate[s] : kRateF32[s]) : (c.es == 2 ? kRateStaged[s] : kRateStagedF32[s]);
             const int64_t slices = (p.k + t.slice - 1) / t.slice, tiles_n = (c.N + t.n - 1) / t.n;

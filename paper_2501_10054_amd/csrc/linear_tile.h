@@ -260,7 +260,6 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
     });
 }
 
-
 // What bounds it: few rows - the weights' stream from HBM; many - the way from L2 to LDS (tiles below 192 x 128) and the matrix cores.
 // DIRECT: x and W in whole, aligned pieces of 16 bytes, which go from memory straight to LDS; D - 1 slices are under way.  Else (odd
 // widths, odd pitches, rows that are 4 GB apart): through registers, D slices ahead, whatever the alignment.
@@ -528,63 +527,72 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, 2) linear_kernel(LinearArgs
 // ---------------------------------------------------------------- launches, for one element type
 namespace {
 
-template <typename T, typename F> void for_linear_shape(bool direct, int shape, F f) {
+// f(direct, row and column blocks of a wavefront, grid of wavefronts, wavefronts and half-lines of each in K, slices in LDS)
+template <typename T, bool GROUPED, typename F> void for_linear_shape(bool direct, int shape, F f) {
+    auto use = [&](auto number, auto d, auto... tile) {
+        if constexpr (linear_has(sizeof(T), decltype(d)::value, GROUPED, decltype(number)::value)) f(d, tile...);
+    };
     if (direct) {
         switch (shape) {
-            case 0: f(std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<5>{}); break;
-            case 1: f(std::true_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<3>{}); break;
-            case 2: f(std::true_type{}, num<1>{}, num<4>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<4>{}); break;
-            case 3: f(std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<5>{}); break;
-            case 4: if constexpr (linear_has(sizeof(T), true, 4)) f(std::true_type{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<6>{}); break;
-            case 5: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}, num<1>{}, num<6>{}); break;
-            case 6: if constexpr (linear_has(sizeof(T), true, 6)) f(std::true_type{}, num<4>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<5>{}); break;
-            case 7: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<5>{}); break;
-            case 8: if constexpr (linear_has(sizeof(T), true, 8)) f(std::true_type{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<6>{}); break;
-            case 9: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<5>{}); break;
-            case 10: f(std::true_type{}, num<6>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}); break;
-            case 11: f(std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<2>{}, num<5>{}); break;
-            case 12: f(std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<2>{}, num<5>{}); break;
+            case 0: use(num<0>{}, std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<5>{}); break;
+            case 1: use(num<1>{}, std::true_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<3>{}); break;
+            case 2: use(num<2>{}, std::true_type{}, num<1>{}, num<4>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<4>{}); break;
+            case 3: use(num<3>{}, std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<5>{}); break;
+            case 4: use(num<4>{}, std::true_type{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<6>{}); break;
+            case 5: use(num<5>{}, std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}, num<1>{}, num<6>{}); break;
+            case 6: use(num<6>{}, std::true_type{}, num<4>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<5>{}); break;
+            case 7: use(num<7>{}, std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<5>{}); break;
+            case 8: use(num<8>{}, std::true_type{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<6>{}); break;
+            case 9: use(num<9>{}, std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<5>{}); break;
+            case 10: use(num<10>{}, std::true_type{}, num<6>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}); break;
+            case 11: use(num<11>{}, std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<2>{}, num<5>{}); break;
+            case 12: use(num<12>{}, std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<2>{}, num<5>{}); break;
             // short rows, whose tiles are mostly beginnings and ends: four wavefronts and two slices, so that 5, 3 and 2 of them are on a CU
             // (3000 x 16384 x 256, us, best of the others / these: 66 / 56; 5000 x 2048 x 256 19.5 / 15.9; 600 x 8000 x 64 9.6 / 7.7)
-            case 13: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
-            case 14: f(std::true_type{}, num<2>{}, num<4>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
-            default: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
+            case 13: use(num<13>{}, std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
+            case 14: use(num<14>{}, std::true_type{}, num<2>{}, num<4>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
+            default: use(num<15>{}, std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
         }
     } else {
         switch (shape) {
-            case 0: f(std::false_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<6>{}); break;
-            case 1: f(std::false_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<4>{}); break;
-            case 2: f(std::false_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<4>{}); break;
-            case 3: f(std::false_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}); break;
-            default: f(std::false_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}); break;
+            case 0: use(num<0>{}, std::false_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<6>{}); break;
+            case 1: use(num<1>{}, std::false_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<4>{}); break;
+            case 2: use(num<2>{}, std::false_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<4>{}); break;
+            case 3: use(num<3>{}, std::false_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}); break;
+            default: use(num<4>{}, std::false_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}); break;
         }
     }
 }
 
-template <typename T> tardis_status_t linear_init() {
+template <typename T, bool GROUPED> bool linear_raise() {
     bool ok = true;
     for (int direct = 0; direct < 2; ++direct)
         for (int shape = 0; shape < (direct ? kLinearShapes : kLinearStagedShapes); ++shape)
-            for_linear_shape<T>(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
+            for_linear_shape<T, GROUPED>(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
                 typedef LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring> G;
                 const LinearShape& is = direct ? kLinearShape[shape] : kLinearStaged[shape];
                 ok &= is.m == G::TM && is.n == G::TN && is.slice == G::SL;
-                auto raise = [&](auto kernel) {
-                    ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds) == hipSuccess;
-                };
-                raise(linear_kernel<T, false, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>);
-                raise(linear_kernel<T, true, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>);
+                ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(linear_kernel<T, GROUPED, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>),
+                                          hipFuncAttributeMaxDynamicSharedMemorySize, G::kLds) == hipSuccess;
             });
-    return ok ? TARDIS_OK : TARDIS_ERR_HIP;
+    return ok;
+}
+
+template <typename T> tardis_status_t linear_init() {
+    return linear_raise<T, false>() && linear_raise<T, true>() ? TARDIS_OK : TARDIS_ERR_HIP;
+}
+
+template <typename T, bool GROUPED> void linear_launch(const LinearArgs& p, bool direct, int shape, int blocks, hipStream_t s) {
+    for_linear_shape<T, GROUPED>(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
+        typedef LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring> G;
+        constexpr int bytes = G::kLds, threads = 64 * G::W;
+        hipLaunchKernelGGL((linear_kernel<T, GROUPED, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(threads), bytes, s, p);
+    });
 }
 
 template <typename T> void linear_launch(const LinearArgs& p, bool grouped, bool direct, int shape, int blocks, hipStream_t s) {
-    for_linear_shape<T>(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
-        typedef LinearTile<T, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring> G;
-        constexpr int bytes = G::kLds, threads = 64 * G::W;
-        if (grouped) hipLaunchKernelGGL((linear_kernel<T, true, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(threads), bytes, s, p);
-        else hipLaunchKernelGGL((linear_kernel<T, false, decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(threads), bytes, s, p);
-    });
+    if (grouped) linear_launch<T, true>(p, direct, shape, blocks, s);
+    else linear_launch<T, false>(p, direct, shape, blocks, s);
 }
 
 }  // namespace

@@ -3,7 +3,7 @@
 
 extern "C" {
 int linear_probe_shapes(int f32, int direct) { return direct ? kLinearShapes + (f32 ? 0 : kLinearQuads) : kLinearStagedShapes; }
-int linear_probe_has(int f32, int direct, int shape) { return (direct && shape >= kLinearShapes) || linear_has(f32 ? 4 : 2, direct, shape); }
+int linear_probe_has(int f32, int direct, int grouped, int shape) { return (direct && shape >= kLinearShapes) || linear_has(f32 ? 4 : 2, direct, grouped, shape); }
 void linear_probe_tile(int direct, int shape, int* out) {
     const LinearShape& s = !direct ? kLinearStaged[shape] : shape < kLinearShapes ? kLinearShape[shape] : kLinearQuad[shape - kLinearShapes];
     out[0] = s.m;
@@ -13,6 +13,7 @@ void linear_probe_tile(int direct, int shape, int* out) {
 // experts = 0: one matrix; ranges > 1: y has the sums of the ranges
 int linear_probe(int f32, int direct, int shape, const void* x, int64_t x_rows, int64_t pitch, const void* W, const void* b, const void* r, void* y, int64_t rows,
                  int64_t N, int64_t k, int act, int out_f32, int ranges, const int32_t* offsets, const int32_t* order, int experts, int per_token, void* stream) {
+    if (!linear_probe_has(f32, direct, experts > 0, shape)) return TARDIS_ERR_SHAPE;
     int t[3];
     linear_probe_tile(direct, shape, t);
     LinearArgs p{};

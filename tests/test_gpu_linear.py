@@ -10,6 +10,7 @@ import math
 import pytest
 import torch
 
+from linear_calls import CALLS
 from paper_2501_10054_amd import tardis as T
 
 pytestmark = pytest.mark.gpu
@@ -211,3 +212,39 @@ def test_the_same_bits_in_every_run():
     for _ in range(10):
         assert torch.equal(a, T.tardis_linear(x, W, out_dtype=torch.float32))
         assert torch.equal(g, T.tardis_grouped_linear(x, We, offsets, out_dtype=torch.float32))
+
+
+@pytest.mark.parametrize("call", range(len(CALLS)))
+def test_every_kernel_as_its_calls_take_it(call):
+    _, dtype, n, n_in, n_out, gap, experts, k = CALLS[call]
+    dtype = torch.float32 if dtype == T.F32 else torch.bfloat16
+    gen, host = torch.Generator(device=DEV).manual_seed(400 + call), torch.Generator().manual_seed(400 + call)
+    x = inside((n, n_in), dtype, gen, gap=gap)
+    if not experts:
+        W = inside((n_out, n_in), dtype, gen, std=2.0 / math.sqrt(n_in))
+        check(T.tardis_linear(x, W, act="relu", out_dtype=torch.bfloat16), *layer64(x, W, None, "relu"))
+        return
+    W = inside((experts, n_out, n_in), dtype, gen, std=2.0 / math.sqrt(n_in))
+    offsets, order = random_groups(host, n * k, experts, "even"), torch.randperm(n * k, generator=host).int().to(DEV)
+    y = T.tardis_grouped_linear(x, W, offsets, act="relu", order=order, per_token=k, out_dtype=torch.bfloat16)
+    check(y, *grouped64(x, W, None, offsets, order, k, n * k, "relu"))
+
+
+def test_gelu_over_the_range_of_bf16():
+    """Every bf16 value goes through GELU in a layer of one input with weight 1, for outputs in bf16 (a fit of its own) and in fp32.
+
+    Tolerance: z is exact.  For outputs in fp32 sigma's error is below 2^-20 of z (as above); in bf16 Phi(-|z|) is off by less than 2^-14 of itself
+    (the fit, 3.4e-5, and five fp32 steps and two approximations of 2^-22), and the result is rounded once.  Below -13 the result leaves
+    the normal values: 1e-37 more."""
+    bits = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).to(DEV)
+    z = bits.view(torch.bfloat16)
+    z = z[torch.isfinite(z)][:, None].contiguous()
+    W = torch.ones(1, 1, dtype=torch.bfloat16, device=DEV)
+    zz = z.double()
+    q = 0.5 * torch.special.erfc(zz.abs() / math.sqrt(2.0))         # Phi(-|z|)
+    want = zz * torch.where(zz > 0, 1.0 - q, q)
+    for out, off in ((torch.bfloat16, 2.0 ** -14 * q * zz.abs()), (torch.float32, 2.0 ** -20 * zz.abs())):
+        y = T.tardis_linear(z, W, act="gelu_erf", out_dtype=out)
+        err = (y.double() - want).abs()
+        bound = off + (torch.finfo(out).eps / 2 + 2.0 ** -22) * (want.abs() + off) + 1e-37
+        assert (err <= bound).all(), (z[err > bound][:5], y[err > bound][:5])

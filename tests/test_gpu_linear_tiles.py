@@ -21,11 +21,11 @@ def _lib():
     return lib
 
 
-def _instances():
+def _instances(grouped=0):
     if not os.path.exists(B.LINEAR_PROBE):
         return []
     lib = _lib()
-    return [(f32, direct, s) for f32 in (0, 1) for direct in (1, 0) for s in range(lib.linear_probe_shapes(f32, direct)) if lib.linear_probe_has(f32, direct, s)]
+    return [(f32, direct, s) for f32 in (0, 1) for direct in (1, 0) for s in range(lib.linear_probe_shapes(f32, direct)) if lib.linear_probe_has(f32, direct, grouped, s)]
 
 
 def tile(lib, direct, shape):
@@ -92,7 +92,7 @@ def test_ranges_of_a_row(f32, direct, shape):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("f32,direct,shape", _instances())
+@pytest.mark.parametrize("f32,direct,shape", _instances(grouped=1))
 def test_groups(f32, direct, shape):
     """Groups of none, one, some, a tile's and more rows; rows of the tokens by their slots, and as they come."""
     lib = _lib()
@@ -117,7 +117,8 @@ def test_groups(f32, direct, shape):
 
 
 def test_the_probe_knows_every_kernel():
-    """(on the CPU) 21 tiles in bf16 and 3 large ones, 18 in fp32, as many as the listing has."""
+    """(on the CPU) in bf16 and fp32, for one matrix and for groups: as many as the listing has."""
     if not os.path.exists(B.LINEAR_PROBE):
         pytest.skip("not built")
-    assert len(_instances()) == 21 + 3 + 18
+    count = lambda f32, grouped: sum(i[0] == f32 for i in _instances(grouped))
+    assert [count(0, 0), count(0, 1), count(1, 0), count(1, 1)] == [21 + 3, 19 + 3, 13, 10]
