@@ -40,6 +40,8 @@ constexpr bool linear_has(int es, bool direct, bool grouped, int shape) {
 }
 // of linear_quad_kernel (bf16, rows in whole pieces)
 constexpr LinearShape kLinearQuad[] = {{256, 256, 128}, {192, 256, 128}, {256, 128, 128}};
+// (rows with which its tiles of groups are full, if the kernel decides so)
+constexpr int linear_least_rows(int m) { return m == 256 ? 192 : m; }
 constexpr int kLinearQuads = sizeof(kLinearQuad) / sizeof(LinearShape);
 
 tardis_status_t td_linear_init_quad();

@@ -212,7 +212,8 @@ tardis_status_t run(LinearArgs p, int32_t dtype, const Call& c, void* work, int6
     p.splits = plan.splits;
     p.slices = plan.slices;
     // (of groups: at most one tile that is not full in each, and no more than rows)
-    const int64_t tiles_m = grouped ? std::min(p.n, (p.n + (int64_t)p.experts * (t.m - 1)) / t.m) : p.tiles_m;
+    const int64_t full = quad ? linear_least_rows(t.m) : t.m;
+    const int64_t tiles_m = grouped ? std::min(p.n, (p.n + (int64_t)p.experts * (full - 1)) / full) : p.tiles_m;
     const int64_t tiles = tiles_m * p.tiles_n * plan.splits;
     if (tiles >= kMostTiles) return TARDIS_ERR_SHAPE;
     if (f32) TD_TRY(td_linear_init_f32());

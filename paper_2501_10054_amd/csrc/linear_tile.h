@@ -81,7 +81,9 @@ __device__ __forceinline__ int wave_scan(int v, int lane) {
 
 // Which group's tile this block has: the rows of a group are known on the device alone, so every wavefront adds up the groups' tiles
 // (a lane has a group) and looks for its own number.  Offsets outside of 0 .. n count as the nearest of the two.
-// EVEN: the tiles of a group have as many rows each, to the next 32.
+// EVEN: the tiles of a group have as many rows each, to the next 32; and tiles of 256 rows are full with 192 where that takes the whole launch
+// fewer rounds of the CUs (a round takes 7/8 of one with 256), which only the rows of the groups tell: 8 groups of 512 rows on average, 4096 ->
+// 8192, us: 3 rounds of 256 rows 320, of 192 rows 282; 8 of 1125, 2048 -> 7168: 5 rounds 305, 6 rounds of 192 rows 320.
 template <int TM, bool EVEN> __device__ __forceinline__ bool find_group(const LinearArgs& p, int lane, LinearBlock& b, int& tile_n) {
     const int positions = (int)p.n;
     auto group = [&](int e, int& from) {
@@ -89,13 +91,34 @@ template <int TM, bool EVEN> __device__ __forceinline__ bool find_group(const Li
         const int to = e < p.experts ? min(max(p.offsets[e + 1], 0), positions) : 0;
         return max(to - from, 0);
     };
+    constexpr int LESS = EVEN ? linear_least_rows(TM) : TM;
+    bool less = false;
+    auto tiles_of = [&](int rows) { return LESS < TM && less ? (rows + LESS - 1) / LESS : (rows + TM - 1) / TM; };
+    auto last = [](int v) { return (uint32_t)__builtin_amdgcn_readlane(v, 63); };
     int from0;
-    const int rows0 = group(lane, from0), sum0 = wave_scan((rows0 + TM - 1) / TM, lane);
-    uint32_t all = (uint32_t)__builtin_amdgcn_readlane(sum0, 63);
-    for (int c = 64; c < p.experts; c += 64) {
-        int from;
-        const int rows = group(c + lane, from);
-        all += (uint32_t)__builtin_amdgcn_readlane(wave_scan((rows + TM - 1) / TM, lane), 63);
+    const int rows0 = group(lane, from0);
+    auto count = [&](int& sum0) {
+        sum0 = wave_scan(tiles_of(rows0), lane);
+        uint32_t all = last(sum0);
+        for (int c = 64; c < p.experts; c += 64) {
+            int from;
+            const int rows = group(c + lane, from);
+            all += last(wave_scan(tiles_of(rows), lane));
+        }
+        return all;
+    };
+    int sum0;
+    uint32_t all = count(sum0);
+    if constexpr (LESS < TM) {
+        int sum_less;
+        less = true;
+        const uint32_t all_less = count(sum_less);
+        auto rounds = [&](uint32_t tiles) { return (tiles * (uint32_t)p.tiles_n + 255) / 256; };
+        less = rounds(all_less) * 7 < rounds(all) * 8;
+        if (less) {
+            all = all_less;
+            sum0 = sum_less;
+        }
     }
     uint32_t t;
     if (!number_of(blockIdx.x, all * (uint32_t)p.tiles_n, t)) return false;
@@ -104,23 +127,24 @@ template <int TM, bool EVEN> __device__ __forceinline__ bool find_group(const Li
         int from = from0, rows = rows0, sum = sum0;
         if (c > 0) {
             rows = group(c + lane, from);
-            sum = wave_scan((rows + TM - 1) / TM, lane);
+            sum = wave_scan(tiles_of(rows), lane);
         }
         const uint64_t past = __ballot((before + (uint32_t)sum) * (uint32_t)p.tiles_n > t);
         if (past) {
             const int at = __builtin_ctzll(past);
             from = __builtin_amdgcn_readlane(from, at);
             rows = __builtin_amdgcn_readlane(rows, at);
-            const int tiles = (rows + TM - 1) / TM;
+            const int tiles = tiles_of(rows);
             const uint32_t mine = before + (uint32_t)__builtin_amdgcn_readlane(sum, at) - (uint32_t)tiles;
             int tile_m;
             tile_of(t - mine * (uint32_t)p.tiles_n, (uint32_t)tiles, (uint32_t)p.tiles_n, tile_m, tile_n);
             b.expert = c + at;
-            int step = TM;
+            int step = LESS < TM && less ? LESS : TM;
             if constexpr (EVEN) {
                 uint32_t rest;
+                const int full = step;
                 step = uniform((int)divide((uint32_t)rows, (uint32_t)tiles, rest));   // (rows < 2^21 in one group: else the tiles are full)
-                step = rows < 1 << 21 ? min((step + (rest > 0) + 31) & ~31, TM) : TM;
+                step = rows < 1 << 21 ? min((step + (rest > 0) + 31) & ~31, full) : full;
             }
             b.first = from + (int64_t)tile_m * step;
             b.rows = max(0, min(step, rows - tile_m * step));

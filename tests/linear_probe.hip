@@ -42,7 +42,8 @@ int linear_probe(int f32, int direct, int shape, const void* x, int64_t x_rows, 
     p.experts = experts;
     p.per_token = per_token;
     p.inv_per_token = per_token > 1 ? (uint32_t)(0x100000000ull / (uint64_t)per_token) : 0xffffffffu;
-    const int64_t most = (rows + (int64_t)experts * (t[0] - 1)) / t[0];
+    const int64_t full = direct && shape >= kLinearShapes ? linear_least_rows(t[0]) : t[0];
+    const int64_t most = (rows + (int64_t)experts * (full - 1)) / full;
     const int64_t tiles = (experts ? (most < rows ? most : rows) : p.tiles_m) * p.tiles_n * ranges;
     const int blocks = (int)((tiles + 7) / 8 * 8);
     const hipStream_t s = static_cast<hipStream_t>(stream);
