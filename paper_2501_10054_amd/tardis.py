@@ -338,6 +338,11 @@ def _route_work_bytes(n, experts, k):
     return bytes_.value
 
 
+def _on(stream):
+    """The stream that a call is given, as the current one: outputs and working memory then are its own, and not given to other work while it runs."""
+    return torch.cuda.stream(stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream)) if int(stream) else torch.cuda.default_stream())
+
+
 def _empty(n, width, dtype, device):
     return torch.empty_strided((n, width), (width, 1), dtype=dtype, device=device)   # (half the host time of torch.empty)
 
@@ -352,6 +357,9 @@ def _rows(x, n_in):
 
 def tardis_linear(x, W, b=None, act: str = "identity", residual=None, out_dtype=None, y=None, stream=None):
     """-> n x n_out: act(x W^T + b) + residual.  Rows of x may have a pitch; out_dtype: of residual and y (default: x's)."""
+    if stream is not None:
+        with _on(stream):
+            return tardis_linear(x, W, b, act, residual, out_dtype, y)
     n_out, n_in = W.shape
     n, pitch = _rows(x, n_in)
     dt, dev = x.dtype, x.get_device()
@@ -367,13 +375,16 @@ def tardis_linear(x, W, b=None, act: str = "identity", residual=None, out_dtype=
     desc = tardis_linear_desc(*sizes, 0, W_at, None if b is None else b.data_ptr())
     bytes_ = _linear_work_bytes(sizes, 0, n, pitch, 0, n, x_at & 15, W_at & 15)
     work = torch.empty(bytes_, dtype=torch.uint8, device=x.device) if bytes_ else None
-    _check(lib().tardis_linear(desc, x_at, n, pitch, _ptr(residual), y.data_ptr(), _ptr(work), bytes_, _stream(stream)), "tardis_linear")
+    _check(lib().tardis_linear(desc, x_at, n, pitch, _ptr(residual), y.data_ptr(), _ptr(work), bytes_, _stream(None)), "tardis_linear")
     return y
 
 
 def tardis_grouped_linear(x, W, offsets, b=None, act: str = "identity", order=None, per_token: int = 1, out_dtype=None, y=None, stream=None):
     """-> positions x n_out: act(x[order[p] // per_token] W[e]^T + b[e]) at positions offsets[e] <= p < offsets[e + 1]; without
     an order x[p].  W: experts x n_out x n_in.  Rows of y in no group are not written."""
+    if stream is not None:
+        with _on(stream):
+            return tardis_grouped_linear(x, W, offsets, b, act, order, per_token, out_dtype, y)
     experts, n_out, n_in = W.shape
     x_rows, pitch = _rows(x, n_in)
     dt, dev = x.dtype, x.get_device()
@@ -392,12 +403,15 @@ def tardis_grouped_linear(x, W, offsets, b=None, act: str = "identity", order=No
     bytes_ = _linear_work_bytes(sizes, experts, x_rows, pitch, int(ordered), positions, x_at & 15, W_at & 15)
     work = torch.empty(bytes_, dtype=torch.uint8, device=x.device) if bytes_ else None
     _check(lib().tardis_grouped_linear(desc, experts, x_at, x_rows, pitch, offsets.data_ptr(), _ptr(order), per_token, positions, y.data_ptr(),
-                                       _ptr(work), bytes_, _stream(stream)), "tardis_grouped_linear")
+                                       _ptr(work), bytes_, _stream(None)), "tardis_grouped_linear")
     return y
 
 
 def tardis_moe_route(logits, k: int, renormalise: bool = True, stream=None):
     """logits n x experts -> (ids int32[n, k], weights float32[n, k], offsets int32[experts + 1], order int32[n k], place int32[n, k])."""
+    if stream is not None:
+        with _on(stream):
+            return tardis_moe_route(logits, k, renormalise)
     n, experts = logits.shape
     assert logits.is_cuda and logits.is_contiguous()
     dev = logits.device
@@ -407,12 +421,15 @@ def tardis_moe_route(logits, k: int, renormalise: bool = True, stream=None):
     bytes_ = _route_work_bytes(n, experts, k)
     work = torch.empty(bytes_, dtype=torch.uint8, device=dev) if bytes_ else None
     _check(lib().tardis_moe_route(logits.data_ptr(), n, experts, k, _DTYPE_CODE[logits.dtype], 1 if renormalise else 0, ids.data_ptr(), weights.data_ptr(),
-                                  offsets.data_ptr(), order.data_ptr(), place.data_ptr(), _ptr(work), bytes_, _stream(stream)), "tardis_moe_route")
+                                  offsets.data_ptr(), order.data_ptr(), place.data_ptr(), _ptr(work), bytes_, _stream(None)), "tardis_moe_route")
     return ids, weights, offsets, order, place
 
 
 def tardis_moe_combine(z, place, weights, residual=None, out_dtype=None, y=None, stream=None):
     """-> n x d: residual[t] + sum_j weights[t, j] z[place[t, j]]; a place below 0 is a dropped slot.  out_dtype: of residual and y (default: z's)."""
+    if stream is not None:
+        with _on(stream):
+            return tardis_moe_combine(z, place, weights, residual, out_dtype, y)
     (rows, d), (n, k), dev = z.shape, place.shape, z.get_device()
     out_dtype = out_dtype or z.dtype
     assert z.is_cuda and z.is_contiguous() and place.is_contiguous() and place.dtype == torch.int32 and place.get_device() == dev
@@ -423,5 +440,5 @@ def tardis_moe_combine(z, place, weights, residual=None, out_dtype=None, y=None,
     else:
         assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, d) and y.get_device() == dev
     _check(lib().tardis_moe_combine(z.data_ptr(), rows, place.data_ptr(), weights.data_ptr(), n, k, d, _DTYPE_CODE[z.dtype], _ptr(residual), y.data_ptr(),
-                                    _DTYPE_CODE[out_dtype], _stream(stream)), "tardis_moe_combine")
+                                    _DTYPE_CODE[out_dtype], _stream(None)), "tardis_moe_combine")
     return y

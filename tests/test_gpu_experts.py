@@ -162,6 +162,28 @@ def test_another_stream_and_a_graph():
         assert torch.equal(experts_layer(t, *weights, k)[0], want)
 
 
+def test_a_stream_that_is_given():
+    """Outputs and working memory belong to the stream of the call: while it waits there, other work of the current stream gets none of it."""
+    gen = torch.Generator(device=DEV).manual_seed(17)
+    x, W = torch.randn(8, 16384, device=DEV, generator=gen).bfloat16(), (torch.randn(256, 16384, device=DEV, generator=gen) * 0.01).bfloat16()
+    logits = torch.randn(4096, 64, device=DEV, generator=gen)
+    want, routed = T.tardis_linear(x, W), T.tardis_moe_route(logits, 4)
+    z = torch.randn(4096 * 4, 64, device=DEV, generator=gen)
+    summed = T.tardis_moe_combine(z, routed[4], routed[1])
+    side = torch.cuda.Stream()
+    for stream in (side, side.cuda_stream):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        y, r = T.tardis_linear(x, W, stream=stream), T.tardis_moe_route(logits, 4, stream=stream)
+        s = T.tardis_moe_combine(z, r[4], r[1], stream=stream)
+        others = [torch.full((size,), 255, dtype=torch.uint8, device=DEV) for size in [1 << b for b in range(9, 21)] * 4]
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(s, summed) and all(torch.equal(a, b) for a, b in zip(r, routed))
+        assert all((o == 255).all() for o in others)
+    assert torch.equal(T.tardis_linear(x, W, stream=0), want)
+
+
 def test_the_example_runs():
     """examples/expert_layer.py: two bf16 roundings on the way and one at the end, 2^-8 each at most in the norm."""
     import importlib.util
