@@ -187,12 +187,17 @@ template <bool GROUPED> __device__ __forceinline__ int64_t token_of_row(const Li
 // acc[i][j][q] = row (WM i + wm) 16 + lane % 16, column (wn FB + j) 16 + 4 (lane / 16) + q of the tile.  RB row blocks of a wavefront at a time
 // pass through LDS, where the parts of K meet (WK = 1: every wavefront's own), so that a store covers whole lines of a row and that what
 // is done to the elements is a loop; a thread finishes 8 neighbouring columns at once.
+// Loads and stores are counted by one counter, in their order: a load in the loop would wait for the stores of the turn before, 1.5 us each
+// (2048 x 16384 x 4096, behind the products of a 256 x 256 tile, us: residual or bias waited for in every turn 24, as here @EPI).  So which rows
+// are there is known before the first store, and residuals are loaded for several turns at once, in a loop of their own.
 template <typename T, bool GROUPED, int W, int FA, int FB, int WM, int WN, int WK, int RB>
 __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearBlock& b, f32x4_t (&acc)[FA][FB], unsigned char* lds, int tid) {
     static_assert(FA % RB == 0, "all row blocks");
     constexpr bool OWN = WK == 1;
     static constexpr int kAtOnce = OWN ? 2 : 1;                  // (one wavefront on a SIMD: two rows side by side; 2048 x 16384 x 4096 210 -> 195 us)
     constexpr int COLS = OWN ? FB * 16 : WN * FB * 16, ROWS = OWN ? RB * 16 : WM * RB * 16, UNITS = COLS / 8, STRIDE = (OWN ? 64 : W * 64) / UNITS;
+    static constexpr int TURNS = (ROWS + STRIDE - 1) / STRIDE, kLoads = OWN ? 8 : 2, AHEAD = TURNS % kLoads == 0 ? kLoads : TURNS % 2 == 0 ? 2 : 1;
+    static_assert(TURNS * (FA / RB) <= 32, "a bit for each row of a thread");
     const int lane = tid & 63, wave = uniform(tid >> 6), wk = wave % WK, wn = wave / WK % WN, wm = wave / WK / WN, frow = lane & 15, fp = lane >> 4;
     const int me = OWN ? lane : tid, unit = me % UNITS;
     float* stage = reinterpret_cast<float*>(lds) + (OWN ? wave * ROWS * COLS : 0);
@@ -203,33 +208,58 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
     };
     const int64_t n = b.n0 + (OWN ? wn * COLS : 0) + unit * 8;
     const int columns = (int)min((int64_t)8, p.N - n);    // (of this thread; none or less: none)
-    auto load8 = [&](const void* from, int64_t at, bool f32, float (&v)[8]) {
+    // (as 16 bytes of 8 bf16 or 32 of 8 fp32; columns that are not there: 0)
+    auto load8 = [&](const void* from, int64_t at, bool f32, td_u32x4 (&w)[2]) {
         if (columns >= 8) {
-            if (f32) {
-                const td_u32x4 lo = load_any16(static_cast<const float*>(from) + at), hi = load_any16(static_cast<const float*>(from) + at + 4);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v[q] = __uint_as_float(lo[q]);
-                    v[4 + q] = __uint_as_float(hi[q]);
-                }
-            } else {
-                const td_u32x4 w = load_any16(static_cast<const bf16_t*>(from) + at);
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v[2 * q] = __uint_as_float(w[q] << 16);
-                    v[2 * q + 1] = __uint_as_float(w[q] & 0xffff0000u);
-                }
-            }
+            w[0] = load_any16(static_cast<const unsigned char*>(from) + at * (f32 ? 4 : 2));
+            if (f32) w[1] = load_any16(static_cast<const float*>(from) + at + 4);
         } else {
+            w[0] = w[1] = td_u32x4{0, 0, 0, 0};
 #pragma unroll
             for (int q = 0; q < 8; ++q)
-                v[q] = q >= columns ? 0.0f : f32 ? static_cast<const float*>(from)[at + q] : td_bf16_to_f32(static_cast<const bf16_t*>(from)[at + q]);
+                if (q < columns) {
+                    const uint32_t e = f32 ? static_cast<const uint32_t*>(from)[at + q] : (uint32_t)static_cast<const bf16_t*>(from)[at + q] << (16 * (q & 1));
+                    const uint32_t as_f32 = f32 ? e : w[q / 4][q % 4], as_bf16 = f32 ? w[0][q / 2] : w[0][q / 2] | e;
+                    if (q / 4 != 0 || q % 4 != q / 2) {
+                        w[q / 4][q % 4] = as_f32;
+                        w[0][q / 2] = as_bf16;
+                    } else {
+                        w[0][q / 2] = f32 ? as_f32 : as_bf16;
+                    }
+                }
         }
     };
+    auto value = [](const td_u32x4 (&w)[2], bool f32, int q) {
+        const uint32_t as_f32 = w[q / 4][q % 4], pair = w[0][q / 2];
+        return __uint_as_float(f32 ? as_f32 : q & 1 ? pair & 0xffff0000u : pair << 16);
+    };
     float bias[8] = {};
-    if (p.b && !p.part && columns > 0) load8(p.b, (int64_t)b.expert * p.N + n, sizeof(T) == 4, bias);
+    if (p.b && !p.part && columns > 0) {
+        td_u32x4 w[2];
+        load8(p.b, (int64_t)b.expert * p.N + n, sizeof(T) == 4, w);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) bias[q] = value(w, sizeof(T) == 4, q);
+    }
+#pragma unroll
+    for (int q = 0; q < 8; ++q) asm volatile("" : "+v"(bias[q]));
+    // row of the tile that the thread has in turn t of the row blocks from i0 on
+    auto row_of = [&](int i0, int t, int& at) {
+        at = me / UNITS + t * STRIDE;
+        const int block = OWN ? wm + WM * (at / 16) : at / (RB * 16) + WM * (at / 16 % RB);
+        return (i0 * WM + block) * 16 + at % 16;
+    };
+    uint32_t there = 0;
+#pragma unroll
+    for (int t = 0; t < TURNS * (FA / RB); ++t) {
+        int at;
+        const int m = row_of(t / TURNS * RB, t % TURNS, at);
+        const bool in = at < ROWS && columns > 0 && (GROUPED ? token_of_row<GROUPED>(p, b, m) >= 0 : m < b.rows);
+        there |= in ? 1u << t : 0u;
+    }
+    asm volatile("" : "+v"(there));
+    const bool residual = p.r && !p.part;
     for_constants<FA / RB>([&](auto batch) {
-        constexpr int i0 = decltype(batch)::value * RB;
+        constexpr int i0 = decltype(batch)::value * RB, first = decltype(batch)::value * TURNS;
         if constexpr (i0 > 0) sync();
 #pragma unroll
         for (int i = 0; i < RB; ++i)
@@ -237,27 +267,19 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
             for (int j = 0; j < FB; ++j)
                 *reinterpret_cast<f32x4_t*>(stage + place_of(wk, ((OWN ? 0 : wm * RB) + i) * 16 + frow, ((OWN ? 0 : wn * FB) + j) * 4 + fp)) = acc[i0 + i][j];
         sync();
+        // (sums of a range of K: act is the identity, without bias and residual)
         with_linear_act(p.act, [&](auto act) {
-#pragma unroll kAtOnce
-            for (int at = me / UNITS; at < ROWS; at += STRIDE) {
-                const int block = OWN ? wm + WM * (at / 16) : at / (RB * 16) + WM * (at / 16 % RB), m = (i0 * WM + block) * 16 + at % 16;   // row of the tile
-                if (m >= b.rows || columns <= 0) continue;
-                if (GROUPED && p.order && token_of_row<GROUPED>(p, b, m) < 0) continue;
-                const int64_t row = b.first + m, to = row * p.N + n;
-                float r[8] = {}, v[8];
-                if (p.r && !p.part) load8(p.r, to, p.out_f32, r);
+            auto sum_and_act = [&](int at, float (&v)[8]) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     f32x4_t sum = *reinterpret_cast<const f32x4_t*>(stage + place_of(0, at, unit * 2 + h));
 #pragma unroll
                     for (int part = 1; part < WK; ++part) sum += *reinterpret_cast<const f32x4_t*>(stage + place_of(part, at, unit * 2 + h));
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) v[4 * h + q] = sum[q];
+                    for (int q = 0; q < 4; ++q) v[4 * h + q] = linear_act<decltype(act)::value>(sum[q] + bias[4 * h + q]);
                 }
-                if (!p.part) {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) v[q] = linear_act<decltype(act)::value>(v[q] + bias[q]) + r[q];
-                }
+            };
+            auto store = [&](int64_t to, const float (&v)[8]) {
                 if (p.part || p.out_f32) {
                     float* y = p.part ? p.part + (int64_t)b.range * p.n * p.N + to : static_cast<float*>(p.y) + to;
                     if (columns >= 8) {
@@ -277,6 +299,39 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
 #pragma unroll
                         for (int q = 0; q < 8; ++q)
                             if (q < columns) y[q] = (bf16_t)(o[q / 2] >> (16 * (q & 1)));
+                    }
+                }
+            };
+            if (!residual) {
+#pragma unroll kAtOnce
+                for (int t = 0; t < TURNS; ++t) {
+                    int at;
+                    const int m = row_of(i0, t, at);
+                    if (!(there >> (first + t) & 1)) continue;
+                    float v[8];
+                    sum_and_act(at, v);
+                    store((b.first + m) * p.N + n, v);
+                }
+            } else {
+#pragma unroll 1
+                for (int t0 = 0; t0 < TURNS; t0 += AHEAD) {
+                    td_u32x4 r[AHEAD][2];
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) {
+                        int at;
+                        const int m = row_of(i0, t0 + u, at);
+                        if (there >> (first + t0 + u) & 1) load8(p.r, (b.first + m) * p.N + n, p.out_f32, r[u]);
+                    }
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) {
+                        int at;
+                        const int m = row_of(i0, t0 + u, at);
+                        if (!(there >> (first + t0 + u) & 1)) continue;
+                        float v[8];
+                        sum_and_act(at, v);
+#pragma unroll
+                        for (int q = 0; q < 8; ++q) v[q] += value(r[u], p.out_f32, q);
+                        store((b.first + m) * p.N + n, v);
                     }
                 }
             }
