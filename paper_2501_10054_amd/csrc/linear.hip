@@ -76,18 +76,18 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, uint32_t
 // What a tile takes, in us:
 //     max(fixed x turns + slices x max(alone x turns, slice x tiles of a CU), 1.5 + bytes / tbs)
 // with `blocks` of them at once on a CU, in `turns` turns: alone is a slice's latency, slice its share of the CU.  Bytes: x, y (the ranges'
-// sums), W, and for every further row of tiles `again` of W.  The constants are those with which the choice is best: over 583 products and 154
-// grouped ones in bf16 (sizes from 64 x 64 to 16384 x 16384, 1 to 5000 rows, weights from HBM; every tile with 1, 2, 4 and 8 ranges) it takes 1.3 % more
+// sums), W, and for every further row of tiles `again` of W.  The constants are those with which the choice is best: over 581 products and 155
+// grouped ones in bf16 (sizes from 64 x 64 to 16384 x 16384, 1 to 5000 rows, weights from HBM; every tile with 1, 2, 4 and 8 ranges) it takes 1.5 and 3.1 % more
 // than the best measured, fp32 (185, 39) 0.8 %, staged (179, 28) 1.0 %, staged fp32 (98) 0.3 %.
 struct Rate { int blocks; float alone, slice, fixed, tbs; };
 // ({}: a tile that is not there, linear_has)
-constexpr Rate kRate[] = {{2, 0.229f, 0.220f, 3.96f, 5.53f}, {2, 0.418f, 0.403f, 3.77f, 5.55f}, {1, 0.544f, 0.544f, 3.98f, 5.27f},
-                          {2, 0.238f, 0.205f, 4.00f, 4.81f}, {1, 0.324f, 0.324f, 4.01f, 5.27f}, {1, 0.276f, 0.276f, 4.15f, 4.16f},
-                          {1, 0.405f, 0.405f, 4.84f, 5.01f}, {2, 0.275f, 0.265f, 3.82f, 5.46f}, {1, 0.373f, 0.373f, 4.85f, 3.97f},
-                          {1, 0.526f, 0.526f, 6.26f, 4.70f}, {1, 0.624f, 0.624f, 8.23f, 3.18f}, {1, 0.375f, 0.375f, 4.56f, 5.52f},
-                          {1, 0.401f, 0.401f, 4.31f, 4.24f}, {5, 0.613f, 0.262f, 3.08f, 4.53f}, {3, 0.770f, 0.368f, 4.10f, 4.62f},
-                          {2, 0.697f, 0.566f, 5.89f, 3.76f}, {1, 1.101f, 1.101f, 16.43f, 3.46f}, {1, 0.930f, 0.930f, 15.57f, 4.28f},
-                          {1, 0.803f, 0.803f, 8.51f, 4.37f}};
+constexpr Rate kRate[] = {{2, 0.244f, 0.223f, 3.80f, 5.50f}, {2, 0.415f, 0.400f, 3.74f, 5.51f}, {1, 0.493f, 0.493f, 4.47f, 5.09f},
+                          {2, 0.238f, 0.205f, 4.00f, 4.83f}, {1, 0.321f, 0.321f, 4.01f, 5.09f}, {1, 0.276f, 0.276f, 4.15f, 4.15f},
+                          {1, 0.417f, 0.417f, 4.98f, 5.46f}, {2, 0.247f, 0.234f, 4.53f, 5.33f}, {1, 0.376f, 0.376f, 5.14f, 4.27f},
+                          {1, 0.512f, 0.512f, 6.21f, 5.25f}, {1, 0.630f, 0.630f, 7.61f, 3.04f}, {1, 0.369f, 0.369f, 4.39f, 5.47f},
+                          {1, 0.399f, 0.399f, 4.31f, 4.24f}, {5, 0.489f, 0.262f, 3.07f, 3.94f}, {3, 0.790f, 0.367f, 3.75f, 4.55f},
+                          {2, 0.725f, 0.639f, 4.82f, 3.77f}, {1, 0.903f, 0.903f, 14.60f, 3.45f}, {1, 0.770f, 0.770f, 12.50f, 3.95f},
+                          {1, 0.788f, 0.788f, 7.70f, 3.77f}};
 constexpr Rate kRateF32[] = {{2, 0.266f, 0.238f, 4.14f, 5.61f}, {2, 0.436f, 0.344f, 4.19f, 6.18f}, {}, {2, 0.368f, 0.323f, 3.75f, 4.50f},
                              {}, {}, {}, {}, {}, {}, {1, 3.086f, 3.086f, 8.00f, 3.83f}, {1, 0.483f, 0.483f, 4.53f, 4.86f},
                              {}, {5, 0.689f, 0.540f, 3.88f, 3.38f}, {3, 1.149f, 1.040f, 5.81f, 2.57f}, {2, 2.066f, 2.073f, 7.14f, 5.23f}};
@@ -99,7 +99,7 @@ static_assert(sizeof(kRate) / sizeof(Rate) == kLinearShapes + kLinearQuads && si
               sizeof(kRateStaged) / sizeof(Rate) == kLinearStagedShapes && sizeof(kRateStagedF32) / sizeof(Rate) == kLinearStagedShapes, "a rate for each tile");
 // one more launch (2.5 on the GPU; callers that are not a graph wait for their host); a byte copied, of partial sums and outputs joined; sigma of an element of a tile, of eight wavefronts and of four
 constexpr double kLaunchUs = 4.0, kCopyUs = 1.0 / 4.5e6, kJoinUs = 1.0 / 5e6, kSigmaUs = 5.0 / 65536, kSigmaQuadUs = 8.0 / 65536;
-constexpr double kAgain = 0.38, kAgainF32 = 0.44, kAgainStaged = 0.20, kAgainStagedF32 = 0.43;
+constexpr double kAgain = 0.34, kAgainF32 = 0.44, kAgainStaged = 0.20, kAgainStagedF32 = 0.43;
 constexpr int64_t kMostTiles = 1 << 21;            // of a launch
 
 // What decides: sizes, types, alignment
