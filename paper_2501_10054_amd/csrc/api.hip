@@ -584,8 +584,8 @@ tardis_status_t tardis_linear_workspace(const tardis_linear_desc* desc, const vo
     TD_TRY(check_linear(desc));
     TD_TRY(check_linear_rows(desc, n, x_pitch));
     if (!bytes) return TARDIS_ERR_INVALID_ARG;
-    *bytes = n > 0 ? td_linear_work_bytes(desc, 0, x, n, x_pitch, false, n) : 0;
-    return TARDIS_OK;
+    *bytes = 0;
+    return n > 0 ? td_linear_work_bytes(desc, 0, x, n, x_pitch, false, n, bytes) : TARDIS_OK;
 }
 
 tardis_status_t tardis_linear(const tardis_linear_desc* desc, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y,
@@ -603,8 +603,8 @@ tardis_status_t tardis_grouped_linear_workspace(const tardis_linear_desc* desc, 
     TD_TRY(check_linear(desc));
     TD_TRY(check_grouped_rows(desc, experts, x_rows, x_pitch, ordered != 0, 1, positions));
     if (!bytes) return TARDIS_ERR_INVALID_ARG;
-    *bytes = x_rows > 0 && positions > 0 ? td_linear_work_bytes(desc, experts, x, x_rows, x_pitch, ordered != 0, positions) : 0;
-    return TARDIS_OK;
+    *bytes = 0;
+    return x_rows > 0 && positions > 0 ? td_linear_work_bytes(desc, experts, x, x_rows, x_pitch, ordered != 0, positions, bytes) : TARDIS_OK;
 }
 
 tardis_status_t tardis_grouped_linear(const tardis_linear_desc* desc, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch,

@@ -324,7 +324,8 @@ tardis_status_t td_stack_decode(tardis_layer_s* const* layers, int n_layers, con
 tardis_status_t td_forward(tardis_layer_s* L, const void* x, int64_t n, void* y, int norm_out, hipStream_t s);
 tardis_status_t td_dense_forward(tardis_layer_s* L, const void* x, int64_t n, void* y, hipStream_t s);
 // linear.hip (rows, x_rows >= 1; experts = 0: one matrix; work: aligned to 16 bytes)
-int64_t td_linear_work_bytes(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, bool gather, int64_t rows);
+tardis_status_t td_linear_work_bytes(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, bool gather, int64_t rows,
+                                     int64_t* bytes);
 tardis_status_t td_linear(const tardis_linear_desc* d, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y, void* work,
                           int64_t work_bytes, hipStream_t s);
 tardis_status_t td_grouped_linear(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, const int32_t* offsets,

@@ -121,7 +121,13 @@ const LinearShape& shape_of(bool direct, int s) { return !direct ? kLinearStaged
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
-// The least time over the ways that the call allows and that take no more than `room` bytes of working memory
+// Rows of tiles of a launch, at most (of groups: one tile that is not full in each, and no more tiles than rows)
+int64_t most_tiles_m(const Call& c, bool quad, const LinearShape& t) {
+    const int64_t full = c.experts && quad ? linear_least_rows(t.m) : t.m;
+    return c.experts ? std::min(c.M, (c.M + (int64_t)c.experts * (full - 1)) / full) : (c.M + t.m - 1) / t.m;
+}
+
+// The least time over the ways that the call allows and that take no more than `room` bytes of working memory (splits = 0: there is none)
 Plan make_plan(const Call& c, int64_t room) {
     Plan best{};
     best.us = 1e300;
@@ -154,7 +160,7 @@ Plan make_plan(const Call& c, int64_t room) {
             const Rate& r = p.direct ? (c.es == 2 ? kRate[s] : kRateF32[s]) : (c.es == 2 ? kRateStaged[s] : kRateStagedF32[s]);
             const int64_t slices = (p.k + t.slice - 1) / t.slice, tiles_n = (c.N + t.n - 1) / t.n;
             const double tiles_m = c.experts ? hit * std::max(1.0, (double)c.M / hit / t.m + 0.5) : (double)((c.M + t.m - 1) / t.m);
-            if (tiles_m * (double)tiles_n >= kMostTiles && s + 1 < shapes_of(p.direct, c.es)) continue;
+            if (most_tiles_m(c, p.direct && s >= kLinearShapes, t) * tiles_n >= kMostTiles) continue;
             for (int splits = 1; splits <= 16; splits *= 2) {
                 const double blocks = tiles_m * (double)tiles_n * splits;
                 if (splits > 1 && (c.experts || slices / splits < 4 || blocks > 1024 || p.at_part + splits * c.M * c.N * 4 > room)) break;
@@ -204,6 +210,7 @@ const Plan& plan_of(const Call& c, int64_t room) {
 // p: operands and sizes as the caller gave them; pitches and k in bytes
 tardis_status_t run(LinearArgs p, int32_t dtype, const Call& c, void* work, int64_t work_bytes, hipStream_t s) {
     const Plan& plan = plan_of(c, work_bytes);
+    if (plan.splits == 0) return TARDIS_ERR_SHAPE;
     const LinearShape& t = shape_of(plan.direct, plan.shape);
     const bool grouped = c.experts > 0, quad = plan.direct && plan.shape >= kLinearShapes, f32 = dtype == TARDIS_F32;
     p.tiles_m = (int)((p.n + t.m - 1) / t.m);
@@ -211,11 +218,7 @@ tardis_status_t run(LinearArgs p, int32_t dtype, const Call& c, void* work, int6
     p.tile_rows = (int)std::min<int64_t>(t.m, round_up((p.n + p.tiles_m - 1) / p.tiles_m, 32));
     p.splits = plan.splits;
     p.slices = plan.slices;
-    // (of groups: at most one tile that is not full in each, and no more than rows)
-    const int64_t full = quad ? linear_least_rows(t.m) : t.m;
-    const int64_t tiles_m = grouped ? std::min(p.n, (p.n + (int64_t)p.experts * (full - 1)) / full) : p.tiles_m;
-    const int64_t tiles = tiles_m * p.tiles_n * plan.splits;
-    if (tiles >= kMostTiles) return TARDIS_ERR_SHAPE;
+    const int64_t tiles = most_tiles_m(c, quad, t) * p.tiles_n * plan.splits;
     if (f32) TD_TRY(td_linear_init_f32());
     else TD_TRY(quad ? td_linear_init_quad() : td_linear_init_bf16());
     unsigned char* memory = static_cast<unsigned char*>(work);
@@ -274,8 +277,12 @@ constexpr int64_t kAnyRoom = (int64_t)1 << 62;
 
 }  // namespace
 
-int64_t td_linear_work_bytes(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, bool gather, int64_t rows) {
-    return make_plan(call_of(d, experts, x, x_rows, x_pitch, gather, rows), kAnyRoom).work;
+tardis_status_t td_linear_work_bytes(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, bool gather, int64_t rows,
+                                     int64_t* bytes) {
+    const Plan plan = make_plan(call_of(d, experts, x, x_rows, x_pitch, gather, rows), kAnyRoom);
+    if (plan.splits == 0) return TARDIS_ERR_SHAPE;
+    *bytes = plan.work;
+    return TARDIS_OK;
 }
 
 tardis_status_t td_linear(const tardis_linear_desc* d, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y, void* work,

@@ -1,0 +1,53 @@
+"""How large a call of linear layers and experts may be, on the CPU: the library's host code on a runtime without a GPU."""
+import ctypes as C
+import random
+
+import pytest
+
+from host_runtime import hip, host  # noqa: F401  (fixtures)
+from paper_2501_10054_amd import tardis as T
+from test_linear_choice import OFFSETS, ORDER, W, WORK, X, Y
+
+
+def grouped(host, dtype, tokens, n_in, n_out, experts, k):  # noqa: F811
+    """Status of the call and of the question for its working memory"""
+    desc, lib = T.tardis_linear_desc(n_in, n_out, dtype, T.BF16, T.ACT["relu"], 0, W, None), host.lib
+    lib.tardis_grouped_linear.argtypes = T.lib().tardis_grouped_linear.argtypes
+    lib.tardis_grouped_linear_workspace.argtypes = T.lib().tardis_grouped_linear_workspace.argtypes
+    asked = lib.tardis_grouped_linear_workspace(desc, experts, X, tokens, n_in, 1, tokens * k, C.c_int64())
+    return lib.tardis_grouped_linear(desc, experts, X, tokens, n_in, OFFSETS, ORDER, k, tokens * k, Y, WORK, 1 << 40, None), asked
+
+
+@pytest.mark.parametrize("dtype,tokens,n_in,n_out,experts", [(T.BF16, 65536, 8, 2048, 65536), (T.BF16, 4096, 8, 32768, 4096), (T.BF16, 16384, 8, 8192, 16384),
+                                                             (T.BF16, 1 << 20, 8, 16384, 4096), (T.F32, 65536, 8, 2048, 65536)])
+def test_groups_take_a_tile_that_a_launch_has_room_for(host, dtype, tokens, n_in, n_out, experts):  # noqa: F811
+    """Many experts with few tokens each: the tile that would be fastest needs more blocks than a launch has, larger ones do not."""
+    assert grouped(host, dtype, tokens, n_in, n_out, experts, 1) == (T.OK, T.OK)
+
+
+def test_what_no_tile_has_room_for_is_refused_alike(host):  # noqa: F811
+    """A launch has less than 2^21 tiles, of 256 columns and at least one for every expert with a token: the call and the question for
+    its working memory give the same answer."""
+    assert grouped(host, T.BF16, 65536, 8, 1 << 14, 65536, 1) == (T.ERR_SHAPE, T.ERR_SHAPE)
+    lib = host.lib
+    lib.tardis_linear_workspace.argtypes = T.lib().tardis_linear_workspace.argtypes
+    big = T.tardis_linear_desc(64, 1 << 22, T.BF16, T.BF16, 0, 0, W, None)
+    assert lib.tardis_linear_workspace(big, X, 1 << 30, 64, C.c_int64()) == T.ERR_SHAPE
+
+
+def test_no_call_that_a_tile_fits_is_refused(host):  # noqa: F811
+    rng = random.Random(5)
+    tried = 0
+    while tried < 3000:
+        experts, tokens, n_in, n_out = (int(2 ** rng.uniform(*r)) for r in ((0, 16), (0, 20), (0, 13), (4, 17)))
+        k, dtype = rng.randint(1, 4), rng.choice([T.BF16, T.F32])
+        columns = 256 if dtype == T.BF16 else 128            # of the widest tiles for rows of any length, their rows: 192 and 128 or less
+        tall = 192 if dtype == T.BF16 else 128
+        positions = tokens * k
+        tiles = min(positions, positions // tall + experts + 1) * -(-n_out // columns)
+        if dtype == T.BF16 and (n_in * 2) % 16 and n_in * n_out * experts > 1 << 33:
+            continue                                         # (rows that are copied first: not where the copy is larger than 16 GB)
+        if tiles >= 1 << 21 or experts * n_out * n_in > 6 << 33 or positions * n_out > 6 << 33:
+            continue
+        tried += 1
+        assert grouped(host, dtype, tokens, n_in, n_out, experts, k) == (T.OK, T.OK), (dtype, tokens, n_in, n_out, experts, k)
