@@ -338,7 +338,8 @@ typedef struct {
     const void* b;       /* n_out (experts x n_out), or NULL for zero */
 } tardis_linear_desc;
 
-/* y = sigma(x W^T + b) + residual, rounded once.
+/* y = sigma(x W^T + b) + residual, rounded once.  sigma is good to fp32, but for GELU
+ * (erf) with outputs in bf16 and no residual, where Phi(-|z|) is off by up to 2^-14 of itself.
  *   x         n rows of n_in values, x_pitch >= n_in values apart.
  *   residual  n x n_out, out_dtype, or NULL; may be y itself.
  *   y         n x n_out, out_dtype; must not overlap x, W or b.

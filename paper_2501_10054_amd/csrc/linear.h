@@ -20,7 +20,7 @@ struct LinearArgs {
     uint32_t inv_per_token;
 };
 
-constexpr int kActGelu16 = 4;                     // behind tardis_act_t's: GELU for outputs in bf16
+constexpr int kActGelu16 = 4;                     // behind tardis_act_t's: GELU for outputs in bf16 without a residual
 constexpr uint32_t kNowhere = 0xe0000000u;        // an offset past the end of any operand that is loaded by offsets
 
 // The tiles: rows, columns and bytes of K in a slice (64 or 128 for each of the wavefronts that divide it)

@@ -256,13 +256,13 @@ tardis_status_t run(LinearArgs p, int32_t dtype, const Call& c, void* work, int6
 
 const unsigned char* bytes_of(const void* p) { return static_cast<const unsigned char*>(p); }
 
-LinearArgs layer(const tardis_linear_desc* d) {
+LinearArgs layer(const tardis_linear_desc* d, bool residual) {
     LinearArgs p{};
     p.W = bytes_of(d->W);
     p.b = d->b;
     p.N = d->n_out;
     p.k = (uint32_t)(d->n_in * (int64_t)td_elem_size(d->dtype));
-    p.act = d->act == TARDIS_ACT_GELU_ERF && d->out_dtype == TARDIS_BF16 ? kActGelu16 : d->act;
+    p.act = d->act == TARDIS_ACT_GELU_ERF && d->out_dtype == TARDIS_BF16 && !residual ? kActGelu16 : d->act;
     p.out_f32 = d->out_dtype == TARDIS_F32;
     return p;
 }
@@ -287,7 +287,7 @@ tardis_status_t td_linear_work_bytes(const tardis_linear_desc* d, int64_t expert
 
 tardis_status_t td_linear(const tardis_linear_desc* d, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y, void* work,
                           int64_t work_bytes, hipStream_t s) {
-    LinearArgs p = layer(d);
+    LinearArgs p = layer(d, residual != nullptr);
     p.x = bytes_of(x);
     p.r = residual;
     p.y = y;
@@ -297,7 +297,7 @@ tardis_status_t td_linear(const tardis_linear_desc* d, const void* x, int64_t n,
 
 tardis_status_t td_grouped_linear(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, const int32_t* offsets,
                                   const int32_t* order, int64_t per_token, int64_t positions, void* y, void* work, int64_t work_bytes, hipStream_t s) {
-    LinearArgs p = layer(d);
+    LinearArgs p = layer(d, false);
     p.x = bytes_of(x);
     p.y = y;
     p.n = positions;

@@ -330,7 +330,7 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
                         if (there >> (first + t0 + u) & 1) store(to[u], v[u]);
                 }
             };
-            if constexpr (!GROUPED)
+            if constexpr (!GROUPED && decltype(act)::value != kActGelu16)   // (alone: linear_act.h)
                 if (residual) return turns(std::true_type{});
             turns(std::false_type{});
         });
