@@ -21,6 +21,8 @@ template <int ACT> __device__ __forceinline__ float linear_act(float z) {
         p = fmaf(p, t, -3.2766187f);
         const float q = t * __builtin_amdgcn_exp2f(fmaf(u * -0.721347520f, u, p));
         return z * (z > 0.0f ? 1.0f - q : q);
+    } else if constexpr (ACT == TARDIS_ACT_RELU) {
+        return z <= 0.0f ? 0.0f : z;                                // (a NaN stays one; act_flat has 0 for it)
     } else {
         return act_flat<ACT>(z);
     }
