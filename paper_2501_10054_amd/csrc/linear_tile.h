@@ -177,10 +177,11 @@ struct LinearTile {
 template <bool GROUPED> __device__ __forceinline__ int64_t token_of_row(const LinearArgs& p, const LinearBlock& b, int m) {
     if (m >= b.rows) return -1;
     if (!GROUPED || !p.order) return b.first + m;
-    const uint32_t slot = (uint32_t)p.order[b.first + m];
+    const int32_t at = p.order[b.first + m];
+    const uint32_t slot = (uint32_t)at;
     uint32_t token = __umulhi(slot, p.inv_per_token);       // the quotient, or one less
     if (slot - token * (uint32_t)p.per_token >= (uint32_t)p.per_token) ++token;
-    return (int64_t)token < p.x_rows ? (int64_t)token : -1; // (a negative slot is a large token)
+    return at >= 0 && (int64_t)token < p.x_rows ? (int64_t)token : -1;
 }
 
 // What follows the products of W wavefronts in a grid of WM x WN, times WK that divide K.

@@ -29,3 +29,25 @@ def test_many_experts_with_few_tokens(dtype, tokens, n_out, experts):
         off = (8 + 40) * 2.0 ** -23 * (4.0 * q + z.abs())
         check(y[p:p + step], z.clamp_min(0.0), off)
     assert math.isfinite(y.float().abs().max().item())
+
+
+@pytest.mark.parametrize("per_token", [1, 2, 64, (1 << 30) - 1, 1 << 30])
+@pytest.mark.parametrize("n_in,n_out,positions", [(64, 24, 20), (63, 24, 20), (256, 512, 1500)])
+def test_negative_slots_are_of_no_token(per_token, n_in, n_out, positions):
+    """Whatever the experts of a token: their rows are left as they are."""
+    gen = torch.Generator(device=DEV).manual_seed(per_token % 1000)
+    x = torch.randn(8, n_in, device=DEV, generator=gen).bfloat16()
+    W = torch.randn(2, n_out, n_in, device=DEV, generator=gen).mul_(0.1).bfloat16()
+    order = torch.randint(0, min(8 * per_token, (1 << 31) - 1), (positions,), device=DEV, generator=gen).int()
+    bad = torch.rand(positions, device=DEV, generator=gen) < 0.3
+    order[bad] = torch.tensor([-1, -2, -64, -(1 << 30), -(1 << 31)], device=DEV).int()[torch.arange(int(bad.sum()), device=DEV) % 5]
+    offsets = torch.tensor([0, positions // 3, positions], device=DEV).int()
+    y = torch.full((positions, n_out), 5.0, device=DEV)
+    T.tardis_grouped_linear(x, W, offsets, order=order, per_token=per_token, out_dtype=torch.float32, y=y)
+    assert (y[bad] == 5.0).all()
+    expert = (torch.arange(positions, device=DEV) >= positions // 3).long()
+    token = torch.div(order.long().clamp_min(0), per_token, rounding_mode="floor")
+    for e in range(2):
+        p = torch.nonzero(~bad & (expert == e)).flatten()
+        terms = torch.mm(W[e].double(), x[token[p]].double().t().contiguous()).t()
+        check(y[p], terms, (n_in / 32 + 40) * 2.0 ** -23 * (4.0 * torch.mm(W[e].double() ** 2, (x[token[p]].double() ** 2).t().contiguous()).t().sqrt() + terms.abs()))
