@@ -323,6 +323,8 @@ tardis_status_t td_stack_decode(tardis_layer_s* const* layers, int n_layers, con
 // norm_out != 0: the output is y / sqrt(mean(y^2) + kRmsEps) per token (glue between stacked layers)
 tardis_status_t td_forward(tardis_layer_s* L, const void* x, int64_t n, void* y, int norm_out, hipStream_t s);
 tardis_status_t td_dense_forward(tardis_layer_s* L, const void* x, int64_t n, void* y, hipStream_t s);
+// Threads of one launch, of which HIP allows less than 2^32: calls with more to do are several launches
+constexpr int64_t kMostThreads = (int64_t)1 << 31;
 // linear.hip (rows, x_rows >= 1; experts = 0: one matrix; work: aligned to 16 bytes)
 tardis_status_t td_linear_work_bytes(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, bool gather, int64_t rows,
                                      int64_t* bytes);

@@ -294,8 +294,8 @@ typedef uint32_t any16_t __attribute__((ext_vector_type(4), aligned(2)));
 
 template <typename T, bool ALIKE> __global__ void __launch_bounds__(256) combine_kernel(CombineArgs p) {
     constexpr int C = 16 / (int)sizeof(T);         // columns of a thread
-    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    int64_t t = u < (1ll << 32) ? (int64_t)((uint32_t)u / (uint32_t)p.units) : u / p.units;
+    const uint32_t u = blockIdx.x * 256u + threadIdx.x;
+    int64_t t = u / (uint32_t)p.units;
     if (t >= p.n) return;
     if constexpr (ALIKE) t = __builtin_amdgcn_readfirstlane((int)t);
     const int64_t c = (u - t * p.units) * C;
@@ -404,23 +404,24 @@ tardis_status_t td_moe_combine(const void* z, int64_t rows, const int32_t* place
                                const void* residual, void* y, int32_t out_dtype, hipStream_t s) {
     CombineArgs p{};
     p.z = static_cast<const unsigned char*>(z);
-    p.place = place;
-    p.weights = weights;
-    p.r = residual;
-    p.y = y;
-    p.n = n;
     p.rows = rows;
     p.d = d;
     p.k = rows > 0 ? (int)k : 0;
     p.out_f32 = out_dtype == TARDIS_F32;
-    const int64_t columns = dtype == TARDIS_F32 ? 4 : 8;
+    const int64_t columns = dtype == TARDIS_F32 ? 4 : 8, eo = (int64_t)td_elem_size(out_dtype);
     p.units = (d + columns - 1) / columns;
-    const int64_t blocks = (p.units * n + 255) / 256;
-    if (blocks > 0x7fffffff) return TARDIS_ERR_SHAPE;
     const bool alike = p.units % 64 == 0;
-    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, s, p); };
-    if (dtype == TARDIS_F32) launch(alike ? combine_kernel<float, true> : combine_kernel<float, false>);
-    else launch(alike ? combine_kernel<bf16_t, true> : combine_kernel<bf16_t, false>);
+    const int64_t most = kMostThreads / p.units;                   // tokens of a launch
+    for (int64_t t = 0; t < n; t += most) {
+        p.n = std::min(most, n - t);
+        p.place = place + t * k;
+        p.weights = weights + t * k;
+        p.r = residual ? static_cast<const unsigned char*>(residual) + t * d * eo : nullptr;
+        p.y = static_cast<unsigned char*>(y) + t * d * eo;
+        auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)((p.units * p.n + 255) / 256)), dim3(256), 0, s, p); };
+        if (dtype == TARDIS_F32) launch(alike ? combine_kernel<float, true> : combine_kernel<float, false>);
+        else launch(alike ? combine_kernel<bf16_t, true> : combine_kernel<bf16_t, false>);
+    }
     TD_HIP(hipGetLastError());
     return TARDIS_OK;
 }

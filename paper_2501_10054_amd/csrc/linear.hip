@@ -11,13 +11,13 @@ namespace {
 bool is_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 typedef uint32_t any16_t __attribute__((ext_vector_type(4), aligned(2)));
 
-// Rows of k bytes, `pitch` apart and at any address, to rows of `units` 16-byte pieces, zeros behind the last element.
+// Rows of k bytes, `pitch` apart and at any address, to rows of `units` 16-byte pieces, zeros behind the last element.  (Fewer than 2^32 pieces)
 template <typename T>
-__global__ void __launch_bounds__(256) linear_pack_kernel(const unsigned char* from, int64_t pitch, uint32_t k, td_u32x4* to, int64_t rows, uint32_t units) {
-    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / units;
+__global__ void __launch_bounds__(256) linear_pack_kernel(const unsigned char* from, int64_t pitch, uint32_t k, td_u32x4* to, uint32_t rows, uint32_t units) {
+    const uint32_t u = blockIdx.x * 256u + threadIdx.x, row = u / units;
     if (row >= rows) return;
-    const uint32_t at = (uint32_t)(u - row * units) * 16u;
-    const unsigned char* p = from + row * pitch + at;
+    const uint32_t at = (u - row * units) * 16u;
+    const unsigned char* p = from + (int64_t)row * pitch + at;
     td_u32x4 v = {0, 0, 0, 0};
     if (at + 16 <= k) {
         v = *reinterpret_cast<const any16_t*>(p);
@@ -224,9 +224,15 @@ tardis_status_t run(LinearArgs p, int32_t dtype, const Call& c, void* work, int6
     unsigned char* memory = static_cast<unsigned char*>(work);
     auto pack = [&](const unsigned char* from, int64_t pitch, int64_t rows, unsigned char* to) {
         const uint32_t units = (uint32_t)(plan.k / 16);
-        const dim3 grid((unsigned)((rows * units + 255) / 256));
-        if (f32) hipLaunchKernelGGL(linear_pack_kernel<float>, grid, dim3(256), 0, s, from, pitch, (uint32_t)c.k, reinterpret_cast<td_u32x4*>(to), rows, units);
-        else hipLaunchKernelGGL(linear_pack_kernel<bf16_t>, grid, dim3(256), 0, s, from, pitch, (uint32_t)c.k, reinterpret_cast<td_u32x4*>(to), rows, units);
+        const int64_t most = kMostThreads / units;                 // rows of a launch
+        for (int64_t row = 0; row < rows; row += most) {
+            const uint32_t here = (uint32_t)std::min(most, rows - row);
+            const unsigned char* first = from + row * pitch;
+            td_u32x4* at = reinterpret_cast<td_u32x4*>(to) + row * units;
+            const dim3 grid((here * units + 255) / 256);
+            if (f32) hipLaunchKernelGGL(linear_pack_kernel<float>, grid, dim3(256), 0, s, first, pitch, (uint32_t)c.k, at, here, units);
+            else hipLaunchKernelGGL(linear_pack_kernel<bf16_t>, grid, dim3(256), 0, s, first, pitch, (uint32_t)c.k, at, here, units);
+        }
         return to;
     };
     if (plan.pack_x) p.x = pack(p.x, c.pitch, c.x_rows, memory);

@@ -14,6 +14,9 @@ struct State {
     bool capturing = false, broken = false;                // a stream is being captured; a call has spoilt that
     int device = 0;
     std::string events, launches;
+    dim3 grid, block;                                      // of the launch that is being made
+    hipError_t last = hipSuccess;                          // (of launches alone)
+    int refused = 0;                                       // launches of 2^32 threads or more
     std::map<const void*, std::string> kernels;
 } g;
 hipError_t note(const char* what) {
@@ -34,6 +37,11 @@ void fake_reset(size_t limit) {
 void fake_capture(int on) { g.capturing = on != 0; }
 int fake_broken() { return g.broken; }
 void fake_device(int device) { g.device = device; }
+int fake_refused() {                                  // since the last call
+    const int n = g.refused;
+    g.refused = 0;
+    return n;
+}
 size_t fake_used() { return g.used; }
 const char* fake_launches() {                         // names of the kernels since the last call
     static std::string out;
@@ -87,8 +95,12 @@ hipError_t hipMemsetAsync(void* p, int, size_t n, hipStream_t) {
     return note("set");
 }
 hipError_t hipMemcpyAsync(void*, const void*, size_t, hipMemcpyKind, hipStream_t) { return note("copy"); }
-hipError_t hipLaunchKernel(const void* kernel, dim3, dim3, void**, size_t, hipStream_t) {
+hipError_t hipLaunchKernel(const void* kernel, dim3 grid, dim3 block, void**, size_t, hipStream_t) {
     std::lock_guard<std::recursive_mutex> guard(lock);
+    if ((uint64_t)grid.x * block.x >= (1ull << 32)) {
+        ++g.refused;
+        return g.last = hipErrorInvalidConfiguration;
+    }
     g.launches += g.kernels[kernel] + ' ';
     return note("launch");
 }
@@ -106,7 +118,11 @@ hipError_t hipSetDevice(int device) {
     g.device = device;
     return hipSuccess;
 }
-hipError_t hipGetLastError() { return hipSuccess; }
+hipError_t hipGetLastError() {
+    const hipError_t e = g.last;
+    g.last = hipSuccess;
+    return e;
+}
 hipError_t hipDeviceGetAttribute(int* v, hipDeviceAttribute_t, int) {
     *v = 256;
     return hipSuccess;
@@ -120,9 +136,14 @@ hipError_t hipOccupancyMaxActiveBlocksPerMultiprocessor(int* n, const void*, int
     *n = 1;
     return hipSuccess;
 }
-hipError_t __hipPushCallConfiguration(dim3, dim3, size_t, hipStream_t) { return hipSuccess; }
+hipError_t __hipPushCallConfiguration(dim3 grid, dim3 block, size_t, hipStream_t) {
+    g.grid = grid;
+    g.block = block;
+    return hipSuccess;
+}
 hipError_t __hipPopCallConfiguration(dim3* grid, dim3* block, size_t* lds, hipStream_t* s) {
-    *grid = *block = dim3(1);
+    *grid = g.grid;
+    *block = g.block;
     *lds = 0;
     *s = nullptr;
     return hipSuccess;

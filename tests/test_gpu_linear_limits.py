@@ -51,3 +51,42 @@ def test_negative_slots_are_of_no_token(per_token, n_in, n_out, positions):
         p = torch.nonzero(~bad & (expert == e)).flatten()
         terms = torch.mm(W[e].double(), x[token[p]].double().t().contiguous()).t()
         check(y[p], terms, (n_in / 32 + 40) * 2.0 ** -23 * (4.0 * torch.mm(W[e].double() ** 2, (x[token[p]].double() ** 2).t().contiguous()).t().sqrt() + terms.abs()))
+
+
+def test_a_sum_of_experts_of_more_than_2_to_the_32_threads():
+    """One slot with weight 1 for a token: its row of z as it is."""
+    torch.cuda.empty_cache()
+    n, d = (1 << 21) + 3, 16384
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    z = torch.randn(7, d, device=DEV, generator=gen).bfloat16()
+    place = torch.randint(-1, 7, (n, 1), device=DEV, generator=gen).int()
+    y = T.tardis_moe_combine(z, place, torch.ones(n, 1, device=DEV))
+    z8 = torch.cat([z, torch.zeros(1, d, device=DEV).bfloat16()])       # (a place of -1: the last)
+    for t in range(0, n, 1 << 16):
+        assert torch.equal(y[t:t + (1 << 16)], z8[place[t:t + (1 << 16), 0].long()])
+    del y
+    torch.cuda.empty_cache()
+
+
+def test_copies_of_more_than_2_to_the_32_pieces():
+    """Rows of an odd length, 64 GB of them: their aligned copy has every row in its place."""
+    torch.cuda.empty_cache()
+    n, n_in, n_out = 4194309, 8191, 2048
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    some = torch.randn(999, n_in, device=DEV, generator=gen).bfloat16()
+    W = (torch.randn(n_out, n_in, device=DEV, generator=gen) * 0.02).bfloat16()
+    x = torch.empty(n, n_in, dtype=torch.bfloat16, device=DEV)
+    for m in range(0, n, 999):
+        x[m:m + 999] = some[:min(999, n - m)]
+    y = T.tardis_linear(x, W)
+    terms = torch.mm(some.double(), W.double().t().contiguous())
+    q = torch.mm(some.double() ** 2, (W.double() ** 2).t().contiguous()).sqrt()
+    off = (n_in / 32 + 40) * 2.0 ** -23 * (4.0 * q + terms.abs())
+    for m in (0, 999 * 1024, 999 * 2099, 999 * 2100, 999 * 4197, n // 999 * 999):
+        rows = min(999, n - m)
+        check(y[m:m + rows], terms[:rows], off[:rows])
+    first = y[:999 * 1024].view(1024, 999, n_out)
+    for m in range(0, n - 999 * 1024, 999 * 1024):   # (the order of a sum goes by the tile: results below 16 may be rounded to neighbours, 2^-4 apart)
+        assert (y[m:m + 999 * 1024].view_as(first).float() - first.float()).abs().max().item() < 0.1
+    del x, y, first
+    torch.cuda.empty_cache()

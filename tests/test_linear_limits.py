@@ -6,7 +6,7 @@ import pytest
 
 from host_runtime import hip, host  # noqa: F401  (fixtures)
 from paper_2501_10054_amd import tardis as T
-from test_linear_choice import OFFSETS, ORDER, W, WORK, X, Y
+from test_linear_choice import OFFSETS, ORDER, W, WORK, X, Y, launched
 
 
 def grouped(host, dtype, tokens, n_in, n_out, experts, k):  # noqa: F811
@@ -51,3 +51,18 @@ def test_no_call_that_a_tile_fits_is_refused(host):  # noqa: F811
             continue
         tried += 1
         assert grouped(host, dtype, tokens, n_in, n_out, experts, k) == (T.OK, T.OK), (dtype, tokens, n_in, n_out, experts, k)
+
+
+def test_no_launch_has_2_to_the_32_threads(hip):  # noqa: F811
+    """Rows of an odd length that are copied first, and sums of experts, over more than 2^32 pieces of 16 bytes (64 GB: a card has 288)."""
+    assert launched(hip, T.BF16, 4194309, 8191, 2048, 0, 0, 1) == ["linear_pack_kernel"] * 4 + ["linear_quad_kernel 0 8 8"]
+    assert launched(hip, T.BF16, 4000000, 8191, 2048, 0, 0, 1) == ["linear_pack_kernel"] * 3 + ["linear_quad_kernel 0 8 8"]
+    assert launched(hip, T.BF16, 2048, 4001, 8192, 0, 0, 1)[:2] == ["linear_pack_kernel"] * 2
+    lib = hip.lib
+    lib.tardis_moe_combine.argtypes = T.lib().tardis_moe_combine.argtypes
+    for n, d, dtype, out, launches in ((1 << 21, 16384, T.BF16, T.BF16, 2), ((1 << 21) + 1, 16384, T.BF16, T.F32, 3), (1 << 20, 16384, T.F32, T.BF16, 2),
+                                       ((1 << 20) - 1, 16384, T.BF16, T.BF16, 1), (8192, 4096, T.BF16, T.BF16, 1), (5000, 1 << 22, T.F32, T.F32, 3)):
+        hip.launches()
+        assert lib.tardis_moe_combine(X, 100, ORDER, OFFSETS, n, 4, d, dtype, None, Y, out, None) == T.OK
+        assert len(hip.launches()) == launches
+    assert lib.fake_refused() == 0
