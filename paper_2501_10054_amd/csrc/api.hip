@@ -569,7 +569,7 @@ bool rows_fit(int64_t rows, int64_t pitch) { return rows >= 0 && rows <= kMaxRow
 namespace {
 
 tardis_status_t check_linear_rows(const tardis_linear_desc* d, int64_t rows, int64_t pitch) {
-    return rows_fit(rows, pitch) && pitch >= d->n_in ? TARDIS_OK : TARDIS_ERR_SHAPE;
+    return rows_fit(rows, rows > 1 ? pitch : 0) && pitch >= d->n_in ? TARDIS_OK : TARDIS_ERR_SHAPE;
 }
 tardis_status_t check_grouped_rows(const tardis_linear_desc* d, int64_t experts, int64_t x_rows, int64_t pitch, bool order, int64_t per_token, int64_t positions) {
     TD_TRY(check_linear_rows(d, x_rows, pitch));

@@ -143,7 +143,7 @@ Plan make_plan(const Call& c, int64_t room) {
         double before = 0.0;
         if (p.direct) {
             p.pack_W = !(k_whole && c.W_aligned);
-            p.pack_x = !(k_whole && c.x_aligned && (c.pitch % 16 == 0 || c.x_rows == 1));
+            p.pack_x = !(k_whole && c.x_aligned && c.pitch % 16 == 0);
             p.k = round_up(c.k, 16);
             if (p.pack_x) p.pitch = p.k;
             const int64_t bytes_x = p.pack_x ? round_up(c.x_rows * p.k, 256) : 0, bytes_W = p.pack_W ? round_up(W_rows * p.k, 256) : 0;
@@ -275,6 +275,7 @@ LinearArgs layer(const tardis_linear_desc* d, bool residual) {
 
 Call call_of(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, bool gather, int64_t rows) {
     const int64_t es = (int64_t)td_elem_size(d->dtype);
+    if (x_rows == 1) x_pitch = d->n_in;            // (of one row there is none, and none that is too long)
     return {rows, d->n_out, x_rows, d->n_in * es, x_pitch * es, (int)es, (int)td_elem_size(d->out_dtype), d->act, (int)experts, gather,
             is_aligned16(x), is_aligned16(d->W)};
 }

@@ -352,7 +352,7 @@ def _rows(x, n_in):
     assert x.is_cuda and x.dim() == 2 and x.shape[1] == n_in
     n, (pitch, step) = x.shape[0], x.stride()
     assert (step == 1 or n_in == 1) and (pitch >= n_in or n <= 1)
-    return n, max(pitch, n_in)
+    return n, pitch if n > 1 else n_in
 
 
 def tardis_linear(x, W, b=None, act: str = "identity", residual=None, out_dtype=None, y=None, stream=None):

@@ -90,3 +90,15 @@ def test_copies_of_more_than_2_to_the_32_pieces():
         assert (y[m:m + 999 * 1024].view_as(first).float() - first.float()).abs().max().item() < 0.1
     del x, y, first
     torch.cuda.empty_cache()
+
+
+def test_the_last_token_of_a_prompt():
+    """One row of a tensor whose rows are a prompt apart, and as it is by itself: the same call."""
+    gen = torch.Generator(device=DEV).manual_seed(10)
+    W = (torch.randn(512, 4096, device=DEV, generator=gen) * 0.02).bfloat16()
+    prompt = torch.randn(1, 1500, 4096, device=DEV, generator=gen).bfloat16()
+    last = prompt[:, -1]
+    assert last.stride(0) * 2 > 1 << 23
+    assert torch.equal(T.tardis_linear(last, W), T.tardis_linear(last.reshape(-1).clone()[None], W))
+    far = torch.as_strided(prompt, (1, 4096), ((1 << 30) + 1, 1))
+    assert torch.equal(T.tardis_linear(far, W), T.tardis_linear(prompt[:, 0].clone(), W))

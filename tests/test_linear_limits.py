@@ -66,3 +66,18 @@ def test_no_launch_has_2_to_the_32_threads(hip):  # noqa: F811
         assert lib.tardis_moe_combine(X, 100, ORDER, OFFSETS, n, 4, d, dtype, None, Y, out, None) == T.OK
         assert len(hip.launches()) == launches
     assert lib.fake_refused() == 0
+
+
+@pytest.mark.parametrize("gap", [1 << 22, 1 << 30, (1 << 40) + 3])
+def test_one_row_has_no_distance_to_the_next(hip, gap):  # noqa: F811
+    """The last token of a long prompt is a row of a tensor whose rows are a prompt apart: the distance says nothing, nor refuses or slows the call."""
+    for experts in (0, 4):
+        for n_in in (4096, 4097):
+            assert launched(hip, T.BF16, 1, n_in, 4096, gap, experts, 2) == launched(hip, T.BF16, 1, n_in, 4096, 0, experts, 2)
+    lib = hip.lib
+    lib.tardis_linear_workspace.argtypes = T.lib().tardis_linear_workspace.argtypes
+    need = []
+    for pitch in (8191, 8191 + gap):
+        need.append(C.c_int64())
+        assert lib.tardis_linear_workspace(T.tardis_linear_desc(8191, 64, T.BF16, T.BF16, 0, 0, W, None), X, 1, pitch, need[-1]) == T.OK
+    assert need[0].value == need[1].value
