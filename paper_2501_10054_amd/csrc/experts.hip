@@ -27,7 +27,7 @@ struct RouteArgs {
     int32_t* counts;                               // [block][counts_of_row(experts)]
 };
 
-// (rows of whole, aligned pieces of 16 bytes)
+// (rows of whole pieces of 16 bytes)
 __host__ __device__ __forceinline__ int counts_of_row(int experts) { return (experts + 3) & ~3; }
 
 template <int CTRL> __device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(v, v, CTRL, 0xf, 0xf, false); }
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_place_kernel(RouteArgs p)
     // four neighbouring experts for a thread, of every `parts`-th block
     const int pieces = counts_of_row(p.experts) / 4, parts = kRouteThreads / pieces, part = tid / pieces, piece = tid % pieces;
     if (part < parts) {
-        typedef int i32x4 __attribute__((ext_vector_type(4)));
+        typedef int i32x4 __attribute__((ext_vector_type(4), aligned(4)));   // (working memory begins at any word)
         const i32x4* rows = reinterpret_cast<const i32x4*>(p.counts) + piece;
         i32x4 a = {0, 0, 0, 0}, b = {0, 0, 0, 0};
 #pragma unroll 8
