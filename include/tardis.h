@@ -324,9 +324,12 @@ tardis_status_t tardis_dense_forward(tardis_handle_t L, const void* x, int64_t n
  * residual stream.  None of these calls needs a handle, allocates or
  * synchronises; what the device alone knows (how many rows an expert has) stays on
  * the device.  Pointers need the alignment of their elements only (rows of x and W that
- * are whole, aligned pieces of 16 bytes are the fast case).  Sums are fp32, in
- * an order that depends on the sizes alone: results are the same bits in every
- * run.  A call with no rows is TARDIS_OK and does nothing. */
+ * are whole, aligned pieces of 16 bytes are the fast case).  Sums are fp32, in an order
+ * that the call decides: its sizes, types and pitch, the working memory that it is given,
+ * the alignment of x and W, and of a grouped product its offsets.  Where these are equal
+ * results are the same bits, in every run; a token's result need not be the same bits
+ * next to other tokens, or where other tokens have chosen other experts.
+ * A call with no rows is TARDIS_OK and does nothing. */
 typedef struct {
     int64_t n_in;        /* 1 .. 2^22 */
     int64_t n_out;       /* 1 .. 2^22 */
