@@ -329,7 +329,9 @@ tardis_status_t tardis_dense_forward(tardis_handle_t L, const void* x, int64_t n
  * the alignment of x and W, and of a grouped product its offsets.  Where these are equal
  * results are the same bits, in every run; a token's result need not be the same bits
  * next to other tokens, or where other tokens have chosen other experts.
- * A call with no rows is TARDIS_OK and does nothing. */
+ * A call with no rows is TARDIS_OK and does nothing; one that would need 2^21 tiles
+ * or more is TARDIS_ERR_SHAPE (a tile has up to 256 x 256 results, in fp32 192 x 128, and
+ * those of an expert none of another). */
 typedef struct {
     int64_t n_in;        /* 1 .. 2^22 */
     int64_t n_out;       /* 1 .. 2^22 */

@@ -13,7 +13,7 @@ namespace {
 // in a fixed order, so the result is the same in every run.
 //
 // What bounds it: round trips and, for many tokens, the vector instructions of the choice (16384 tokens, 128 experts, 8 chosen, the choice in 64 blocks
-// 25.6 us, in 256 8.8, the placement 6.7).  One block does all of a call of few tokens (tokens_of_block); more take two launches, the choice with
+// 25.6 us, in 256 8.3, the placement 6.0).  One block does all of a call of few tokens (tokens_of_block); more take two launches, the choice with
 // the counts of every block, then the placement, for which every block adds up the counts of those before it (at most kMostBlocks), which
 // costs less than a launch of its own for that.
 constexpr int kRouteThreads = 1024, kMostBlocks = 256, kRouteWaves = kRouteThreads / 64;

@@ -188,8 +188,8 @@ Plan make_plan(const Call& c, int64_t room) {
     return best;
 }
 
-// make_plan's answer depends on sizes, alignment and working memory alone, of which a program has few: the last plans of a thread, by a hash (1.2 us of the 8 that a small
-// call takes of its host)
+// make_plan's answer depends on sizes, alignment and working memory alone, of which a program has few: the last plans of a thread, by a hash
+// (1.2 us of the 8 that a small call takes of its host)
 const Plan& plan_of(const Call& c, int64_t room) {
     struct Kept {
         Call call;

@@ -2,7 +2,8 @@
 
 Argument marshalling only: every step of the method runs in the library's HIP
 kernels.  Tensors are torch CUDA tensors used as plain device buffers; the
-current torch stream is passed unless one is given.  The library must have been
+current torch stream is passed unless one is given.  Inference only: results carry no
+gradient, also where operands ask for one.  The library must have been
 built (``python -m paper_2501_10054_amd.build``); there is no fallback path.
 """
 from __future__ import annotations
