@@ -329,6 +329,7 @@ tardis_status_t tardis_dense_forward(tardis_handle_t L, const void* x, int64_t n
  * the alignment of x and W, and of a grouped product its offsets.  Where these are equal
  * results are the same bits, in every run; a token's result need not be the same bits
  * next to other tokens, or where other tokens have chosen other experts.
+ * Rows (n, x_rows, positions, rows) and the distance between them are 2^30 at most.
  * A call with no rows is TARDIS_OK and does nothing; one that would need 2^21 tiles
  * or more is TARDIS_ERR_SHAPE (a tile has up to 256 x 256 results, in fp32 192 x 128, and
  * those of an expert none of another). */
@@ -383,7 +384,8 @@ tardis_status_t tardis_grouped_linear_workspace(const tardis_linear_desc* desc, 
  * among equal ones; weights are the softmax over the chosen ones (renormalise = 1) or over all
  * experts of the token (0).  A logit of minus infinity, or a NaN, is an expert that is not there:
  * a token with fewer than k others has ids of -1 and weights of 0 behind them.
- *   logits   n x experts, TARDIS_F32 or TARDIS_BF16.   1 <= experts <= 1024, 1 <= k <= 16, k <= experts.
+ *   logits   n x experts, TARDIS_F32 or TARDIS_BF16.   1 <= experts <= 1024, 1 <= k <= 16, k <= experts,
+ *            n k <= 2^30.
  *   ids      n x k ints, from the largest logit down.   weights  n x k floats.
  *   offsets  experts + 1 ints: the chosen slots (token k + place) sorted by expert, stable;
  *            expert e has positions offsets[e] .. offsets[e+1].

@@ -562,6 +562,9 @@ tardis_status_t check_linear(const tardis_linear_desc* d) {
     const size_t es = td_elem_size(d->dtype);
     return aligned_to(d->W, es) && aligned_to(d->b, es) ? TARDIS_OK : TARDIS_ERR_INVALID_ARG;
 }
+bool choice_fits(int64_t n, int64_t experts, int64_t k) {
+    return experts >= 1 && experts <= kMaxExperts && k >= 1 && k <= kMaxChosen && k <= experts && n >= 0 && n <= kMaxRows / k;
+}
 bool rows_fit(int64_t rows, int64_t pitch) { return rows >= 0 && rows <= kMaxRows && pitch <= kMaxPitch; }
 
 }  // namespace
@@ -623,7 +626,7 @@ tardis_status_t tardis_grouped_linear(const tardis_linear_desc* desc, int64_t ex
 
 tardis_status_t tardis_moe_route_workspace(int64_t n, int64_t experts, int64_t k, int64_t* bytes) {
     if (!bytes) return TARDIS_ERR_INVALID_ARG;
-    if (!rows_fit(n, 0) || experts < 1 || experts > kMaxExperts || k < 1 || k > kMaxChosen || k > experts) return TARDIS_ERR_SHAPE;
+    if (!choice_fits(n, experts, k)) return TARDIS_ERR_SHAPE;
     *bytes = n > 0 ? (int64_t)td_route_work_bytes(n, experts, k) : 0;
     return TARDIS_OK;
 }
@@ -631,7 +634,7 @@ tardis_status_t tardis_moe_route_workspace(int64_t n, int64_t experts, int64_t k
 tardis_status_t tardis_moe_route(const void* logits, int64_t n, int64_t experts, int64_t k, int32_t dtype, int32_t renormalise, int32_t* ids,
                                  float* weights, int32_t* offsets, int32_t* order, int32_t* place, void* work, int64_t work_bytes, void* stream) {
     if (!linear_dtype(dtype)) return TARDIS_ERR_DTYPE;
-    if (experts < 1 || experts > kMaxExperts || k < 1 || k > kMaxChosen || k > experts || !rows_fit(n, 0) || n * k > kMaxRows) return TARDIS_ERR_SHAPE;
+    if (!choice_fits(n, experts, k)) return TARDIS_ERR_SHAPE;
     if (renormalise != 0 && renormalise != 1) return TARDIS_ERR_INVALID_ARG;
     if (!offsets || !aligned_to(offsets, 4)) return TARDIS_ERR_INVALID_ARG;
     if (n > 0 && (!logits || !ids || !weights || !order || !place)) return TARDIS_ERR_INVALID_ARG;

@@ -81,3 +81,15 @@ def test_one_row_has_no_distance_to_the_next(hip, gap):  # noqa: F811
         need.append(C.c_int64())
         assert lib.tardis_linear_workspace(T.tardis_linear_desc(8191, 64, T.BF16, T.BF16, 0, 0, W, None), X, 1, pitch, need[-1]) == T.OK
     assert need[0].value == need[1].value
+
+
+def test_the_router_s_question_and_call_have_the_same_limits():
+    """2^30 slots at most."""
+    from test_linear_host import route
+    lib, P = T.lib(), C.c_void_p(0x4000)
+    for n, k, status in ((1 << 30, 2, T.ERR_SHAPE), ((1 << 26) + 1, 16, T.ERR_SHAPE), ((1 << 30) + 1, 1, T.ERR_SHAPE)):
+        need = C.c_int64(5)
+        assert lib.tardis_moe_route_workspace(n, 64, k, need) == status
+        assert route(n=n, experts=64, k=k, work=P, bytes_=1 << 40) == status
+    need = C.c_int64()
+    assert lib.tardis_moe_route_workspace(1 << 26, 64, 16, need) == T.OK and need.value > 0
