@@ -70,7 +70,7 @@ typedef enum {
 typedef enum {
     TARDIS_F32 = 0,
     TARDIS_BF16 = 1,
-    TARDIS_FP8_E4M3 = 2 /* storage of the folded matrix only (tardis_fold_opts.folded_dtype) */
+    TARDIS_FP8_E4M3 = 2 /* storage of the folded matrix (tardis_fold_opts.folded_dtype), outputs of tardis_rms_norm; OCP e4m3, largest value 448 */
 } tardis_dtype_t;
 
 /* One FFN layer (Sec. "Opportunity": FFN(x) = sigma(x W1) W2, here transposed
@@ -404,6 +404,82 @@ tardis_status_t tardis_moe_route_workspace(int64_t n, int64_t experts, int64_t k
 tardis_status_t tardis_moe_combine(const void* z, int64_t rows, const int32_t* place, const float* weights, int64_t n,
                                    int64_t k, int64_t d, int32_t dtype, const void* residual, void* y,
                                    int32_t out_dtype, void* stream);
+
+/* ------------------------------------------------- norms, layers in 8 and 4 bits */
+
+/* What stands in front of a layer, and layers whose weights (and tokens) are held in 8 or 4
+ * bits, for tokens one at a time as for prompts:
+ *     norm (codes and scales) -> tardis_linear_fp8 -> tardis_fp8_rows -> tardis_linear_fp8
+ *     norm (bf16) -> tardis_linear_4bit -> tardis_linear_4bit
+ * As above: no handle, no allocation, no synchronisation, pointers aligned to their elements,
+ * rows and distances up to 2^30, a call with no rows is TARDIS_OK and does nothing, equal calls
+ * give equal bits.  Nothing is written but the outputs named. */
+typedef struct {
+    int64_t d;           /* 1 .. 2^22 */
+    int32_t dtype;       /* of x, weight, residual and sum: TARDIS_F32 or TARDIS_BF16 */
+    int32_t out_dtype;   /* of y: TARDIS_F32, TARDIS_BF16 or TARDIS_FP8_E4M3 */
+    float eps;           /* finite, >= 0 */
+    int32_t reserved;    /* 0 */
+    const void* weight;  /* d, or NULL for ones */
+} tardis_norm_desc;
+
+/* s = x + residual (fp32);  y = s / sqrt(mean(s^2) + eps) * weight, rounded once; the squares are summed
+ * in 64 bits (no row of finite values overflows).  y of a row of zeros is 0 also with eps = 0.
+ *   x         n rows of d values, x_pitch >= d values apart.
+ *   residual  n x d, dtype, or NULL.
+ *   sum       n x d, dtype: s, rounded; or NULL.  May be residual itself, or x itself where x_pitch = d.
+ *   y         n x d, out_dtype; must not overlap the others.
+ *   scales    n floats, where out_dtype is TARDIS_FP8_E4M3 (else NULL): a row's y is its codes
+ *             times scale = max(max |y| / 448, 2^-126), codes rounded to nearest even.  A NaN is a NaN
+ *             code; a row with an infinity has scale infinity and codes of 0 (finite) and NaN. */
+tardis_status_t tardis_rms_norm(const tardis_norm_desc* desc, const void* x, int64_t n, int64_t x_pitch, const void* residual,
+                                void* sum, void* y, float* scales, void* stream);
+
+/* Rows as e4m3 codes with a scale each, as tardis_rms_norm's, without a norm: codes n x d, scales n floats. */
+tardis_status_t tardis_fp8_rows(const void* x, int64_t n, int64_t d, int64_t x_pitch, int32_t dtype, void* codes, float* scales,
+                                void* stream);
+
+typedef struct {
+    int64_t n_in;            /* 1 .. 2^22 */
+    int64_t n_out;           /* 1 .. 2^22 */
+    int32_t out_dtype;       /* of b, the residual and y: TARDIS_F32 or TARDIS_BF16 */
+    int32_t act;             /* tardis_act_t */
+    const void* W;           /* n_out x n_in e4m3 codes */
+    const float* W_scales;   /* n_out, or NULL for ones */
+    const void* b;           /* n_out, or NULL for zero */
+} tardis_linear_fp8_desc;
+
+/* y = sigma(x W^T + b) + residual with x and W in e4m3, a scale for each row of either: products are exact,
+ * sums fp32, scales applied to the sums (the token's first).  sigma, residual, y and work as tardis_linear's.
+ *   x         n rows of n_in codes, x_pitch >= n_in bytes apart.
+ *   x_scales  n floats, or NULL for ones. */
+tardis_status_t tardis_linear_fp8(const tardis_linear_fp8_desc* desc, const void* x, const float* x_scales, int64_t n, int64_t x_pitch,
+                                  const void* residual, void* y, void* work, int64_t work_bytes, void* stream);
+tardis_status_t tardis_linear_fp8_workspace(const tardis_linear_fp8_desc* desc, const void* x, int64_t n, int64_t x_pitch,
+                                            int64_t* bytes);
+
+typedef struct {
+    int64_t n_in;            /* 1 .. 2^22 */
+    int64_t n_out;           /* 1 .. 2^22 */
+    int32_t dtype;           /* of x and scales: TARDIS_F32 or TARDIS_BF16 */
+    int32_t out_dtype;       /* of b, the residual and y: TARDIS_F32 or TARDIS_BF16 */
+    int32_t act;             /* tardis_act_t */
+    int32_t group;           /* columns that share a scale: 32, 64 or 128 */
+    const uint32_t* W;       /* n_out rows of whole groups, G = ceil(n_in / group): G group / 8 words a row, 16-byte
+                              * aligned.  A word has eight columns: column c of them at bit 4 (c / 2) + 16 (c % 2).
+                              * Codes behind n_in count for nothing. */
+    const void* scales;      /* n_out x G */
+    const uint8_t* zeros;    /* n_out x G, 0 .. 128 (more counts as 128), or NULL for 8 */
+    const void* b;           /* n_out, or NULL for zero */
+} tardis_linear_4bit_desc;
+
+/* y = sigma(sum_G scale_jG sum_(k in G) (q_jk - zero_jG) x_k + b_j) + residual, codes q of 4 bits, 0 .. 15.  Products
+ * are exact, sums fp32 (of code and zero point each: tokens up to 2^115), scales applied to the sums of their groups; a
+ * token with an infinity or a NaN is NaN.  x, sigma, residual and y as tardis_linear's.
+ *   work      as tardis_linear's: tardis_linear_4bit_workspace says how much the call can use (0 for many). */
+tardis_status_t tardis_linear_4bit(const tardis_linear_4bit_desc* desc, const void* x, int64_t n, int64_t x_pitch, const void* residual,
+                                   void* y, void* work, int64_t work_bytes, void* stream);
+tardis_status_t tardis_linear_4bit_workspace(const tardis_linear_4bit_desc* desc, int64_t n, int64_t x_pitch, int64_t* bytes);
 
 /* ------------------------------------------------------------- inspection */
 

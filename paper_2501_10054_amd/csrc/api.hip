@@ -657,6 +657,88 @@ tardis_status_t tardis_moe_combine(const void* z, int64_t rows, const int32_t* p
     return td_moe_combine(z, rows, place, weights, n, k, d, dtype, residual, y, out_dtype, static_cast<hipStream_t>(stream));
 }
 
+namespace {
+
+// (a row by itself has no distance to a next one)
+bool norm_rows_fit(int64_t n, int64_t d, int64_t pitch) { return d >= 1 && d <= kMaxWidth && rows_fit(n, n > 1 ? pitch : 0) && pitch >= d; }
+
+tardis_status_t check_layer(int64_t n_in, int64_t n_out, int32_t out_dtype, int32_t act, const void* b) {
+    if (!linear_dtype(out_dtype)) return TARDIS_ERR_DTYPE;
+    if (act < TARDIS_ACT_GELU_ERF || act > TARDIS_ACT_IDENTITY) return TARDIS_ERR_INVALID_ARG;
+    if (n_in < 1 || n_out < 1 || n_in > kMaxWidth || n_out > kMaxWidth) return TARDIS_ERR_SHAPE;
+    return aligned_to(b, td_elem_size(out_dtype)) ? TARDIS_OK : TARDIS_ERR_INVALID_ARG;
+}
+tardis_status_t check_fp8(const tardis_linear_fp8_desc* d, int64_t n, int64_t pitch) {
+    if (!d || !d->W || !aligned_to(d->W_scales, 4)) return TARDIS_ERR_INVALID_ARG;
+    TD_TRY(check_layer(d->n_in, d->n_out, d->out_dtype, d->act, d->b));
+    return rows_fit(n, n > 1 ? pitch : 0) && pitch >= d->n_in ? TARDIS_OK : TARDIS_ERR_SHAPE;
+}
+tardis_status_t check_4bit(const tardis_linear_4bit_desc* d, int64_t n, int64_t pitch) {
+    if (!d || !d->W || !d->scales || !aligned16(d->W)) return TARDIS_ERR_INVALID_ARG;
+    if (!linear_dtype(d->dtype)) return TARDIS_ERR_DTYPE;
+    if ((d->group != 32 && d->group != 64 && d->group != 128) || !aligned_to(d->scales, td_elem_size(d->dtype))) return TARDIS_ERR_INVALID_ARG;
+    TD_TRY(check_layer(d->n_in, d->n_out, d->out_dtype, d->act, d->b));
+    return rows_fit(n, n > 1 ? pitch : 0) && pitch >= d->n_in ? TARDIS_OK : TARDIS_ERR_SHAPE;
+}
+
+}  // namespace
+
+tardis_status_t tardis_rms_norm(const tardis_norm_desc* desc, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* sum, void* y,
+                                float* scales, void* stream) {
+    if (!desc || desc->reserved != 0) return TARDIS_ERR_INVALID_ARG;
+    const bool codes = desc->out_dtype == TARDIS_FP8_E4M3;
+    if (!linear_dtype(desc->dtype) || !(codes || linear_dtype(desc->out_dtype))) return TARDIS_ERR_DTYPE;
+    if (!norm_rows_fit(n, desc->d, x_pitch)) return TARDIS_ERR_SHAPE;
+    const size_t es = td_elem_size(desc->dtype);
+    if (!(desc->eps >= 0.0f && desc->eps <= 3.402823466e38f) || !aligned_to(desc->weight, es)) return TARDIS_ERR_INVALID_ARG;
+    if (n == 0) return TARDIS_OK;
+    if (!x || !y || codes != (scales != nullptr) || !aligned_to(x, es) || !aligned_to(residual, es) || !aligned_to(sum, es) || !aligned_to(scales, 4) ||
+        !(codes || aligned_to(y, td_elem_size(desc->out_dtype))) || (sum && sum == x && n > 1 && x_pitch != desc->d))
+        return TARDIS_ERR_INVALID_ARG;
+    return td_rms_norm(x, n, desc->d, x_pitch, desc->dtype, 1, desc->eps, desc->weight, residual, sum, y, scales, desc->out_dtype,
+                       static_cast<hipStream_t>(stream));
+}
+
+tardis_status_t tardis_fp8_rows(const void* x, int64_t n, int64_t d, int64_t x_pitch, int32_t dtype, void* codes, float* scales, void* stream) {
+    if (!linear_dtype(dtype)) return TARDIS_ERR_DTYPE;
+    if (!norm_rows_fit(n, d, x_pitch)) return TARDIS_ERR_SHAPE;
+    if (n == 0) return TARDIS_OK;
+    if (!x || !codes || !scales || !aligned_to(x, td_elem_size(dtype)) || !aligned_to(scales, 4)) return TARDIS_ERR_INVALID_ARG;
+    return td_rms_norm(x, n, d, x_pitch, dtype, 0, 0.0f, nullptr, nullptr, nullptr, codes, scales, TARDIS_FP8_E4M3, static_cast<hipStream_t>(stream));
+}
+
+tardis_status_t tardis_linear_fp8_workspace(const tardis_linear_fp8_desc* desc, const void* x, int64_t n, int64_t x_pitch, int64_t* bytes) {
+    TD_TRY(check_fp8(desc, n, x_pitch));
+    if (!bytes) return TARDIS_ERR_INVALID_ARG;
+    *bytes = 0;
+    return n > 0 ? td_linear_fp8_work_bytes(desc, x, n, x_pitch, bytes) : TARDIS_OK;
+}
+
+tardis_status_t tardis_linear_fp8(const tardis_linear_fp8_desc* desc, const void* x, const float* x_scales, int64_t n, int64_t x_pitch,
+                                  const void* residual, void* y, void* work, int64_t work_bytes, void* stream) {
+    TD_TRY(check_fp8(desc, n, x_pitch));
+    if (n == 0) return TARDIS_OK;
+    const size_t eo = td_elem_size(desc->out_dtype);
+    if (!x || !y || !aligned_to(x_scales, 4) || !aligned_to(y, eo) || !aligned_to(residual, eo) || !work_ok(work, work_bytes)) return TARDIS_ERR_INVALID_ARG;
+    return td_linear_fp8(desc, x, x_scales, n, x_pitch, residual, y, work, work ? work_bytes : 0, static_cast<hipStream_t>(stream));
+}
+
+tardis_status_t tardis_linear_4bit_workspace(const tardis_linear_4bit_desc* desc, int64_t n, int64_t x_pitch, int64_t* bytes) {
+    TD_TRY(check_4bit(desc, n, x_pitch));
+    if (!bytes) return TARDIS_ERR_INVALID_ARG;
+    *bytes = 0;
+    return n > 0 ? td_linear_4bit_work_bytes(desc, n, x_pitch, bytes) : TARDIS_OK;
+}
+
+tardis_status_t tardis_linear_4bit(const tardis_linear_4bit_desc* desc, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y,
+                                   void* work, int64_t work_bytes, void* stream) {
+    TD_TRY(check_4bit(desc, n, x_pitch));
+    if (n == 0) return TARDIS_OK;
+    const size_t es = td_elem_size(desc->dtype), eo = td_elem_size(desc->out_dtype);
+    if (!x || !y || !aligned_to(x, es) || !aligned_to(y, eo) || !aligned_to(residual, eo) || !work_ok(work, work_bytes)) return TARDIS_ERR_INVALID_ARG;
+    return td_linear_4bit(desc, x, n, x_pitch, residual, y, work, work ? work_bytes : 0, static_cast<hipStream_t>(stream));
+}
+
 tardis_status_t tardis_destroy(tardis_handle_t L) {
     if (!L) return TARDIS_OK;
     {

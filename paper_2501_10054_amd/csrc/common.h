@@ -338,3 +338,14 @@ tardis_status_t td_moe_route(const void* logits, int64_t n, int64_t experts, int
                              int32_t* offsets, int32_t* order, int32_t* place, void* work, hipStream_t s);
 tardis_status_t td_moe_combine(const void* z, int64_t rows, const int32_t* place, const float* weights, int64_t n, int64_t k, int64_t d, int32_t dtype,
                                const void* residual, void* y, int32_t out_dtype, hipStream_t s);
+// norm.hip (n >= 1; norm = 0: y = s)
+tardis_status_t td_rms_norm(const void* x, int64_t n, int64_t d, int64_t x_pitch, int32_t dtype, int norm, float eps, const void* weight,
+                            const void* residual, void* sum, void* y, float* scales, int32_t out_dtype, hipStream_t s);
+// linear.hip: tokens and weights in e4m3
+tardis_status_t td_linear_fp8_work_bytes(const tardis_linear_fp8_desc* d, const void* x, int64_t n, int64_t x_pitch, int64_t* bytes);
+tardis_status_t td_linear_fp8(const tardis_linear_fp8_desc* d, const void* x, const float* x_scales, int64_t n, int64_t x_pitch, const void* residual,
+                              void* y, void* work, int64_t work_bytes, hipStream_t s);
+// linear_4bit.hip
+tardis_status_t td_linear_4bit_work_bytes(const tardis_linear_4bit_desc* d, int64_t n, int64_t x_pitch, int64_t* bytes);
+tardis_status_t td_linear_4bit(const tardis_linear_4bit_desc* d, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y, void* work,
+                               int64_t work_bytes, hipStream_t s);

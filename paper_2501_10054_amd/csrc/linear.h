@@ -5,7 +5,7 @@
 // C = sigma(x W^T + b) + r.  Pitches and k in bytes.
 struct LinearArgs {
     const unsigned char *x, *W;
-    const void *b, *r;             // per column (of every group), element type of W; like y (null: none)
+    const void *b, *r;             // per column (of every group), element type of W (e4m3: of y); like y (null: none)
     void* y;                       // n x N, bf16 or (out_f32) fp32, rows without a gap
     float* part;                   // not null: sums of one range of K each go here, [range][n][N], and nothing else is done
     int64_t n, N, x_pitch, x_rows;
@@ -18,7 +18,11 @@ struct LinearArgs {
     const int32_t *offsets, *order;
     int experts, per_token;
     uint32_t inv_per_token;
+    const float *x_scales, *W_scales;   // e4m3: a scale for each row of x, of W (null: ones)
 };
+
+struct e4m3_t { uint8_t code; };
+struct e4m3_near_t { uint8_t code; };             // multiplied by the faster instruction, for outputs in bf16
 
 constexpr int kActGelu16 = 4;                     // behind tardis_act_t's: GELU for outputs in bf16 without a residual
 constexpr uint32_t kNowhere = 0xe0000000u;        // an offset past the end of any operand that is loaded by offsets
@@ -38,6 +42,12 @@ constexpr bool linear_has(int es, bool direct, bool grouped, int shape) {
     if (es == 2) return !(grouped && shape == 8);
     return !(shape == 2 || (shape >= 4 && shape <= 9) || shape == 12 || (grouped && (shape == 10 || shape == 15)));
 }
+// of e4m3; from kLinearNearFp8 on with outputs in bf16 by the faster instruction, which takes two half-lines of each wavefront
+constexpr LinearShape kLinearShapeFp8[] = {{16, 16, 512}, {16, 32, 512}, {16, 16, 1024}, {32, 32, 512}, {64, 64, 256}, {128, 128, 256}, {128, 128, 128}, {64, 64, 128}};
+constexpr int kLinearNearFp8 = 3;
+constexpr int kLinearShapesFp8 = sizeof(kLinearShapeFp8) / sizeof(LinearShape);
+constexpr LinearShape kLinearStagedFp8[] = {{16, 16, 512}, {32, 32, 256}, {64, 64, 128}, {128, 128, 128}};
+constexpr int kLinearStagedShapesFp8 = sizeof(kLinearStagedFp8) / sizeof(LinearShape);
 // of linear_quad_kernel (bf16, rows in whole pieces)
 constexpr LinearShape kLinearQuad[] = {{256, 256, 128}, {192, 256, 128}, {256, 128, 128}};
 // (rows with which its tiles of groups are full, if the kernel decides so)
@@ -49,4 +59,6 @@ void td_linear_launch_quad(const LinearArgs& p, bool grouped, int shape, int blo
 tardis_status_t td_linear_init_bf16();
 tardis_status_t td_linear_init_f32();
 void td_linear_launch_bf16(const LinearArgs& p, bool grouped, bool direct, int shape, int blocks, hipStream_t s);
+tardis_status_t td_linear_init_fp8();
+void td_linear_launch_fp8(const LinearArgs& p, bool direct, int shape, int blocks, hipStream_t s);
 void td_linear_launch_f32(const LinearArgs& p, bool grouped, bool direct, int shape, int blocks, hipStream_t s);

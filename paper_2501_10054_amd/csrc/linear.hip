@@ -10,6 +10,7 @@ namespace {
 
 bool is_aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 typedef uint32_t any16_t __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t byte16_t __attribute__((ext_vector_type(4), aligned(1)));
 
 // Rows of k bytes, `pitch` apart and at any address, to rows of `units` 16-byte pieces, zeros behind the last element.  (Fewer than 2^32 pieces)
 template <typename T>
@@ -20,13 +21,15 @@ __global__ void __launch_bounds__(256) linear_pack_kernel(const unsigned char* f
     const unsigned char* p = from + (int64_t)row * pitch + at;
     td_u32x4 v = {0, 0, 0, 0};
     if (at + 16 <= k) {
-        v = *reinterpret_cast<const any16_t*>(p);
+        if constexpr (sizeof(T) == 1) v = *reinterpret_cast<const byte16_t*>(p);
+        else v = *reinterpret_cast<const any16_t*>(p);
     } else {
         const T* el = reinterpret_cast<const T*>(p);
 #pragma unroll
         for (uint32_t q = 0; q < 16 / sizeof(T); ++q)
             if (at + q * sizeof(T) < k) {
-                if constexpr (sizeof(T) == 2) v[q / 2] |= (uint32_t)el[q] << (16 * (q & 1));
+                if constexpr (sizeof(T) == 1) v[q / 4] |= (uint32_t)el[q].code << (8 * (q & 3));
+                else if constexpr (sizeof(T) == 2) v[q / 2] |= (uint32_t)el[q] << (16 * (q & 1));
                 else v[q] = __float_as_uint(el[q]);
             }
     }
@@ -45,7 +48,11 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, uint32_t
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         if (q >= columns) continue;
-        if (p.b) bias[q] = td_load<T>(static_cast<const T*>(p.b) + n + q);
+        if constexpr (sizeof(T) == 1) {
+            if (p.b) bias[q] = p.out_f32 ? static_cast<const float*>(p.b)[n + q] : td_load<bf16_t>(static_cast<const bf16_t*>(p.b) + n + q);
+        } else {
+            if (p.b) bias[q] = td_load<T>(static_cast<const T*>(p.b) + n + q);
+        }
         if (p.r) r[q] = p.out_f32 ? static_cast<const float*>(p.r)[at + q] : td_load<bf16_t>(static_cast<const bf16_t*>(p.r) + at + q);
     }
     if (columns == 4) {
@@ -59,6 +66,14 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, uint32_t
         for (int s = 0; s < p.splits; ++s)
             for (int q = 0; q < 4; ++q)
                 if (q < columns) v[q] += p.part[s * range + at + q];
+    }
+    if constexpr (sizeof(T) == 1) {
+        const float token_scale = p.x_scales ? p.x_scales[row] : 1.0f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            v[q] = fmaf(v[q] * token_scale, p.W_scales && q < columns ? p.W_scales[n + q] : 1.0f, bias[q]);
+            bias[q] = 0.0f;
+        }
     }
     with_linear_act(p.act, [&](auto act) {
 #pragma unroll
@@ -95,6 +110,10 @@ constexpr Rate kRateStaged[] = {{2, 0.246f, 0.231f, 4.77f, 3.34f}, {1, 0.389f, 0
                                 {2, 0.228f, 0.214f, 4.34f, 2.79f}, {1, 0.560f, 0.560f, 7.05f, 2.77f}};
 constexpr Rate kRateStagedF32[] = {{2, 0.104f, 0.250f, 4.45f, 4.01f}, {1, 0.377f, 0.377f, 4.45f, 4.01f}, {2, 0.053f, 0.305f, 4.21f, 4.46f},
                                    {2, 0.556f, 0.550f, 4.53f, 5.00f}, {1, 2.042f, 2.042f, 6.55f, 4.71f}};
+constexpr Rate kRateFp8[] = {{2, 0.244f, 0.223f, 3.80f, 5.50f}, {2, 0.415f, 0.400f, 3.74f, 5.51f}, {1, 0.369f, 0.369f, 4.39f, 5.47f}, {1, 0.399f, 0.399f, 4.31f, 4.24f},
+                             {1, 0.450f, 0.450f, 4.53f, 5.33f}, {1, 1.000f, 1.000f, 6.21f, 5.25f}, {2, 0.725f, 0.639f, 4.82f, 3.77f}, {5, 0.489f, 0.262f, 3.07f, 3.94f}};
+constexpr Rate kRateStagedFp8[] = {{2, 0.246f, 0.231f, 4.77f, 3.34f}, {2, 0.176f, 0.227f, 4.35f, 4.73f}, {2, 0.228f, 0.214f, 4.34f, 2.79f}, {1, 0.560f, 0.560f, 7.05f, 2.77f}};
+static_assert(sizeof(kRateFp8) / sizeof(Rate) == kLinearShapesFp8 && sizeof(kRateStagedFp8) / sizeof(Rate) == kLinearStagedShapesFp8, "a rate for each tile");
 static_assert(sizeof(kRate) / sizeof(Rate) == kLinearShapes + kLinearQuads && sizeof(kRateF32) / sizeof(Rate) == kLinearShapes &&
               sizeof(kRateStaged) / sizeof(Rate) == kLinearStagedShapes && sizeof(kRateStagedF32) / sizeof(Rate) == kLinearStagedShapes, "a rate for each tile");
 // one more launch (2.5 on the GPU; callers that are not a graph wait for their host); a byte copied, of partial sums and outputs joined; sigma of an element of a tile, of eight wavefronts and of four
@@ -116,8 +135,18 @@ struct Plan {
     double us;
 };
 
-int shapes_of(bool direct, int es) { return direct ? kLinearShapes + (es == 2 ? kLinearQuads : 0) : kLinearStagedShapes; }
-const LinearShape& shape_of(bool direct, int s) { return !direct ? kLinearStaged[s] : s < kLinearShapes ? kLinearShape[s] : kLinearQuad[s - kLinearShapes]; }
+// (es: bytes of an element - 1 e4m3, 2 bf16, 4 fp32)
+int shapes_below_quads(bool direct, int es) { return es == 1 ? (direct ? kLinearShapesFp8 : kLinearStagedShapesFp8) : direct ? kLinearShapes : kLinearStagedShapes; }
+int shapes_of(bool direct, int es) { return shapes_below_quads(direct, es) + (direct && es == 2 ? kLinearQuads : 0); }
+bool is_quad(bool direct, int es, int s) { return direct && s >= shapes_below_quads(direct, es); }
+const LinearShape& shape_of(bool direct, int es, int s) {
+    if (is_quad(direct, es, s)) return kLinearQuad[s - shapes_below_quads(direct, es)];
+    return es == 1 ? (direct ? kLinearShapeFp8[s] : kLinearStagedFp8[s]) : direct ? kLinearShape[s] : kLinearStaged[s];
+}
+const Rate& rate_of(bool direct, int es, int s) {
+    if (es == 1) return direct ? kRateFp8[s] : kRateStagedFp8[s];
+    return direct ? (es == 2 ? kRate[s] : kRateF32[s]) : es == 2 ? kRateStaged[s] : kRateStagedF32[s];
+}
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
@@ -155,12 +184,13 @@ Plan make_plan(const Call& c, int64_t room) {
         }
         if (p.at_part > room) continue;
         for (int s = 0; s < shapes_of(p.direct, c.es); ++s) {
-            if (!(p.direct && s >= kLinearShapes) && !linear_has(c.es, p.direct, c.experts > 0, s)) continue;
-            const LinearShape& t = shape_of(p.direct, s);
-            const Rate& r = p.direct ? (c.es == 2 ? kRate[s] : kRateF32[s]) : (c.es == 2 ? kRateStaged[s] : kRateStagedF32[s]);
+            const bool quad = is_quad(p.direct, c.es, s);
+            if (c.es != 1 && !quad && !linear_has(c.es, p.direct, c.experts > 0, s)) continue;
+            const LinearShape& t = shape_of(p.direct, c.es, s);
+            const Rate& r = rate_of(p.direct, c.es, s);
             const int64_t slices = (p.k + t.slice - 1) / t.slice, tiles_n = (c.N + t.n - 1) / t.n;
             const double tiles_m = c.experts ? hit * std::max(1.0, (double)c.M / hit / t.m + 0.5) : (double)((c.M + t.m - 1) / t.m);
-            if (most_tiles_m(c, p.direct && s >= kLinearShapes, t) * tiles_n >= kMostTiles) continue;
+            if (most_tiles_m(c, quad, t) * tiles_n >= kMostTiles) continue;
             for (int splits = 1; splits <= 16; splits *= 2) {
                 const double blocks = tiles_m * (double)tiles_n * splits;
                 if (splits > 1 && (c.experts || slices / splits < 4 || blocks > 1024 || p.at_part + splits * c.M * c.N * 4 > room)) break;
@@ -168,9 +198,9 @@ Plan make_plan(const Call& c, int64_t room) {
                 const double rounds = c.experts ? std::max(1.0, blocks / 256 + 0.5) : std::ceil(blocks / 256);
                 const double turns = c.experts ? std::max(1.0, rounds / r.blocks) : std::ceil(rounds / r.blocks);
                 const double per = (double)((slices + splits - 1) / splits);
-                const double sigma = c.act == TARDIS_ACT_GELU_ERF || c.act == TARDIS_ACT_GELU_TANH ? (p.direct && s >= kLinearShapes ? kSigmaQuadUs : kSigmaUs) * t.m * t.n * rounds : 0.0;
+                const double sigma = c.act == TARDIS_ACT_GELU_ERF || c.act == TARDIS_ACT_GELU_TANH ? (quad ? kSigmaQuadUs : kSigmaUs) * t.m * t.n * rounds : 0.0;
                 const double multiply = r.fixed * turns + per * std::max(r.alone * turns, r.slice * rounds) + (splits > 1 ? 0.0 : sigma);
-                const double again = p.direct ? (c.es == 2 ? kAgain : kAgainF32) : (c.es == 2 ? kAgainStaged : kAgainStagedF32);
+                const double again = p.direct ? (c.es == 4 ? kAgainF32 : kAgain) : (c.es == 4 ? kAgainStagedF32 : kAgainStaged);
                 const double bytes = (hit + again * std::max(0.0, tiles_m - hit)) * c.N * p.k + (double)c.M * p.k + (double)c.M * c.N * (splits > 1 ? 4.0 * splits : c.eo);
                 double us = before + std::max(multiply, 1.5 + bytes / (r.tbs * 1e6));
                 if (splits > 1) us += kLaunchUs + (double)c.M * c.N * (4.0 * splits + c.eo) * kJoinUs;
@@ -208,18 +238,19 @@ const Plan& plan_of(const Call& c, int64_t room) {
 }
 
 // p: operands and sizes as the caller gave them; pitches and k in bytes
-tardis_status_t run(LinearArgs p, int32_t dtype, const Call& c, void* work, int64_t work_bytes, hipStream_t s) {
+tardis_status_t run(LinearArgs p, const Call& c, void* work, int64_t work_bytes, hipStream_t s) {
     const Plan& plan = plan_of(c, work_bytes);
     if (plan.splits == 0) return TARDIS_ERR_SHAPE;
-    const LinearShape& t = shape_of(plan.direct, plan.shape);
-    const bool grouped = c.experts > 0, quad = plan.direct && plan.shape >= kLinearShapes, f32 = dtype == TARDIS_F32;
+    const LinearShape& t = shape_of(plan.direct, c.es, plan.shape);
+    const bool grouped = c.experts > 0, quad = is_quad(plan.direct, c.es, plan.shape), f32 = c.es == 4, fp8 = c.es == 1;
     p.tiles_m = (int)((p.n + t.m - 1) / t.m);
     p.tiles_n = (int)((p.N + t.n - 1) / t.n);
     p.tile_rows = (int)std::min<int64_t>(t.m, round_up((p.n + p.tiles_m - 1) / p.tiles_m, 32));
     p.splits = plan.splits;
     p.slices = plan.slices;
     const int64_t tiles = most_tiles_m(c, quad, t) * p.tiles_n * plan.splits;
-    if (f32) TD_TRY(td_linear_init_f32());
+    if (fp8) TD_TRY(td_linear_init_fp8());
+    else if (f32) TD_TRY(td_linear_init_f32());
     else TD_TRY(quad ? td_linear_init_quad() : td_linear_init_bf16());
     unsigned char* memory = static_cast<unsigned char*>(work);
     auto pack = [&](const unsigned char* from, int64_t pitch, int64_t rows, unsigned char* to) {
@@ -230,7 +261,8 @@ tardis_status_t run(LinearArgs p, int32_t dtype, const Call& c, void* work, int6
             const unsigned char* first = from + row * pitch;
             td_u32x4* at = reinterpret_cast<td_u32x4*>(to) + row * units;
             const dim3 grid((here * units + 255) / 256);
-            if (f32) hipLaunchKernelGGL(linear_pack_kernel<float>, grid, dim3(256), 0, s, first, pitch, (uint32_t)c.k, at, here, units);
+            if (fp8) hipLaunchKernelGGL(linear_pack_kernel<e4m3_t>, grid, dim3(256), 0, s, first, pitch, (uint32_t)c.k, at, here, units);
+            else if (f32) hipLaunchKernelGGL(linear_pack_kernel<float>, grid, dim3(256), 0, s, first, pitch, (uint32_t)c.k, at, here, units);
             else hipLaunchKernelGGL(linear_pack_kernel<bf16_t>, grid, dim3(256), 0, s, first, pitch, (uint32_t)c.k, at, here, units);
         }
         return to;
@@ -246,14 +278,16 @@ tardis_status_t run(LinearArgs p, int32_t dtype, const Call& c, void* work, int6
         q.act = TARDIS_ACT_IDENTITY;
     }
     const int blocks = (int)((tiles + 7) / 8 * 8);
-    if (quad) td_linear_launch_quad(q, grouped, plan.shape - kLinearShapes, blocks, s);
+    if (fp8) td_linear_launch_fp8(q, plan.direct, plan.shape, blocks, s);
+    else if (quad) td_linear_launch_quad(q, grouped, plan.shape - kLinearShapes, blocks, s);
     else if (f32) td_linear_launch_f32(q, grouped, plan.direct, plan.shape, blocks, s);
     else td_linear_launch_bf16(q, grouped, plan.direct, plan.shape, blocks, s);
     if (plan.splits > 1) {
         p.part = q.part;
         const int64_t units = (p.N + 3) / 4;
         const dim3 grid((unsigned)((units * p.n + 255) / 256));
-        if (f32) hipLaunchKernelGGL(linear_join_kernel<float>, grid, dim3(256), 0, s, p, (uint32_t)units);
+        if (fp8) hipLaunchKernelGGL(linear_join_kernel<e4m3_t>, grid, dim3(256), 0, s, p, (uint32_t)units);
+        else if (f32) hipLaunchKernelGGL(linear_join_kernel<float>, grid, dim3(256), 0, s, p, (uint32_t)units);
         else hipLaunchKernelGGL(linear_join_kernel<bf16_t>, grid, dim3(256), 0, s, p, (uint32_t)units);
     }
     TD_HIP(hipGetLastError());
@@ -280,6 +314,11 @@ Call call_of(const tardis_linear_desc* d, int64_t experts, const void* x, int64_
             is_aligned16(x), is_aligned16(d->W)};
 }
 
+Call call_of(const tardis_linear_fp8_desc* d, const void* x, int64_t n, int64_t x_pitch) {
+    if (n == 1) x_pitch = d->n_in;
+    return {n, d->n_out, n, d->n_in, x_pitch, 1, (int)td_elem_size(d->out_dtype), d->act, 0, false, is_aligned16(x), is_aligned16(d->W)};
+}
+
 constexpr int64_t kAnyRoom = (int64_t)1 << 62;
 
 }  // namespace
@@ -299,7 +338,32 @@ tardis_status_t td_linear(const tardis_linear_desc* d, const void* x, int64_t n,
     p.r = residual;
     p.y = y;
     p.n = p.x_rows = n;
-    return run(p, d->dtype, call_of(d, 0, x, n, x_pitch, false, n), work, work_bytes, s);
+    return run(p, call_of(d, 0, x, n, x_pitch, false, n), work, work_bytes, s);
+}
+
+tardis_status_t td_linear_fp8_work_bytes(const tardis_linear_fp8_desc* d, const void* x, int64_t n, int64_t x_pitch, int64_t* bytes) {
+    const Plan plan = make_plan(call_of(d, x, n, x_pitch), kAnyRoom);
+    if (plan.splits == 0) return TARDIS_ERR_SHAPE;
+    *bytes = plan.work;
+    return TARDIS_OK;
+}
+
+tardis_status_t td_linear_fp8(const tardis_linear_fp8_desc* d, const void* x, const float* x_scales, int64_t n, int64_t x_pitch, const void* residual,
+                              void* y, void* work, int64_t work_bytes, hipStream_t s) {
+    LinearArgs p{};
+    p.x = bytes_of(x);
+    p.W = bytes_of(d->W);
+    p.b = d->b;
+    p.r = residual;
+    p.y = y;
+    p.n = p.x_rows = n;
+    p.N = d->n_out;
+    p.k = (uint32_t)d->n_in;
+    p.act = d->act == TARDIS_ACT_GELU_ERF && d->out_dtype == TARDIS_BF16 && !residual ? kActGelu16 : d->act;
+    p.out_f32 = d->out_dtype == TARDIS_F32;
+    p.x_scales = x_scales;
+    p.W_scales = d->W_scales;
+    return run(p, call_of(d, x, n, x_pitch), work, work_bytes, s);
 }
 
 tardis_status_t td_grouped_linear(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, const int32_t* offsets,
@@ -314,5 +378,5 @@ tardis_status_t td_grouped_linear(const tardis_linear_desc* d, int64_t experts, 
     p.experts = (int)experts;
     p.per_token = (int)per_token;
     p.inv_per_token = per_token > 1 ? (uint32_t)(0x100000000ull / (uint64_t)per_token) : 0xffffffffu;
-    return run(p, d->dtype, call_of(d, experts, x, x_rows, x_pitch, order != nullptr, positions), work, work_bytes, s);
+    return run(p, call_of(d, experts, x, x_rows, x_pitch, order != nullptr, positions), work, work_bytes, s);
 }

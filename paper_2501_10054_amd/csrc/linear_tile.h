@@ -1,5 +1,5 @@
 // y = sigma(x W^T + b) + r for one weight matrix, or for one of several by groups of rows (mixture of experts): the kernel, for one
-// element type of x, W and b (linear_bf16.hip, linear_f32.hip); which tile a call takes is linear.hip's.
+// element type of x, W and b (linear_bf16.hip, linear_f32.hip), or x and W in e4m3 with scales (linear_fp8.hip); which tile a call takes is linear.hip's.
 #pragma once
 #include "linear_act.h"
 #include "tiles.h"
@@ -11,6 +11,11 @@ typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x4_any_t __attribute__((ext_vector_type(4), aligned(2)));
 
 __device__ __forceinline__ td_u32x4 load_any16(const void* p) { return *static_cast<const u32x4_any_t*>(p); }
+typedef uint32_t u32x4_byte_t __attribute__((ext_vector_type(4), aligned(1)));
+template <typename T> __device__ __forceinline__ td_u32x4 load_elements16(const void* p) {
+    if constexpr (sizeof(T) == 1) return *static_cast<const u32x4_byte_t*>(p);
+    else return load_any16(p);
+}
 __device__ __forceinline__ void store_any16(void* p, const td_u32x4& v) { *static_cast<u32x4_any_t*>(p) = v; }
 
 // One 16 x 16 block of sums: w, x hold 16 bytes of row lane % 16 at piece lane / 16 of 64 bytes of K.  (fp32: element q of all four
@@ -22,6 +27,31 @@ template <> __device__ __forceinline__ void mma_pieces<bf16_t>(f32x4_t& c, const
 template <> __device__ __forceinline__ void mma_pieces<float>(f32x4_t& c, const td_u32x4& w, const td_u32x4& x) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w[q]), __uint_as_float(x[q]), c, 0, 0, 0);
+}
+
+// Codes, exactly: as bf16 values, which every code is, so that the sums are those of bf16.  (How a lane's bytes lie in K is the same for both operands)
+__device__ __forceinline__ bf16x8_t codes_as_bf16(uint32_t a, uint32_t b) {
+    bf16x8_t v;
+    const bf16x2_t p[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(a, 1.0f, true),
+                           __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(b, 1.0f, true)};
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = p[q / 2][q % 2];
+    return v;
+}
+template <> __device__ __forceinline__ void mma_pieces<e4m3_t>(f32x4_t& c, const td_u32x4& w, const td_u32x4& x) {
+#pragma unroll
+    for (int h = 0; h < 4; h += 2)
+        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(codes_as_bf16(w[h], w[h + 1]), codes_as_bf16(x[h], x[h + 1]), c, 0, 0, 0);
+}
+// Codes at twice bf16's rate: a lane has two pieces of 128 bytes of K.  The instruction adds a lane's products up before they meet the accumulator, and
+// drops of each what is less than 2^-13 of the largest (measured: 2^16 and 2^2 are 2^16; parts of other lanes and the accumulator are added in fp32): for
+// sums of many products 1e-4 of their root of squares at most, against the 2e-3 by which outputs in bf16 are rounded.  So it is for these
+// outputs, and where tiles are large enough for the matrix cores to count.
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ void mma_two_pieces(f32x4_t& c, const td_u32x4& w0, const td_u32x4& w1, const td_u32x4& x0, const td_u32x4& x1) {
+    const i32x8_t w = {(int)w0[0], (int)w0[1], (int)w0[2], (int)w0[3], (int)w1[0], (int)w1[1], (int)w1[2], (int)w1[3]};
+    const i32x8_t x = {(int)x0[0], (int)x0[1], (int)x0[2], (int)x0[3], (int)x1[0], (int)x1[1], (int)x1[2], (int)x1[3]};
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, c, 0, 0, 0, 0, 0, 0);   // (without scales)
 }
 
 // n / d for n < 2^21
@@ -233,15 +263,34 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
         const uint32_t as_f32 = w[q / 4][q % 4], pair = w[0][q / 2];
         return __uint_as_float(f32 ? as_f32 : q & 1 ? pair & 0xffff0000u : pair << 16);
     };
+    constexpr bool SCALED = sizeof(T) == 1;
+    const bool bias_f32 = SCALED ? p.out_f32 != 0 : sizeof(T) == 4;
     float bias[8] = {};
     if (p.b && !p.part && columns > 0) {
         td_u32x4 w[2];
-        load8(p.b, (int64_t)b.expert * p.N + n, sizeof(T) == 4, w);
+        load8(p.b, (int64_t)b.expert * p.N + n, bias_f32, w);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) bias[q] = value(w, sizeof(T) == 4, q);
+        for (int q = 0; q < 8; ++q) bias[q] = value(w, bias_f32, q);
     }
 #pragma unroll
     for (int q = 0; q < 8; ++q) asm volatile("" : "+v"(bias[q]));
+    // scales of codes: a token's go to the sums on their way to LDS, a column's behind it (of ranges' sums: when they are joined)
+    float scale[8], token_scale[FA];
+    if constexpr (SCALED) {
+        td_u32x4 w[2];
+        if (p.W_scales && !p.part && columns > 0) load8(p.W_scales, n, true, w);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) scale[q] = p.W_scales && !p.part && columns > 0 ? value(w, true, q) : 1.0f;
+#pragma unroll
+        for (int i = 0; i < FA; ++i) {
+            const int m = (WM * i + wm) * 16 + frow;
+            token_scale[i] = p.x_scales && !p.part && m < b.rows ? p.x_scales[b.first + m] : 1.0f;
+        }
+#pragma unroll
+        for (int q = 0; q < 8; ++q) asm volatile("" : "+v"(scale[q]));
+#pragma unroll
+        for (int i = 0; i < FA; ++i) asm volatile("" : "+v"(token_scale[i]));
+    }
     // row of the tile that the thread has in turn t of the row blocks from i0 on
     auto row_of = [&](int i0, int t, int& at) {
         at = me / UNITS + t * STRIDE;
@@ -265,7 +314,7 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
         for (int i = 0; i < RB; ++i)
 #pragma unroll
             for (int j = 0; j < FB; ++j)
-                *reinterpret_cast<f32x4_t*>(stage + place_of(wk, ((OWN ? 0 : wm * RB) + i) * 16 + frow, ((OWN ? 0 : wn * FB) + j) * 4 + fp)) = acc[i0 + i][j];
+                *reinterpret_cast<f32x4_t*>(stage + place_of(wk, ((OWN ? 0 : wm * RB) + i) * 16 + frow, ((OWN ? 0 : wn * FB) + j) * 4 + fp)) = SCALED ? acc[i0 + i][j] * token_scale[i0 + i] : acc[i0 + i][j];
         sync();
         // (sums of a range of K: act is the identity, without bias and residual)
         with_linear_act(p.act, [&](auto act) {
@@ -276,7 +325,7 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
 #pragma unroll
                     for (int part = 1; part < WK; ++part) sum += *reinterpret_cast<const f32x4_t*>(stage + place_of(part, at, unit * 2 + h));
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) v[4 * h + q] = linear_act<decltype(act)::value>(sum[q] + bias[4 * h + q]);
+                    for (int q = 0; q < 4; ++q) v[4 * h + q] = linear_act<decltype(act)::value>(SCALED ? fmaf(sum[q], scale[4 * h + q], bias[4 * h + q]) : sum[q] + bias[4 * h + q]);
                 }
             };
             auto store = [&](int64_t to, const float (&v)[8]) {
@@ -343,7 +392,7 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
 // registers, D slices ahead, whatever the alignment (odd widths, odd pitches, rows that are 8 MB apart, gathered ones of 3.5 GB; aligned ones where the rule in linear.hip finds
 // it faster: 509 x 1500 x 1000 in fp32).
 template <typename T, bool GROUPED, bool DIRECT, int FA, int FB, int WM, int WN, int WK, int KS, int D>
-__global__ void __launch_bounds__(64 * WM * WN * WK, 2) linear_kernel(LinearArgs p) {
+__device__ __forceinline__ void linear_tile(const LinearArgs& p) {
     typedef LinearTile<T, DIRECT, FA, FB, WM, WN, WK, KS, D> G;
     constexpr int TM = G::TM, TN = G::TN, SL = G::SL, LA = G::LA, LB = G::LB, PS = SL / 16, RPL = 64 / PS, SWZ = PS < 16 ? PS - 1 : 15;
     extern __shared__ __align__(1024) unsigned char lds[];
@@ -407,12 +456,21 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, 2) linear_kernel(LinearArgs
         }
     };
     auto multiply = [&](auto rows, const Fragments& f) {
+        if constexpr (std::is_same_v<T, e4m3_near_t>) {
 #pragma unroll
-        for (int s = 0; s < KS; ++s)
+            for (int s = 0; s < KS; s += 2)
 #pragma unroll
-            for (int i = 0; i < decltype(rows)::value; ++i)
+                for (int i = 0; i < decltype(rows)::value; ++i)
 #pragma unroll
-                for (int j = 0; j < FB; ++j) mma_pieces<T>(acc[i][j], f.b[s][j], f.a[s][i]);
+                    for (int j = 0; j < FB; ++j) mma_two_pieces(acc[i][j], f.b[s][j], f.b[s + 1][j], f.a[s][i], f.a[s + 1][i]);
+        } else {
+#pragma unroll
+            for (int s = 0; s < KS; ++s)
+#pragma unroll
+                for (int i = 0; i < decltype(rows)::value; ++i)
+#pragma unroll
+                    for (int j = 0; j < FB; ++j) mma_pieces<T>(acc[i][j], f.b[s][j], f.a[s][i]);
+        }
     };
 
     if constexpr (DIRECT) {
@@ -545,9 +603,9 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, 2) linear_kernel(LinearArgs
         auto load_slice = [&](Pieces& v, int t) {         // (past the last whole slice: that one again)
             const uint32_t soff = (uint32_t)slice_of(min(t, whole - 1)) * SL;
 #pragma unroll
-            for (int i = 0; i < LB; ++i) v.b[i] = load_any16(from_b[i] + soff);
+            for (int i = 0; i < LB; ++i) v.b[i] = load_elements16<T>(from_b[i] + soff);
 #pragma unroll
-            for (int i = 0; i < LA; ++i) v.a[i] = load_any16(from_a[i] + soff);
+            for (int i = 0; i < LA; ++i) v.a[i] = load_elements16<T>(from_a[i] + soff);
         };
         Pieces v[D];
         auto step = [&](Pieces& now, int t) {             // (the place in LDS was read two slices ago, before the last barrier)
@@ -580,7 +638,8 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, 2) linear_kernel(LinearArgs
 #pragma unroll
                 for (uint32_t u = 0; u < 16 / sizeof(T); ++u)
                     if (u < n) {
-                        if constexpr (sizeof(T) == 2) w[u / 2] |= (uint32_t)el[u] << (16 * (u & 1));
+                        if constexpr (sizeof(T) == 1) w[u / 4] |= (uint32_t)el[u].code << (8 * (u & 3));
+                        else if constexpr (sizeof(T) == 2) w[u / 2] |= (uint32_t)el[u] << (16 * (u & 1));
                         else w[u] = __float_as_uint(el[u]);
                     }
                 return w;
@@ -599,6 +658,11 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, 2) linear_kernel(LinearArgs
     __syncthreads();
 
     finish_linear<T, GROUPED, G::W, FA, FB, WM, WN, WK, G::RB>(p, b, acc, lds, tid);
+}
+
+template <typename T, bool GROUPED, bool DIRECT, int FA, int FB, int WM, int WN, int WK, int KS, int D>
+__global__ void __launch_bounds__(64 * WM * WN * WK, 2) linear_kernel(LinearArgs p) {
+    linear_tile<T, GROUPED, DIRECT, FA, FB, WM, WN, WK, KS, D>(p);
 }
 
 }  // namespace

@@ -1,0 +1,269 @@
+// The root-mean-square norm in front of a layer, with the residual's addition in front of it, and rows put into 8 bits:
+//     s = x + residual,  y = s / sqrt(mean(s^2) + eps) * weight,  output in bf16, fp32, or e4m3 codes with a scale for each row.
+#include <algorithm>
+
+#include "tiles.h"
+
+namespace {
+
+struct NormArgs {
+    const unsigned char *x, *residual, *weight;   // (null: none)
+    unsigned char *sum, *y;                       // (sum null: not asked for)
+    float* scales;                                // of outputs in e4m3
+    int64_t n, x_pitch;                           // (bytes)
+    uint32_t d, units;                            // columns, pieces of 8 of them
+    int waves;                                    // of a row
+    int norm;                                     // 0: y = s
+    double inv_d, eps;
+};
+
+constexpr float kE4m3Most = 448.0f, kLeastScale = 0x1p-126f;
+// (rows begin at any element's address)
+typedef uint32_t norm_u32x4_t __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t norm_u32x2_t __attribute__((ext_vector_type(2), aligned(1)));
+
+// 8 elements from an element's address; `left` of them are there, the others 0
+template <typename T> __device__ __forceinline__ void load8(float (&v)[8], const unsigned char* from, uint32_t left) {
+    if (left >= 8) {
+        const norm_u32x4_t a = *reinterpret_cast<const norm_u32x4_t*>(from);
+        if constexpr (sizeof(T) == 4) {
+            const norm_u32x4_t b = *reinterpret_cast<const norm_u32x4_t*>(from + 16);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] = __uint_as_float(a[q]), v[4 + q] = __uint_as_float(b[q]);
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[2 * q] = __uint_as_float(a[q] << 16), v[2 * q + 1] = __uint_as_float(a[q] & 0xffff0000u);
+        }
+    } else {
+#pragma unroll
+        for (uint32_t q = 0; q < 8; ++q) v[q] = q < left ? td_load<T>(reinterpret_cast<const T*>(from) + q) : 0.0f;
+    }
+}
+
+// f32: as they are; else two in a word, rounded to bf16
+template <bool F32> __device__ __forceinline__ void store8(unsigned char* to, const float (&v)[8], uint32_t left) {
+    if constexpr (F32) {
+        if (left >= 8) {
+            norm_u32x4_t a, b;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) a[q] = __float_as_uint(v[q]), b[q] = __float_as_uint(v[4 + q]);
+            *reinterpret_cast<norm_u32x4_t*>(to) = a;
+            *reinterpret_cast<norm_u32x4_t*>(to + 16) = b;
+        } else {
+#pragma unroll
+            for (uint32_t q = 0; q < 8; ++q)
+                if (q < left) reinterpret_cast<float*>(to)[q] = v[q];
+        }
+    } else {
+        norm_u32x4_t a;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) a[q] = to_bf16x2(v[2 * q], v[2 * q + 1]);
+        if (left >= 8) {
+            *reinterpret_cast<norm_u32x4_t*>(to) = a;
+        } else {
+#pragma unroll
+            for (uint32_t q = 0; q < 8; ++q)
+                if (q < left) reinterpret_cast<bf16_t*>(to)[q] = (bf16_t)(a[q / 2] >> (16 * (q & 1)));
+        }
+    }
+}
+
+__device__ __forceinline__ void store_codes(unsigned char* to, const float (&v)[8], float inverse, uint32_t left) {
+    norm_u32x2_t c = {0, 0};
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        int w = 0;
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h] * inverse, v[4 * h + 1] * inverse, w, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2] * inverse, v[4 * h + 3] * inverse, w, true);
+        c[h] = (uint32_t)w;
+    }
+    if (left >= 8) {
+        *reinterpret_cast<norm_u32x2_t*>(to) = c;
+    } else {
+#pragma unroll
+        for (uint32_t q = 0; q < 8; ++q)
+            if (q < left) to[q] = (unsigned char)(c[q / 4] >> (8 * (q & 3)));
+    }
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+    return v;
+}
+
+// s / rms = ldexp(s, -half) * factor: the squares are summed in 64 bits and the exponent is taken out, so that rows of any magnitude that
+// fp32 holds have the norm of the formula (a row of zeros with eps = 0: zeros).
+struct RowScale {
+    int half;
+    float factor;
+};
+__device__ __forceinline__ RowScale row_scale(double sum, const NormArgs& p) {
+    const double v = sum * p.inv_d + p.eps;
+    RowScale r;
+    r.half = __builtin_amdgcn_frexp_exp(v) >> 1;
+    r.factor = v > 0.0 || v != v ? (float)(1.0 / sqrt(__builtin_amdgcn_ldexp(v, -2 * r.half))) : 0.0f;
+    return r;
+}
+
+// U pieces of 8 elements of a thread stay in registers; U = 0: rows of any length, read again for each step.  OUT: tardis_dtype_t.
+template <typename T, int OUT, int U>
+__global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs p) {
+    constexpr bool KEPT = U > 0;
+    constexpr int N = KEPT ? U : 1;
+    __shared__ double sums[16];
+    __shared__ float tops[16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), mine = wave % p.waves;
+    const int64_t row = (int64_t)blockIdx.x * ((int)(blockDim.x >> 6) / p.waves) + wave / p.waves;
+    const bool there = row < p.n;                 // (no return: all wavefronts come to the barriers)
+    const uint32_t step = (uint32_t)p.waves * 64u, first = (uint32_t)(mine * 64 + lane), units = there ? p.units : 0u;
+    const unsigned char* x = p.x + row * p.x_pitch;
+    const int64_t at = row * (int64_t)p.d;
+    auto summand = [&](uint32_t u, float (&s)[8]) {
+        const uint32_t left = p.d - u * 8u;
+        load8<T>(s, x + (size_t)u * 8 * sizeof(T), left);
+        if (p.residual) {
+            float r[8];
+            load8<T>(r, p.residual + (at + (int64_t)u * 8) * sizeof(T), left);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s[q] += r[q];
+        }
+    };
+    auto weighed = [&](uint32_t u, float (&s)[8], const RowScale& r) {
+        if (p.norm) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s[q] = __builtin_amdgcn_ldexpf(s[q], -r.half) * r.factor;
+        }
+        if (p.weight) {
+            float w[8];
+            load8<T>(w, p.weight + (size_t)u * 8 * sizeof(T), p.d - u * 8u);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) s[q] *= w[q];
+        }
+    };
+    auto over_row = [&](auto f) {                  // f(piece, kept values of it)
+        if constexpr (KEPT) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const uint32_t u = first + (uint32_t)i * step;
+                if (u < units) f(u, i);
+            }
+        } else {
+            for (uint32_t u = first; u < units; u += step) f(u, 0);
+        }
+    };
+    float s[N][8];
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s[i][q] = 0.0f;
+    RowScale r{0, 1.0f};
+    double sum = 0.0;
+    if (KEPT || p.norm)
+        over_row([&](uint32_t u, int i) {
+            summand(u, s[i]);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) sum += (double)s[i][q] * (double)s[i][q];
+        });
+    if (p.norm) {
+        sum = wave_sum(sum);
+        if (p.waves > 1) {
+            if (lane == 0) sums[wave] = sum;
+            __syncthreads();
+            sum = 0.0;
+            for (int w = 0; w < p.waves; ++w) sum += sums[wave - mine + w];
+        }
+        r = row_scale(sum, p);
+    }
+    if (KEPT && p.sum) over_row([&](uint32_t u, int i) { store8<sizeof(T) == 4>(p.sum + (at + (int64_t)u * 8) * sizeof(T), s[i], p.d - u * 8u); });
+    if constexpr (OUT == TARDIS_FP8_E4M3) {
+        float top = 0.0f;
+        over_row([&](uint32_t u, int i) {
+            if (!KEPT) summand(u, s[i]);
+            weighed(u, s[i], r);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) top = fmaxf(top, fabsf(s[i][q]));
+        });
+        top = td_wave_max(top);
+        if (p.waves > 1) {
+            if (lane == 0) tops[wave] = top;
+            __syncthreads();
+            for (int w = 0; w < p.waves; ++w) top = fmaxf(top, tops[wave - mine + w]);
+        }
+        const float scale = fmaxf(top / kE4m3Most, kLeastScale), inverse = 1.0f / scale;
+        if (there && mine == 0 && lane == 0) p.scales[row] = scale;
+        over_row([&](uint32_t u, int i) {
+            const uint32_t left = p.d - u * 8u;
+            if (!KEPT) {
+                summand(u, s[i]);
+                if (p.sum) store8<sizeof(T) == 4>(p.sum + (at + (int64_t)u * 8) * sizeof(T), s[i], left);
+                weighed(u, s[i], r);
+            }
+            store_codes(p.y + at + (int64_t)u * 8, s[i], inverse, left);
+        });
+    } else {
+        over_row([&](uint32_t u, int i) {
+            const uint32_t left = p.d - u * 8u;
+            if (!KEPT) {
+                summand(u, s[i]);
+                if (p.sum) store8<sizeof(T) == 4>(p.sum + (at + (int64_t)u * 8) * sizeof(T), s[i], left);
+            }
+            weighed(u, s[i], r);
+            store8<OUT == TARDIS_F32>(p.y + (at + (int64_t)u * 8) * (OUT == TARDIS_F32 ? 4 : 2), s[i], left);
+        });
+    }
+}
+
+template <typename T, int OUT> void launch(const NormArgs& p, int each, dim3 grid, dim3 block, hipStream_t s) {
+    if (each == 1) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, 1>), grid, block, 0, s, p);
+    else if (each == 2) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, 2>), grid, block, 0, s, p);
+    else if (each <= 4) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, 4>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((rms_norm_kernel<T, OUT, 0>), grid, block, 0, s, p);
+}
+
+template <typename T> void launch(const NormArgs& p, int out, int each, dim3 grid, dim3 block, hipStream_t s) {
+    if (out == TARDIS_FP8_E4M3) launch<T, TARDIS_FP8_E4M3>(p, each, grid, block, s);
+    else if (out == TARDIS_F32) launch<T, TARDIS_F32>(p, each, grid, block, s);
+    else launch<T, TARDIS_BF16>(p, each, grid, block, s);
+}
+
+}  // namespace
+
+tardis_status_t td_rms_norm(const void* x, int64_t n, int64_t d, int64_t x_pitch, int32_t dtype, int norm, float eps, const void* weight,
+                            const void* residual, void* sum, void* y, float* scales, int32_t out_dtype, hipStream_t s) {
+    NormArgs p{};
+    p.x = static_cast<const unsigned char*>(x);
+    p.residual = static_cast<const unsigned char*>(residual);
+    p.weight = static_cast<const unsigned char*>(weight);
+    p.sum = static_cast<unsigned char*>(sum);
+    p.y = static_cast<unsigned char*>(y);
+    p.scales = scales;
+    p.n = n;
+    p.x_pitch = x_pitch * (int64_t)td_elem_size(dtype);
+    p.d = (uint32_t)d;
+    p.units = (uint32_t)((d + 7) / 8);
+    p.norm = norm;
+    p.inv_d = 1.0 / (double)d;
+    p.eps = (double)eps;
+    p.waves = 1;
+    while (p.waves < 16 && (int64_t)p.waves * 64 < p.units) p.waves *= 2;
+    const int each = (int)((p.units + p.waves * 64 - 1) / (p.waves * 64));
+    const int rows = std::max(1, 4 / p.waves), threads = 64 * p.waves * rows;
+    const int64_t most = kMostThreads / threads;                       // blocks of a launch
+    const int64_t blocks = (n + rows - 1) / rows;
+    for (int64_t b = 0; b < blocks; b += most) {
+        const dim3 grid((unsigned)std::min(most, blocks - b)), block((unsigned)threads);
+        NormArgs q = p;
+        const int64_t row = b * rows;
+        q.x += row * p.x_pitch;
+        if (q.residual) q.residual += row * d * (int64_t)td_elem_size(dtype);
+        if (q.sum) q.sum += row * d * (int64_t)td_elem_size(dtype);
+        q.y += row * d * (out_dtype == TARDIS_FP8_E4M3 ? 1 : (int64_t)td_elem_size(out_dtype));
+        if (q.scales) q.scales += row;
+        q.n = n - row;
+        if (dtype == TARDIS_F32) launch<float>(q, out_dtype, each, grid, block, s);
+        else launch<bf16_t>(q, out_dtype, each, grid, block, s);
+    }
+    TD_HIP(hipGetLastError());
+    return TARDIS_OK;
+}

@@ -28,6 +28,7 @@ EXPORTS = (
     "tardis_ffn_forward_static", "tardis_stack_forward", "tardis_dense_forward", "tardis_get_folded", "tardis_get_predictor_state",
     "tardis_get_sketch_groups", "tardis_get_last_outliers", "tardis_get_last_union", "tardis_get_handover", "tardis_set_next_layer",
     "tardis_linear", "tardis_linear_workspace", "tardis_grouped_linear", "tardis_grouped_linear_workspace", "tardis_moe_route", "tardis_moe_route_workspace", "tardis_moe_combine",
+    "tardis_rms_norm", "tardis_fp8_rows", "tardis_linear_fp8", "tardis_linear_fp8_workspace", "tardis_linear_4bit", "tardis_linear_4bit_workspace",
     "tardis_destroy", "tardis_release_memory", "tardis_status_string", "tardis_version",
 )
 
@@ -51,6 +52,20 @@ class tardis_fold_opts(C.Structure):
 class tardis_linear_desc(C.Structure):
     _fields_ = [("n_in", C.c_int64), ("n_out", C.c_int64), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("act", C.c_int32),
                 ("reserved", C.c_int32), ("W", C.c_void_p), ("b", C.c_void_p)]
+
+
+class tardis_norm_desc(C.Structure):
+    _fields_ = [("d", C.c_int64), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("eps", C.c_float), ("reserved", C.c_int32), ("weight", C.c_void_p)]
+
+
+class tardis_linear_fp8_desc(C.Structure):
+    _fields_ = [("n_in", C.c_int64), ("n_out", C.c_int64), ("out_dtype", C.c_int32), ("act", C.c_int32), ("W", C.c_void_p), ("W_scales", C.c_void_p),
+                ("b", C.c_void_p)]
+
+
+class tardis_linear_4bit_desc(C.Structure):
+    _fields_ = [("n_in", C.c_int64), ("n_out", C.c_int64), ("dtype", C.c_int32), ("out_dtype", C.c_int32), ("act", C.c_int32), ("group", C.c_int32),
+                ("W", C.c_void_p), ("scales", C.c_void_p), ("zeros", C.c_void_p), ("b", C.c_void_p)]
 
 
 _lib_handle = None
@@ -89,6 +104,13 @@ def lib() -> C.CDLL:
         L.tardis_moe_route.argtypes = [vp, i64, i64, i64, C.c_int32, C.c_int32, vp, vp, vp, vp, vp, vp, i64, vp]
         L.tardis_moe_route_workspace.argtypes = [i64, i64, i64, C.POINTER(i64)]
         L.tardis_moe_combine.argtypes = [vp, i64, vp, vp, i64, i64, i64, C.c_int32, vp, vp, C.c_int32, vp]
+        norm, fp8, four = C.POINTER(tardis_norm_desc), C.POINTER(tardis_linear_fp8_desc), C.POINTER(tardis_linear_4bit_desc)
+        L.tardis_rms_norm.argtypes = [norm, vp, i64, i64, vp, vp, vp, vp, vp]
+        L.tardis_fp8_rows.argtypes = [vp, i64, i64, i64, C.c_int32, vp, vp, vp]
+        L.tardis_linear_fp8.argtypes = [fp8, vp, vp, i64, i64, vp, vp, vp, i64, vp]
+        L.tardis_linear_fp8_workspace.argtypes = [fp8, vp, i64, i64, C.POINTER(i64)]
+        L.tardis_linear_4bit.argtypes = [four, vp, i64, i64, vp, vp, vp, i64, vp]
+        L.tardis_linear_4bit_workspace.argtypes = [four, i64, i64, C.POINTER(i64)]
         L.tardis_destroy.argtypes = [vp]
         L.tardis_release_memory.argtypes = []
         L.tardis_status_string.argtypes = [C.c_int]
@@ -442,4 +464,148 @@ def tardis_moe_combine(z, place, weights, residual=None, out_dtype=None, y=None,
         assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, d) and y.get_device() == dev
     _check(lib().tardis_moe_combine(z.data_ptr(), rows, place.data_ptr(), weights.data_ptr(), n, k, d, _DTYPE_CODE[z.dtype], _ptr(residual), y.data_ptr(),
                                     _DTYPE_CODE[out_dtype], _stream(None)), "tardis_moe_combine")
+    return y
+
+
+# ---------------------------------------------------------------- norms, layers in 8 and 4 bits
+FP8 = torch.float8_e4m3fn
+_OUT_CODE = {torch.float32: F32, torch.bfloat16: BF16, FP8: FP8_E4M3}
+
+
+def tardis_rms_norm(x, weight=None, residual=None, eps: float = 1e-6, out_dtype=None, sum=None, y=None, scales=None, stream=None):
+    """s = x + residual -> y = s / sqrt(mean(s^2) + eps) * weight, in out_dtype (default: x's; torch.float8_e4m3fn: codes, with a scale for each row).
+
+    Returns y; (y, scales) with codes; with a residual s behind them: (y, sum), (y, scales, sum).  Rows of x may have a pitch.  sum, y, scales:
+    where to write them (sum may be the residual itself)."""
+    if stream is not None:
+        with _on(stream):
+            return tardis_rms_norm(x, weight, residual, eps, out_dtype, sum, y, scales)
+    d = x.shape[-1]
+    n, pitch = _rows(x, d)
+    dt, dev = x.dtype, x.get_device()
+    out_dtype = out_dtype or dt
+    codes = out_dtype == FP8
+    assert weight is None or (weight.is_contiguous() and weight.dtype == dt and weight.numel() == d and weight.get_device() == dev)
+    assert residual is None or (residual.is_contiguous() and residual.dtype == dt and residual.shape == (n, d) and residual.get_device() == dev)
+    assert codes or scales is None
+    if residual is not None and sum is None:
+        sum = _empty(n, d, dt, x.device)
+    elif sum is not None:
+        assert sum.is_contiguous() and sum.dtype == dt and sum.shape == (n, d) and sum.get_device() == dev
+    if y is None:
+        y = _empty(n, d, out_dtype, x.device)
+    else:
+        assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, d) and y.get_device() == dev
+    if codes and scales is None:
+        scales = torch.empty_strided((n,), (1,), dtype=torch.float32, device=x.device)
+    elif codes:
+        assert scales.is_contiguous() and scales.dtype == torch.float32 and scales.shape == (n,) and scales.get_device() == dev
+    desc = tardis_norm_desc(d, _DTYPE_CODE[dt], _OUT_CODE[out_dtype], eps, 0, None if weight is None else weight.data_ptr())
+    _check(lib().tardis_rms_norm(desc, x.data_ptr(), n, pitch, _ptr(residual), _ptr(sum), y.data_ptr(), _ptr(scales), _stream(None)), "tardis_rms_norm")
+    outs = (y, scales) if codes else (y,)
+    if residual is not None:
+        outs += (sum,)
+    return outs if len(outs) > 1 else y
+
+
+def tardis_fp8_rows(x, codes=None, scales=None, stream=None):
+    """n x d -> (e4m3 codes n x d, scales float32[n]): a row is its codes times its scale.  Rows of x may have a pitch."""
+    if stream is not None:
+        with _on(stream):
+            return tardis_fp8_rows(x, codes, scales)
+    d = x.shape[-1]
+    n, pitch = _rows(x, d)
+    dev = x.get_device()
+    if codes is None:
+        codes = _empty(n, d, FP8, x.device)
+    else:
+        assert codes.is_contiguous() and codes.dtype == FP8 and codes.shape == (n, d) and codes.get_device() == dev
+    if scales is None:
+        scales = torch.empty_strided((n,), (1,), dtype=torch.float32, device=x.device)
+    else:
+        assert scales.is_contiguous() and scales.dtype == torch.float32 and scales.shape == (n,) and scales.get_device() == dev
+    _check(lib().tardis_fp8_rows(x.data_ptr(), n, d, pitch, _DTYPE_CODE[x.dtype], codes.data_ptr(), scales.data_ptr(), _stream(None)), "tardis_fp8_rows")
+    return codes, scales
+
+
+@functools.lru_cache(maxsize=4096)
+def _fp8_work_bytes(n_in, n_out, out, act, n, pitch, x_at, W_at):
+    bytes_ = C.c_int64()
+    _check(lib().tardis_linear_fp8_workspace(tardis_linear_fp8_desc(n_in, n_out, out, act, 256 + W_at, None, None), 256 + x_at, n, pitch, bytes_),
+           "tardis_linear_fp8_workspace")
+    return bytes_.value
+
+
+@functools.lru_cache(maxsize=4096)
+def _four_work_bytes(n_in, n_out, dtype, out, act, group, n, pitch):
+    bytes_ = C.c_int64()
+    _check(lib().tardis_linear_4bit_workspace(tardis_linear_4bit_desc(n_in, n_out, dtype, out, act, group, 256, 256, None, None), n, pitch, bytes_),
+           "tardis_linear_4bit_workspace")
+    return bytes_.value
+
+
+def _layer_outputs(n, n_out, out_dtype, b, residual, y, x):
+    """The checks that layers in 8 and 4 bits share -> y"""
+    dev = x.get_device()
+    assert b is None or (b.is_contiguous() and b.dtype == out_dtype and b.numel() == n_out and b.get_device() == dev)
+    assert residual is None or (residual.is_contiguous() and residual.dtype == out_dtype and residual.shape == (n, n_out) and residual.get_device() == dev)
+    if y is None:
+        return _empty(n, n_out, out_dtype, x.device)
+    assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, n_out) and y.get_device() == dev
+    return y
+
+
+def tardis_linear_fp8(x, x_scales, W, W_scales, b=None, act: str = "identity", residual=None, out_dtype=torch.bfloat16, y=None, stream=None):
+    """-> n x n_out: act(x W^T + b) + residual with x and W in e4m3, each row with a scale (None: ones).  Rows of x may have a pitch; out_dtype: of b,
+    residual and y."""
+    if stream is not None:
+        with _on(stream):
+            return tardis_linear_fp8(x, x_scales, W, W_scales, b, act, residual, out_dtype, y)
+    n_out, n_in = W.shape
+    n, pitch = _rows(x, n_in)
+    dev = x.get_device()
+    assert W.is_contiguous() and W.dtype == FP8 and x.dtype == FP8 and W.get_device() == dev
+    assert x_scales is None or (x_scales.is_contiguous() and x_scales.dtype == torch.float32 and x_scales.numel() == n and x_scales.get_device() == dev)
+    assert W_scales is None or (W_scales.is_contiguous() and W_scales.dtype == torch.float32 and W_scales.numel() == n_out and W_scales.get_device() == dev)
+    y = _layer_outputs(n, n_out, out_dtype, b, residual, y, x)
+    out, a, x_at, W_at = _DTYPE_CODE[out_dtype], ACT[act], x.data_ptr(), W.data_ptr()
+    desc = tardis_linear_fp8_desc(n_in, n_out, out, a, W_at, None if W_scales is None else W_scales.data_ptr(), None if b is None else b.data_ptr())
+    bytes_ = _fp8_work_bytes(n_in, n_out, out, a, n, pitch, x_at & 15, W_at & 15)
+    work = torch.empty(bytes_, dtype=torch.uint8, device=x.device) if bytes_ else None
+    _check(lib().tardis_linear_fp8(desc, x_at, _ptr(x_scales), n, pitch, _ptr(residual), y.data_ptr(), _ptr(work), bytes_, _stream(None)), "tardis_linear_fp8")
+    return y
+
+
+def tardis_pack_4bit(codes, group: int):
+    """Codes n_out x n_in, 0 to 15 -> what tardis_linear_4bit reads: int32[n_out, G group / 8], G = ceil(n_in / group), on the codes' device (rows
+    are filled with zeros to whole groups).  Done once for a layer, in torch."""
+    n_out, n_in = codes.shape
+    words = torch.zeros(n_out, -(-n_in // group) * group, dtype=torch.int64, device=codes.device)
+    words[:, :n_in] = codes
+    at = torch.tensor([4 * (c // 2) + 16 * (c % 2) for c in range(8)], device=codes.device)
+    words = ((words.view(n_out, -1, 8) & 15) << at).sum(2)
+    return torch.where(words >= 1 << 31, words - (1 << 32), words).int()
+
+
+def tardis_linear_4bit(x, W, scales, zeros=None, b=None, group: int = 128, act: str = "identity", residual=None, out_dtype=None, y=None, stream=None):
+    """-> n x n_out: act(x W'^T + b) + residual, W' = scales (codes - zeros) for each group of columns.  W: tardis_pack_4bit's; scales: n_out x G,
+    dtype of x; zeros: uint8 n_out x G (None: 8).  Rows of x may have a pitch; out_dtype: of b, residual and y (default: x's)."""
+    if stream is not None:
+        with _on(stream):
+            return tardis_linear_4bit(x, W, scales, zeros, b, group, act, residual, out_dtype, y)
+    n_out, n_in = W.shape[0], x.shape[-1]
+    n, pitch = _rows(x, n_in)
+    dt, dev = x.dtype, x.get_device()
+    out_dtype = out_dtype or dt
+    assert group in (32, 64, 128)
+    groups = -(-n_in // group)
+    assert W.is_contiguous() and W.dtype == torch.int32 and W.shape == (n_out, groups * group // 8) and W.get_device() == dev
+    assert scales.is_contiguous() and scales.dtype == dt and scales.shape == (n_out, groups) and scales.get_device() == dev
+    assert zeros is None or (zeros.is_contiguous() and zeros.dtype == torch.uint8 and zeros.shape == (n_out, groups) and zeros.get_device() == dev)
+    y = _layer_outputs(n, n_out, out_dtype, b, residual, y, x)
+    sizes = (n_in, n_out, _DTYPE_CODE[dt], _DTYPE_CODE[out_dtype], ACT[act], group)
+    desc = tardis_linear_4bit_desc(*sizes, W.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), None if b is None else b.data_ptr())
+    bytes_ = _four_work_bytes(*sizes, n, pitch)
+    work = torch.empty(bytes_, dtype=torch.uint8, device=x.device) if bytes_ else None
+    _check(lib().tardis_linear_4bit(desc, x.data_ptr(), n, pitch, _ptr(residual), y.data_ptr(), _ptr(work), bytes_, _stream(None)), "tardis_linear_4bit")
     return y
