@@ -27,6 +27,8 @@ struct e4m3_near_t { uint8_t code; };             // multiplied by the faster in
 constexpr int kActGelu16 = 4;                     // behind tardis_act_t's: GELU for outputs in bf16 without a residual
 constexpr uint32_t kNowhere = 0xe0000000u;        // an offset past the end of any operand that is loaded by offsets
 
+struct four_t { uint8_t codes; };                  // 4-bit weights (linear_4bit.hip)
+
 // The tiles: rows, columns and bytes of K in a slice (64 or 128 for each of the wavefronts that divide it)
 struct LinearShape { int m, n, slice; };
 constexpr LinearShape kLinearShape[] = {{16, 16, 512}, {16, 32, 512}, {16, 64, 512}, {32, 32, 256}, {32, 64, 256}, {64, 32, 256},
@@ -54,6 +56,8 @@ constexpr LinearShape kLinearQuad[] = {{256, 256, 128}, {192, 256, 128}, {256, 1
 constexpr int linear_least_rows(int m) { return m == 256 ? 192 : m; }
 constexpr int kLinearQuads = sizeof(kLinearQuad) / sizeof(LinearShape);
 
+// sums of ranges and the epilogue, with a bias of y's type (scales: as above)
+void td_linear_join(const LinearArgs& p, hipStream_t s);
 tardis_status_t td_linear_init_quad();
 void td_linear_launch_quad(const LinearArgs& p, bool grouped, int shape, int blocks, hipStream_t s);
 tardis_status_t td_linear_init_bf16();

@@ -87,6 +87,11 @@ __global__ void __launch_bounds__(256) linear_join_kernel(LinearArgs p, uint32_t
     }
 }
 
+template <typename T> void join(const LinearArgs& p, hipStream_t s) {
+    const int64_t units = (p.N + 3) / 4;
+    hipLaunchKernelGGL(linear_join_kernel<T>, dim3((unsigned)((units * p.n + 255) / 256)), dim3(256), 0, s, p, (uint32_t)units);
+}
+
 // ---------------------------------------------------------------- how a call is done
 // What a tile takes, in us:
 //     max(fixed x turns + slices x max(alone x turns, slice x tiles of a CU), 1.5 + bytes / tbs)
@@ -284,11 +289,9 @@ tardis_status_t run(LinearArgs p, const Call& c, void* work, int64_t work_bytes,
     else td_linear_launch_bf16(q, grouped, plan.direct, plan.shape, blocks, s);
     if (plan.splits > 1) {
         p.part = q.part;
-        const int64_t units = (p.N + 3) / 4;
-        const dim3 grid((unsigned)((units * p.n + 255) / 256));
-        if (fp8) hipLaunchKernelGGL(linear_join_kernel<e4m3_t>, grid, dim3(256), 0, s, p, (uint32_t)units);
-        else if (f32) hipLaunchKernelGGL(linear_join_kernel<float>, grid, dim3(256), 0, s, p, (uint32_t)units);
-        else hipLaunchKernelGGL(linear_join_kernel<bf16_t>, grid, dim3(256), 0, s, p, (uint32_t)units);
+        if (fp8) td_linear_join(p, s);
+        else if (f32) join<float>(p, s);
+        else join<bf16_t>(p, s);
     }
     TD_HIP(hipGetLastError());
     return TARDIS_OK;
@@ -322,6 +325,8 @@ Call call_of(const tardis_linear_fp8_desc* d, const void* x, int64_t n, int64_t 
 constexpr int64_t kAnyRoom = (int64_t)1 << 62;
 
 }  // namespace
+
+void td_linear_join(const LinearArgs& p, hipStream_t s) { join<e4m3_t>(p, s); }
 
 tardis_status_t td_linear_work_bytes(const tardis_linear_desc* d, int64_t experts, const void* x, int64_t x_rows, int64_t x_pitch, bool gather, int64_t rows,
                                      int64_t* bytes) {

@@ -6,12 +6,10 @@
 // the sum.  Tokens in fp32 are three bf16 parts each, which together hold all of their 24 bits.
 #include <algorithm>
 
-#include "linear_act.h"
+#include "linear_tile.h"
 
 namespace {
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-typedef uint32_t u32x4_any_t __attribute__((ext_vector_type(4), aligned(2)));
 template <int N> struct words_of { typedef uint32_t type __attribute__((ext_vector_type(N))); };
 template <> struct words_of<1> { typedef uint32_t type; };
 
@@ -201,6 +199,210 @@ __global__ void __launch_bounds__(64 * kWaves, 2) linear4_kernel(FourArgs p) {
     }
 }
 
+// ---------------------------------------------------------------- many tokens
+// Tokens as the tiles read them: PARTS parts in bf16, rows of whole steps with zeros behind the last column, and the sums of every group, [group][token].
+constexpr int kStep = 128;                          // columns of a step
+struct FourTokens {
+    const unsigned char* x;
+    td_u32x4* parts;                               // [part][token][units]
+    float* sums;
+    int64_t n, x_pitch;
+    uint32_t k, units;                             // columns; pieces of 8 of a row, in whole steps
+};
+template <typename T, int GW>
+__global__ void __launch_bounds__(256) linear4_tokens_kernel(FourTokens p) {
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / p.units;
+    const uint32_t unit = (uint32_t)(u - row * p.units);
+    if (row >= p.n) return;                        // (rows are whole groups: no group is divided)
+    const unsigned char* at = p.x + row * p.x_pitch + (size_t)unit * 8 * sizeof(T);
+    const int left = (int)p.k - (int)unit * 8;
+    Token<T> t;
+    float v[8];
+    if (left >= 8) load_token<T>(t, at);
+    else load_token_end<T>(t, at, left);
+    double sum = 0.0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) v[q] = q < left ? td_load<T>(reinterpret_cast<const T*>(at) + q) : 0.0f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) sum += (double)v[q];
+#pragma unroll
+    for (int o = 1; o < 4 * GW; o *= 2) sum += __shfl_xor(sum, o, 64);
+    if (unit % (4 * GW) == 0) p.sums[(int64_t)(unit / (4 * GW)) * p.n + row] = (float)sum;
+#pragma unroll
+    for (int i = 0; i < Token<T>::PARTS; ++i) p.parts[((int64_t)i * p.n + row) * p.units + unit] = t.part[i];
+}
+
+struct FourTile : LinearArgs {                     // (x: the parts; k: bytes of a row of theirs)
+    const void* scales;
+    const uint8_t* zeros;
+    const float* sums;
+    uint32_t groups;
+    int scales_f32;
+};
+
+template <int FA, int FB, int WM, int WN, int GROUPS> struct FourTileShape {
+    static constexpr int W = WM * WN, TM = 16 * FA * WM, TN = 16 * FB * WN, G = GROUPS, SLOT = TM * 2 * kStep;
+    static constexpr int kLds = 2 * SLOT + 2 * G * (TM * 4 + TN * 8), kRowBytes = W * 16 * FB * 16 * 4;
+    static constexpr int RB = FA * kRowBytes <= kLds ? FA : FA % 2 == 0 && 2 * kRowBytes <= kLds ? 2 : 1;   // row blocks behind the products
+    static_assert(SLOT % (1024 * W) == 0 && RB * kRowBytes <= kLds && TM * G <= 64 * W && (64 * W) % G == 0 && kLds <= kLdsBytes, "slots");
+};
+
+// A tile of TM = 16 FA WM tokens x TN = 16 FB WN rows of W: a step of 128 columns of the tokens goes to LDS, of which there are two; codes go
+// from memory to registers, scales and zero points by way of registers to LDS, a step ahead.  A wavefront makes the codes of 16 rows into bf16 and
+// multiplies them with all of its tokens, group by group: a group's sum begins with -(16 + zero) times the sum of the token's columns, and is added to
+// the result with the group's scale.
+template <int PARTS, int GW, bool ZEROS, int FA, int FB, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, 2) linear4_tile_kernel(FourTile p) {
+    typedef typename words_of<GW>::type words_t;
+    typedef FourTileShape<FA, FB, WM, WN, 4 / GW> S;
+    constexpr int W = S::W, TM = S::TM, TN = S::TN, G = S::G, SLOT = S::SLOT, LA = SLOT / (1024 * W), PER = (TN * G + 64 * W - 1) / (64 * W);
+    extern __shared__ __align__(1024) unsigned char lds[];
+    float* sums = reinterpret_cast<float*>(lds + 2 * SLOT);                   // [2][G][TM]
+    f32x2_t* scales = reinterpret_cast<f32x2_t*>(sums + 2 * G * TM);          // [2][G][TN]: scale, -(16 + zero)
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wn = wave % WN, wm = wave / WN, low = lane & 15, high = lane >> 4;
+    uint32_t t, in_range;
+    if (!number_of(blockIdx.x, (uint32_t)(p.tiles_m * p.tiles_n * p.splits), t)) return;
+    LinearBlock b;
+    int tile_m, tile_n;
+    const int steps = (int)(p.k / (2 * kStep));
+    b.range = uniform((int)divide(t, (uint32_t)(p.tiles_m * p.tiles_n), in_range));
+    tile_of(in_range, (uint32_t)p.tiles_m, (uint32_t)p.tiles_n, tile_m, tile_n);
+    b.expert = 0;
+    b.first = (int64_t)tile_m * TM;
+    b.rows = (int)min((int64_t)TM, p.n - b.first);
+    b.s0 = b.range * p.slices;
+    b.nk = max(0, min(p.slices, steps - b.s0));
+    b.n0 = (int64_t)tile_n * TN;
+    const int rows_w = (int)min((int64_t)TN, p.N - b.n0);
+
+    // tokens: a load is 4 rows of 256 bytes, lane -> row lane / 16, slot lane % 16, which holds piece slot ^ row
+    const uint32_t base = (uint32_t)uniform((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds);
+    uint32_t off[LA];
+#pragma unroll
+    for (int i = 0; i < LA; ++i) {
+        const int row = wave * (TM / W) + 4 * i + high;
+        off[i] = (row < b.rows ? (uint32_t)row * p.k : kNowhere) + (uint32_t)((low ^ (row & 15)) * 16);
+        asm volatile("" : "+v"(off[i]));
+    }
+    auto load_tokens = [&](int step, int part, uint32_t slot) {
+        const i32x4_t rx = buffer_of(p.x + ((int64_t)part * p.n + b.first) * p.k, (uint32_t)b.rows * p.k);
+#pragma unroll
+        for (int i = 0; i < LA; ++i) load_to_lds(base + slot * SLOT + (uint32_t)wave * (SLOT / W) + i * 1024u, off[i], rx, (uint32_t)step * (2 * kStep));
+    };
+    // (rows and groups of W that are not there: the last one's; the tokens have zeros there, and nothing is kept of the rows)
+    const unsigned char* weights = p.W + b.n0 * ((int64_t)p.groups * (16 * GW));
+    uint32_t row_at[FB];
+#pragma unroll
+    for (int j = 0; j < FB; ++j) row_at[j] = (uint32_t)min((wn * FB + j) * 16 + low, rows_w - 1) * (p.groups * (16u * GW)) + (uint32_t)high * (4 * GW);
+    struct Words {
+        words_t w[FB][G];
+    };
+    auto load_words = [&](Words& v, int step) {
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            const uint32_t group = min((uint32_t)(step * G + g), p.groups - 1);
+#pragma unroll
+            for (int j = 0; j < FB; ++j) v.w[j][g] = *reinterpret_cast<const words_t*>(weights + (row_at[j] + group * (16u * GW)));
+        }
+    };
+    // a thread's scales: row tid / G + u 64 W / G, group tid % G of the step
+    struct Scales {
+        float scale[PER];
+        uint32_t zero[PER];
+        float sum;
+    };
+    const int sum_group = tid / TM, sum_row = tid % TM;
+    auto load_scales = [&](Scales& v, int step) {
+        const uint32_t group = min((uint32_t)(step * G + tid % G), p.groups - 1);
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            const int64_t at = (b.n0 + min(tid / G + u * (64 * W / G), rows_w - 1)) * p.groups + group;
+            v.scale[u] = p.scales_f32 ? static_cast<const float*>(p.scales)[at] : td_load<bf16_t>(static_cast<const bf16_t*>(p.scales) + at);
+            if constexpr (ZEROS) v.zero[u] = p.zeros[at];
+        }
+        v.sum = sum_group < G && sum_row < b.rows ? p.sums[(int64_t)(step * G + sum_group) * p.n + b.first + sum_row] : 0.0f;
+    };
+    auto store_scales = [&](const Scales& v, int slot) {
+#pragma unroll
+        for (int u = 0; u < PER; ++u)
+            if (tid / G + u * (64 * W / G) < TN) scales[(slot * G + tid % G) * TN + tid / G + u * (64 * W / G)] = f32x2_t{v.scale[u], ZEROS ? -16.0f - (float)min(v.zero[u], 128u) : 0.0f};
+        if (sum_group < G) sums[(slot * G + sum_group) * TM + sum_row] = v.sum;
+    };
+    f32x4_t acc[FA][FB];
+#pragma unroll
+    for (int i = 0; i < FA; ++i)
+#pragma unroll
+        for (int j = 0; j < FB; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
+    auto products = [&](const Words& v, uint32_t slot, int scale_slot, bool first_part) {
+        const unsigned char* from = lds + slot * SLOT + (wm * 16 + low) * (2 * kStep);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            td_u32x4 x[FA][GW];
+            f32x4_t sum[FA];
+#pragma unroll
+            for (int i = 0; i < FA; ++i) {
+#pragma unroll
+                for (int s = 0; s < GW; ++s)
+                    x[i][s] = *reinterpret_cast<const td_u32x4*>(from + i * WM * 16 * (2 * kStep) + (((g * (4 * GW) + high * GW + s) ^ low) * 16));
+                sum[i] = *reinterpret_cast<const f32x4_t*>(sums + (scale_slot * G + g) * TM + (WM * i + wm) * 16 + 4 * high);
+                if (!ZEROS) sum[i] *= -24.0f;
+                if (PARTS > 1 && !first_part) sum[i] = f32x4_t{0, 0, 0, 0};
+            }
+#pragma unroll
+            for (int j = 0; j < FB; ++j) {
+                f32x4_t c[FA];
+                const f32x2_t scale = scales[(scale_slot * G + g) * TN + (wn * FB + j) * 16 + low];
+#pragma unroll
+                for (int i = 0; i < FA; ++i) c[i] = ZEROS ? sum[i] * scale[1] : sum[i];
+#pragma unroll
+                for (int s = 0; s < GW; ++s) {
+                    uint32_t word;
+                    if constexpr (GW == 1) word = v.w[j][g];
+                    else word = v.w[j][g][s];
+                    const td_u32x4 codes = sixteen_more(word);
+#pragma unroll
+                    for (int i = 0; i < FA; ++i) c[i] = mma(x[i][s], codes, c[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < FA; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[i][j][q] = fmaf(scale[0], c[i][q], acc[i][j][q]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+    Words now, next;
+    Scales coming;
+    if (b.nk > 0) {
+        load_tokens(b.s0, 0, 0);
+        load_words(next, b.s0);
+        load_scales(coming, b.s0);
+    }
+    uint32_t slot = 0;
+#pragma unroll 1
+    for (int at = 0; at < b.nk; ++at) {
+        const bool more = at + 1 < b.nk;
+        now = next;
+        store_scales(coming, at & 1);
+#pragma unroll 1
+        for (int part = 0; part < PARTS; ++part) {
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (part + 1 < PARTS) load_tokens(b.s0 + at, part + 1, slot ^ 1);
+            else if (more) load_tokens(b.s0 + at + 1, 0, slot ^ 1);
+            if (part == 0 && more) {
+                load_words(next, b.s0 + at + 1);
+                load_scales(coming, b.s0 + at + 1);
+            }
+            products(now, slot, at & 1, part == 0);
+            slot ^= 1;
+        }
+    }
+    __syncthreads();
+    finish_linear<four_t, false, W, FA, FB, WM, WN, 1, S::RB, true>(p, b, acc, lds, tid);
+}
+
 template <typename T, int GW> void launch(const FourArgs& p, int tokens, dim3 grid, hipStream_t s) {
     const dim3 block(64 * kWaves);
     if (tokens == 1) hipLaunchKernelGGL((linear4_kernel<T, GW, 1>), grid, block, 0, s, p);
@@ -213,15 +415,136 @@ template <typename T> void launch(const FourArgs& p, int group, int tokens, dim3
     else launch<T, 4>(p, tokens, grid, s);
 }
 
+
+// f(group words, zeros, token blocks of a wavefront, row blocks, grid of wavefronts)
+template <typename F> void for_four_tile(int group, bool zeros, int shape, F f) {
+    auto with_tile = [&](auto gw, auto z) {
+        if (shape == 0) f(gw, z, num<2>{}, num<4>{}, num<2>{}, num<4>{});
+        else f(gw, z, num<4>{}, num<4>{}, num<2>{}, num<4>{});
+    };
+    auto with_zeros = [&](auto gw) {
+        if (zeros) with_tile(gw, std::true_type{});
+        else with_tile(gw, std::false_type{});
+    };
+    if (group == 32) with_zeros(num<1>{});
+    else if (group == 64) with_zeros(num<2>{});
+    else with_zeros(num<4>{});
+}
+
+tardis_status_t init_tiles() {
+    static td_once once;
+    return once.run([]() -> tardis_status_t {
+        bool ok = true;
+        for (int group = 32; group <= 128; group *= 2)
+            for (int zeros = 0; zeros < 2; ++zeros)
+                for (int shape = 0; shape < 2; ++shape)
+                    for_four_tile(group, zeros, shape, [&](auto gw, auto z, auto fa, auto fb, auto wm, auto wn) {
+                        constexpr int bytes = FourTileShape<fa, fb, wm, wn, 4 / gw>::kLds;
+                        ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(linear4_tile_kernel<1, gw, decltype(z)::value, fa, fb, wm, wn>),
+                                                  hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
+                        ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(linear4_tile_kernel<3, gw, decltype(z)::value, fa, fb, wm, wn>),
+                                                  hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
+                    });
+        return ok ? TARDIS_OK : TARDIS_ERR_HIP;
+    });
+}
+
+// How a call is done, by its sizes and the working memory that it has
+struct FourPlan {
+    bool tiles;
+    int shape, splits, slices, tm, tn;
+    int64_t n_parts, units, at_sums, at_part, work;
+};
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+FourPlan plan_four(const tardis_linear_4bit_desc* d, int64_t n, int64_t room) {
+    FourPlan p{};
+    if (n <= 64) return p;
+    p.shape = d->dtype == TARDIS_F32 || n <= 64 ? 0 : 1;
+    p.tm = p.shape == 0 ? 64 : 128;
+    p.tn = 256;
+    p.n_parts = d->dtype == TARDIS_F32 ? 3 : 1;
+    const int64_t steps = (d->n_in + kStep - 1) / kStep, tiles = ((n + p.tm - 1) / p.tm) * ((d->n_out + p.tn - 1) / p.tn);
+    p.units = steps * (kStep / 8);
+    p.at_sums = round_up(p.n_parts * n * p.units * 16, 256);
+    p.at_part = p.at_sums + round_up(steps * (kStep / d->group) * n * 4, 256);
+    if (tiles >= 1 << 21 || p.units * 16 * p.tm >= kNowhere || n * p.units >= kMostThreads || p.at_part > room) return FourPlan{};
+    p.splits = 1;
+    while (p.splits < 16 && tiles * p.splits * 2 <= 256 && steps >= 4 * p.splits * 2 && p.at_part + 2 * p.splits * n * d->n_out * 4 <= room) p.splits *= 2;
+    p.slices = (int)((steps + p.splits - 1) / p.splits);
+    p.work = p.at_part + (p.splits > 1 ? p.splits * n * d->n_out * 4 : 0);
+    p.tiles = true;
+    return p;
+}
+
+tardis_status_t run_tiles(const tardis_linear_4bit_desc* d, const FourPlan& plan, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y,
+                          unsigned char* work, hipStream_t s) {
+    TD_TRY(init_tiles());
+    const bool f32 = d->dtype == TARDIS_F32;
+    FourTokens t{};
+    t.x = static_cast<const unsigned char*>(x);
+    t.parts = reinterpret_cast<td_u32x4*>(work);
+    t.sums = reinterpret_cast<float*>(work + plan.at_sums);
+    t.n = n;
+    t.x_pitch = x_pitch * (int64_t)td_elem_size(d->dtype);
+    t.k = (uint32_t)d->n_in;
+    t.units = (uint32_t)plan.units;
+    FourTile p{};
+    p.x = work;
+    p.W = reinterpret_cast<const unsigned char*>(d->W);
+    p.b = d->b;
+    p.r = residual;
+    p.y = y;
+    p.n = p.x_rows = n;
+    p.N = d->n_out;
+    p.k = (uint32_t)(plan.units * 16);
+    p.act = d->act == TARDIS_ACT_GELU_ERF && d->out_dtype == TARDIS_BF16 && !residual ? kActGelu16 : d->act;
+    p.out_f32 = d->out_dtype == TARDIS_F32;
+    p.tiles_m = (int)((n + plan.tm - 1) / plan.tm);
+    p.tiles_n = (int)((d->n_out + plan.tn - 1) / plan.tn);
+    p.splits = plan.splits;
+    p.slices = plan.slices;
+    p.scales = d->scales;
+    p.zeros = d->zeros;
+    p.sums = t.sums;
+    p.groups = (uint32_t)((d->n_in + d->group - 1) / d->group);
+    p.scales_f32 = f32;
+    FourTile q = p;
+    if (plan.splits > 1) {
+        q.part = reinterpret_cast<float*>(work + plan.at_part);
+        q.act = TARDIS_ACT_IDENTITY;
+    }
+    const dim3 token_grid((unsigned)((n * plan.units + 255) / 256));
+    const int blocks = (int)(((int64_t)p.tiles_m * p.tiles_n * p.splits + 7) / 8 * 8);
+    for_four_tile(d->group, d->zeros != nullptr, plan.shape, [&](auto gw, auto z, auto fa, auto fb, auto wm, auto wn) {
+        constexpr int bytes = FourTileShape<fa, fb, wm, wn, 4 / gw>::kLds, threads = 64 * wm * wn;
+        if (f32) {
+            hipLaunchKernelGGL((linear4_tokens_kernel<float, gw>), token_grid, dim3(256), 0, s, t);
+            hipLaunchKernelGGL((linear4_tile_kernel<3, gw, decltype(z)::value, fa, fb, wm, wn>), dim3((unsigned)blocks), dim3(threads), bytes, s, q);
+        } else {
+            hipLaunchKernelGGL((linear4_tokens_kernel<bf16_t, gw>), token_grid, dim3(256), 0, s, t);
+            hipLaunchKernelGGL((linear4_tile_kernel<1, gw, decltype(z)::value, fa, fb, wm, wn>), dim3((unsigned)blocks), dim3(threads), bytes, s, q);
+        }
+    });
+    if (plan.splits > 1) {
+        p.part = q.part;
+        td_linear_join(p, s);
+    }
+    TD_HIP(hipGetLastError());
+    return TARDIS_OK;
+}
+
 }  // namespace
 
 tardis_status_t td_linear_4bit_work_bytes(const tardis_linear_4bit_desc* d, int64_t n, int64_t x_pitch, int64_t* bytes) {
-    *bytes = 0;
+    *bytes = plan_four(d, n, (int64_t)1 << 62).work;
     return TARDIS_OK;
 }
 
 tardis_status_t td_linear_4bit(const tardis_linear_4bit_desc* d, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y, void* work,
                                int64_t work_bytes, hipStream_t s) {
+    const FourPlan plan = plan_four(d, n, work_bytes);
+    if (plan.tiles) return run_tiles(d, plan, x, n, x_pitch, residual, y, static_cast<unsigned char*>(work), s);
     FourArgs p{};
     const int64_t es = (int64_t)td_elem_size(d->dtype), eo = (int64_t)td_elem_size(d->out_dtype);
     p.x = static_cast<const unsigned char*>(x);

@@ -221,7 +221,8 @@ template <bool GROUPED> __device__ __forceinline__ int64_t token_of_row(const Li
 // Loads and stores are counted by one counter, in their order: a load in the loop would wait for the stores of the turn before, 1.5 us each
 // (behind the products of a 256 x 256 tile with GELU 21.4 us, as here 15.6, of which the activation's instructions are 8.5).  So which rows are
 // there is known before the first store, bias is waited for there, and residuals are loaded for several rows at once, in a loop of their own.
-template <typename T, bool GROUPED, int W, int FA, int FB, int WM, int WN, int WK, int RB>
+// ACROSS: acc[i][j][q] = row (WM i + wm) 16 + 4 (lane / 16) + q, column (wn FB + j) 16 + lane % 16.
+template <typename T, bool GROUPED, int W, int FA, int FB, int WM, int WN, int WK, int RB, bool ACROSS = false>
 __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearBlock& b, f32x4_t (&acc)[FA][FB], unsigned char* lds, int tid) {
     static_assert(FA % RB == 0, "all row blocks");
     constexpr bool OWN = WK == 1;
@@ -263,8 +264,8 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
         const uint32_t as_f32 = w[q / 4][q % 4], pair = w[0][q / 2];
         return __uint_as_float(f32 ? as_f32 : q & 1 ? pair & 0xffff0000u : pair << 16);
     };
-    constexpr bool SCALED = sizeof(T) == 1;
-    const bool bias_f32 = SCALED ? p.out_f32 != 0 : sizeof(T) == 4;
+    constexpr bool SCALED = std::is_same_v<T, e4m3_t> || std::is_same_v<T, e4m3_near_t>;
+    const bool bias_f32 = sizeof(T) == 1 ? p.out_f32 != 0 : sizeof(T) == 4;
     float bias[8] = {};
     if (p.b && !p.part && columns > 0) {
         td_u32x4 w[2];
@@ -314,7 +315,12 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
         for (int i = 0; i < RB; ++i)
 #pragma unroll
             for (int j = 0; j < FB; ++j)
-                *reinterpret_cast<f32x4_t*>(stage + place_of(wk, ((OWN ? 0 : wm * RB) + i) * 16 + frow, ((OWN ? 0 : wn * FB) + j) * 4 + fp)) = SCALED ? acc[i0 + i][j] * token_scale[i0 + i] : acc[i0 + i][j];
+                if constexpr (ACROSS) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        stage[place_of(wk, ((OWN ? 0 : wm * RB) + i) * 16 + 4 * fp + q, ((OWN ? 0 : wn * FB) + j) * 4 + frow / 4) + frow % 4] = acc[i0 + i][j][q];
+                } else
+                    *reinterpret_cast<f32x4_t*>(stage + place_of(wk, ((OWN ? 0 : wm * RB) + i) * 16 + frow, ((OWN ? 0 : wn * FB) + j) * 4 + fp)) = SCALED ? acc[i0 + i][j] * token_scale[i0 + i] : acc[i0 + i][j];
         sync();
         // (sums of a range of K: act is the identity, without bias and residual)
         with_linear_act(p.act, [&](auto act) {
