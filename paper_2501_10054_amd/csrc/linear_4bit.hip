@@ -31,10 +31,14 @@ __device__ __forceinline__ f32x4_t mma(const td_u32x4& w, const td_u32x4& x, con
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, w), __builtin_bit_cast(bf16x8_t, x), c, 0, 0, 0);
 }
 
-// 16 + q of the eight codes of a word, in bf16
-__device__ __forceinline__ td_u32x4 sixteen_more(uint32_t w) {
-    return {(w << 3 & 0x00780078u) | 0x41804180u, (w >> 1 & 0x00780078u) | 0x41804180u, (w >> 5 & 0x00780078u) | 0x41804180u, (w >> 9 & 0x00780078u) | 0x41804180u};
-}
+// 16 + q of the eight codes of a word, in bf16.  (Both constants in registers: an instruction has room for one, and takes two steps with literals)
+struct Sixteen {
+    uint32_t mask = 0x00780078u, exponent = 0x41804180u;
+    __device__ __forceinline__ Sixteen() { asm("" : "+v"(mask), "+v"(exponent)); }
+    __device__ __forceinline__ td_u32x4 more(uint32_t w) const {
+        return {(w << 3 & mask) | exponent, (w >> 1 & mask) | exponent, (w >> 5 & mask) | exponent, (w >> 9 & mask) | exponent};
+    }
+};
 // -(16 + z), twice in a word
 __device__ __forceinline__ uint32_t sixteen_less(uint32_t z) {
     return (__float_as_uint(-16.0f - (float)min(z, 128u)) >> 16) * 0x10001u;
@@ -92,6 +96,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) linear4_kernel(FourArgs p) {
     __shared__ f32x4_t sums[kWaves * TT * 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), low = lane & 15, high = lane >> 4;
     const int tile_n = (int)(blockIdx.x % (uint32_t)p.tiles_n), rest = (int)(blockIdx.x / (uint32_t)p.tiles_n), range = rest % p.splits, tile_m = rest / p.splits;
+    const Sixteen sixteen;
     const int64_t n0 = (int64_t)tile_n * 16, m0 = (int64_t)tile_m * (16 * TT);
     // (rows and tokens that are not there: the last one's, of which nothing is kept)
     const int64_t row = min(n0 + low, p.N - 1);
@@ -117,7 +122,7 @@ __global__ void __launch_bounds__(64 * kWaves, 2) linear4_kernel(FourArgs p) {
             uint32_t word;
             if constexpr (GW == 1) word = w;
             else word = w[s];
-            const td_u32x4 codes = sixteen_more(word);
+            const td_u32x4 codes = sixteen.more(word);
 #pragma unroll
             for (int t = 0; t < TT; ++t) {
                 Token<T> v;
@@ -200,66 +205,87 @@ __global__ void __launch_bounds__(64 * kWaves, 2) linear4_kernel(FourArgs p) {
 }
 
 // ---------------------------------------------------------------- many tokens
-// Tokens as the tiles read them: PARTS parts in bf16, rows of whole steps with zeros behind the last column, and the sums of every group, [group][token].
 constexpr int kStep = 128;                          // columns of a step
+// What the tiles read beside the codes, made by one launch before theirs:
+//   tokens  PARTS parts in bf16, [part][token][units], zeros behind the last column
+//   sums    of every group's columns, [group][sum_pitch]
+//   table   of W's scales and zero points, [group][table_pitch] rows: scale and -(16 + zero), in bf16 side by side (of tokens in bf16) or in fp32
+// Groups are as many as whole steps have, those behind the last with scales of 0.
 struct FourTokens {
     const unsigned char* x;
-    td_u32x4* parts;                               // [part][token][units]
+    const void* scales;
+    const uint8_t* zeros;
+    td_u32x4* parts;
     float* sums;
-    int64_t n, x_pitch;
-    uint32_t k, units;                             // columns; pieces of 8 of a row, in whole steps
+    unsigned char* table;
+    int64_t n, N, x_pitch, sum_pitch, table_pitch;
+    uint32_t k, units, groups, all_groups, token_blocks;   // columns; pieces of 8 of a row in whole steps
 };
 template <typename T, int GW>
-__global__ void __launch_bounds__(256) linear4_tokens_kernel(FourTokens p) {
+__global__ void __launch_bounds__(256) linear4_prepare_kernel(FourTokens p) {
+    if (blockIdx.x >= p.token_blocks) {
+        const int64_t i = (int64_t)(blockIdx.x - p.token_blocks) * 256 + threadIdx.x;
+        const uint32_t group = (uint32_t)(i / p.table_pitch);
+        const int64_t row = i - group * p.table_pitch;
+        if (group >= p.all_groups) return;
+        float scale = 0.0f;
+        uint32_t zero = 8;
+        if (row < p.N && group < p.groups) {
+            scale = td_load<T>(static_cast<const T*>(p.scales) + row * p.groups + group);
+            if (p.zeros) zero = min((uint32_t)p.zeros[row * p.groups + group], 128u);
+        }
+        const float less = -16.0f - (float)zero;
+        if constexpr (sizeof(T) == 2) reinterpret_cast<uint32_t*>(p.table)[i] = __float_as_uint(scale) | __float_as_uint(less) >> 16;
+        else reinterpret_cast<f32x2_t*>(p.table)[i] = f32x2_t{scale, less};
+        return;
+    }
     const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / p.units;
     const uint32_t unit = (uint32_t)(u - row * p.units);
     if (row >= p.n) return;                        // (rows are whole groups: no group is divided)
     const unsigned char* at = p.x + row * p.x_pitch + (size_t)unit * 8 * sizeof(T);
     const int left = (int)p.k - (int)unit * 8;
     Token<T> t;
-    float v[8];
     if (left >= 8) load_token<T>(t, at);
     else load_token_end<T>(t, at, left);
     double sum = 0.0;
 #pragma unroll
-    for (int q = 0; q < 8; ++q) v[q] = q < left ? td_load<T>(reinterpret_cast<const T*>(at) + q) : 0.0f;
+    for (int i = 0; i < Token<T>::PARTS; ++i)
 #pragma unroll
-    for (int q = 0; q < 8; ++q) sum += (double)v[q];
+        for (int q = 0; q < 4; ++q) sum += (double)__uint_as_float(t.part[i][q] << 16) + (double)__uint_as_float(t.part[i][q] & 0xffff0000u);
 #pragma unroll
     for (int o = 1; o < 4 * GW; o *= 2) sum += __shfl_xor(sum, o, 64);
-    if (unit % (4 * GW) == 0) p.sums[(int64_t)(unit / (4 * GW)) * p.n + row] = (float)sum;
+    if (unit % (4 * GW) == 0) p.sums[(int64_t)(unit / (4 * GW)) * p.sum_pitch + row] = (float)sum;
 #pragma unroll
     for (int i = 0; i < Token<T>::PARTS; ++i) p.parts[((int64_t)i * p.n + row) * p.units + unit] = t.part[i];
 }
 
 struct FourTile : LinearArgs {                     // (x: the parts; k: bytes of a row of theirs)
-    const void* scales;
-    const uint8_t* zeros;
     const float* sums;
+    const unsigned char* table;
+    int64_t sum_pitch, table_pitch;
     uint32_t groups;
-    int scales_f32;
 };
 
-template <int FA, int FB, int WM, int WN, int GROUPS> struct FourTileShape {
-    static constexpr int W = WM * WN, TM = 16 * FA * WM, TN = 16 * FB * WN, G = GROUPS, SLOT = TM * 2 * kStep;
-    static constexpr int kLds = 2 * SLOT + 2 * G * (TM * 4 + TN * 8), kRowBytes = W * 16 * FB * 16 * 4;
+template <int PARTS, int GW, int FA, int FB, int WN> struct FourTileShape {
+    static constexpr int TM = 16 * FA, TN = 16 * FB * WN, G = 4 / GW;
+    static constexpr int X = TM * 2 * kStep, CODES = TN * kStep / 2, ROW = PARTS == 1 ? 4 : 8, TABLE = G * TN * ROW, SUMS = 1024;
+    static constexpr int kLds = 2 * (X + CODES + TABLE + SUMS), kRowBytes = WN * 16 * FB * 16 * 4;
     static constexpr int RB = FA * kRowBytes <= kLds ? FA : FA % 2 == 0 && 2 * kRowBytes <= kLds ? 2 : 1;   // row blocks behind the products
-    static_assert(SLOT % (1024 * W) == 0 && RB * kRowBytes <= kLds && TM * G <= 64 * W && (64 * W) % G == 0 && kLds <= kLdsBytes, "slots");
+    static_assert(X % (1024 * WN) == 0 && CODES % (1024 * WN) == 0 && TABLE % 1024 == 0 && RB * kRowBytes <= kLds && G * TM * 4 <= SUMS && kLds <= kLdsBytes, "slots");
 };
 
-// A tile of TM = 16 FA WM tokens x TN = 16 FB WN rows of W: a step of 128 columns of the tokens goes to LDS, of which there are two; codes go
-// from memory to registers, scales and zero points by way of registers to LDS, a step ahead.  A wavefront makes the codes of 16 rows into bf16 and
-// multiplies them with all of its tokens, group by group: a group's sum begins with -(16 + zero) times the sum of the token's columns, and is added to
-// the result with the group's scale.
-template <int PARTS, int GW, bool ZEROS, int FA, int FB, int WM, int WN>
-__global__ void __launch_bounds__(64 * WM * WN, 2) linear4_tile_kernel(FourTile p) {
+// A tile of TM = 16 FA tokens x TN = 16 FB WN rows of W.  A step of 128 columns - tokens, codes, table, sums - goes to LDS, which has room for two, and two blocks
+// are on a CU: while one waits for its step the other multiplies.  A wavefront has 16 FB rows to itself, makes the codes of 16 of them into bf16
+// and multiplies them with all tokens, group by group: a group's sum begins with -(16 + zero) times the sum of the token's columns, and is
+// added to the result with the group's scale.
+template <int PARTS, int GW, int FA, int FB, int WN>
+__global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
     typedef typename words_of<GW>::type words_t;
-    typedef FourTileShape<FA, FB, WM, WN, 4 / GW> S;
-    constexpr int W = S::W, TM = S::TM, TN = S::TN, G = S::G, SLOT = S::SLOT, LA = SLOT / (1024 * W), PER = (TN * G + 64 * W - 1) / (64 * W);
+    typedef FourTileShape<PARTS, GW, FA, FB, WN> S;
+    constexpr int TM = S::TM, TN = S::TN, G = S::G, LX = S::X / (1024 * WN), LC = S::CODES / (1024 * WN), LT = S::TABLE / 1024;
     extern __shared__ __align__(1024) unsigned char lds[];
-    float* sums = reinterpret_cast<float*>(lds + 2 * SLOT);                   // [2][G][TM]
-    f32x2_t* scales = reinterpret_cast<f32x2_t*>(sums + 2 * G * TM);          // [2][G][TN]: scale, -(16 + zero)
-    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), wn = wave % WN, wm = wave / WN, low = lane & 15, high = lane >> 4;
+    unsigned char *at_x = lds, *at_codes = at_x + 2 * S::X, *at_table = at_codes + 2 * S::CODES, *at_sums = at_table + 2 * S::TABLE;
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), low = lane & 15, high = lane >> 4;
     uint32_t t, in_range;
     if (!number_of(blockIdx.x, (uint32_t)(p.tiles_m * p.tiles_n * p.splits), t)) return;
     LinearBlock b;
@@ -274,67 +300,54 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) linear4_tile_kernel(FourTile 
     b.nk = max(0, min(p.slices, steps - b.s0));
     b.n0 = (int64_t)tile_n * TN;
     const int rows_w = (int)min((int64_t)TN, p.N - b.n0);
+    const int rot = first_slice((int)blockIdx.x & 7, (int)blockIdx.x >> 3, b.nk);
+    auto step_of = [&](int at) { return (uint32_t)(b.s0 + (at + rot >= b.nk ? at + rot - b.nk : at + rot)); };
 
-    // tokens: a load is 4 rows of 256 bytes, lane -> row lane / 16, slot lane % 16, which holds piece slot ^ row
+    // tokens: a load is 4 rows of 256 bytes, lane -> row lane / 16, slot lane % 16, which holds piece slot ^ row; codes: 16 rows of 64 bytes, as they lie; table: 1024
+    // bytes of a group's rows; sums: 4 groups of 64 tokens
     const uint32_t base = (uint32_t)uniform((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds);
-    uint32_t off[LA];
+    const uint32_t row_bytes = p.groups * (16u * GW);
+    uint32_t off_x[LX], off_codes[LC];
 #pragma unroll
-    for (int i = 0; i < LA; ++i) {
-        const int row = wave * (TM / W) + 4 * i + high;
-        off[i] = (row < b.rows ? (uint32_t)row * p.k : kNowhere) + (uint32_t)((low ^ (row & 15)) * 16);
-        asm volatile("" : "+v"(off[i]));
+    for (int i = 0; i < LX; ++i) {
+        const int row = wave * (TM / WN) + 4 * i + high;
+        off_x[i] = (row < b.rows ? (uint32_t)row * p.k : kNowhere) + (uint32_t)((low ^ (row & 15)) * 16);
     }
-    auto load_tokens = [&](int step, int part, uint32_t slot) {
-        const i32x4_t rx = buffer_of(p.x + ((int64_t)part * p.n + b.first) * p.k, (uint32_t)b.rows * p.k);
 #pragma unroll
-        for (int i = 0; i < LA; ++i) load_to_lds(base + slot * SLOT + (uint32_t)wave * (SLOT / W) + i * 1024u, off[i], rx, (uint32_t)step * (2 * kStep));
+    for (int i = 0; i < LC; ++i) {
+        const int row = wave * (TN / WN) + 16 * i + (lane >> 2);
+        off_codes[i] = (row < rows_w ? (uint32_t)row * row_bytes : kNowhere) + (uint32_t)(lane & 3) * 16u;
+    }
+    const uint32_t off_sums = high < G && 4 * low < b.rows ? (uint32_t)(high * p.sum_pitch + 4 * low) * 4u : kNowhere;
+    const i32x4_t rc = buffer_of(p.W + b.n0 * row_bytes, (uint32_t)rows_w * row_bytes);
+    auto load_x = [&](uint32_t step, int part, uint32_t slot) {
+        const i32x4_t r = buffer_of(p.x + ((int64_t)part * p.n + b.first) * p.k, (uint32_t)b.rows * p.k);
+#pragma unroll
+        for (int i = 0; i < LX; ++i) load_to_lds(base + slot * S::X + (uint32_t)wave * (S::X / WN) + i * 1024u, off_x[i], r, step * (2 * kStep));
     };
-    // (rows and groups of W that are not there: the last one's; the tokens have zeros there, and nothing is kept of the rows)
-    const unsigned char* weights = p.W + b.n0 * ((int64_t)p.groups * (16 * GW));
-    uint32_t row_at[FB];
+    auto load_codes = [&](uint32_t step, uint32_t slot) {
 #pragma unroll
-    for (int j = 0; j < FB; ++j) row_at[j] = (uint32_t)min((wn * FB + j) * 16 + low, rows_w - 1) * (p.groups * (16u * GW)) + (uint32_t)high * (4 * GW);
-    struct Words {
-        words_t w[FB][G];
-    };
-    auto load_words = [&](Words& v, int step) {
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const uint32_t group = min((uint32_t)(step * G + g), p.groups - 1);
-#pragma unroll
-            for (int j = 0; j < FB; ++j) v.w[j][g] = *reinterpret_cast<const words_t*>(weights + (row_at[j] + group * (16u * GW)));
+        for (int i = 0; i < LC; ++i) load_to_lds(base + 2 * S::X + slot * S::CODES + (uint32_t)wave * (S::CODES / WN) + i * 1024u, off_codes[i], rc, step * (kStep / 2));
+        const i32x4_t rt = buffer_of(p.table + ((int64_t)step * G * p.table_pitch + b.n0) * S::ROW, (uint32_t)(((G - 1) * p.table_pitch + TN) * S::ROW));
+        for (int i = wave; i < LT; i += WN) {
+            const uint32_t group = (uint32_t)i / (LT / G), in = (uint32_t)i % (LT / G);
+            const uint32_t to = (uint32_t)uniform((int)(base + 2 * S::X + 2 * S::CODES + slot * S::TABLE + (uint32_t)i * 1024u));
+            load_to_lds(to, (uint32_t)(group * p.table_pitch) * S::ROW + in * 1024u + lane * 16u, rt, 0);
+        }
+        if (wave == WN - 1) {
+            const i32x4_t rs = buffer_of(p.sums + (int64_t)step * G * p.sum_pitch + b.first, (uint32_t)((G - 1) * p.sum_pitch + p.sum_pitch - b.first) * 4u);
+            load_to_lds(base + 2 * (S::X + S::CODES + S::TABLE) + slot * S::SUMS, off_sums, rs, 0);
         }
     };
-    // a thread's scales: row tid / G + u 64 W / G, group tid % G of the step
-    struct Scales {
-        float scale[PER];
-        uint32_t zero[PER];
-        float sum;
-    };
-    const int sum_group = tid / TM, sum_row = tid % TM;
-    auto load_scales = [&](Scales& v, int step) {
-        const uint32_t group = min((uint32_t)(step * G + tid % G), p.groups - 1);
-#pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            const int64_t at = (b.n0 + min(tid / G + u * (64 * W / G), rows_w - 1)) * p.groups + group;
-            v.scale[u] = p.scales_f32 ? static_cast<const float*>(p.scales)[at] : td_load<bf16_t>(static_cast<const bf16_t*>(p.scales) + at);
-            if constexpr (ZEROS) v.zero[u] = p.zeros[at];
-        }
-        v.sum = sum_group < G && sum_row < b.rows ? p.sums[(int64_t)(step * G + sum_group) * p.n + b.first + sum_row] : 0.0f;
-    };
-    auto store_scales = [&](const Scales& v, int slot) {
-#pragma unroll
-        for (int u = 0; u < PER; ++u)
-            if (tid / G + u * (64 * W / G) < TN) scales[(slot * G + tid % G) * TN + tid / G + u * (64 * W / G)] = f32x2_t{v.scale[u], ZEROS ? -16.0f - (float)min(v.zero[u], 128u) : 0.0f};
-        if (sum_group < G) sums[(slot * G + sum_group) * TM + sum_row] = v.sum;
-    };
+    const Sixteen sixteen;
     f32x4_t acc[FA][FB];
 #pragma unroll
     for (int i = 0; i < FA; ++i)
 #pragma unroll
         for (int j = 0; j < FB; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
-    auto products = [&](const Words& v, uint32_t slot, int scale_slot, bool first_part) {
-        const unsigned char* from = lds + slot * SLOT + (wm * 16 + low) * (2 * kStep);
+    auto products = [&](uint32_t x_slot, uint32_t slot, bool first_part) {
+        const unsigned char* from = at_x + x_slot * S::X + low * (2 * kStep);
+        const unsigned char* codes_from = at_codes + slot * S::CODES + (wave * FB * 16 + low) * (kStep / 2) + high * (4 * GW);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             td_u32x4 x[FA][GW];
@@ -342,65 +355,65 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) linear4_tile_kernel(FourTile 
 #pragma unroll
             for (int i = 0; i < FA; ++i) {
 #pragma unroll
-                for (int s = 0; s < GW; ++s)
-                    x[i][s] = *reinterpret_cast<const td_u32x4*>(from + i * WM * 16 * (2 * kStep) + (((g * (4 * GW) + high * GW + s) ^ low) * 16));
-                sum[i] = *reinterpret_cast<const f32x4_t*>(sums + (scale_slot * G + g) * TM + (WM * i + wm) * 16 + 4 * high);
-                if (!ZEROS) sum[i] *= -24.0f;
+                for (int s = 0; s < GW; ++s) x[i][s] = *reinterpret_cast<const td_u32x4*>(from + i * 16 * (2 * kStep) + (((g * (4 * GW) + high * GW + s) ^ low) * 16));
+                sum[i] = *reinterpret_cast<const f32x4_t*>(at_sums + slot * S::SUMS + (g * 64 + i * 16 + 4 * high) * 4);
                 if (PARTS > 1 && !first_part) sum[i] = f32x4_t{0, 0, 0, 0};
             }
 #pragma unroll
             for (int j = 0; j < FB; ++j) {
+                const words_t words = *reinterpret_cast<const words_t*>(codes_from + j * 16 * (kStep / 2) + g * (16 * GW));
+                const unsigned char* entry = at_table + slot * S::TABLE + (g * TN + (wave * FB + j) * 16 + low) * S::ROW;
+                float scale, less;
+                if constexpr (S::ROW == 4) {
+                    const uint32_t e = *reinterpret_cast<const uint32_t*>(entry);
+                    scale = __uint_as_float(e & 0xffff0000u);
+                    less = __uint_as_float(e << 16);
+                } else {
+                    const f32x2_t e = *reinterpret_cast<const f32x2_t*>(entry);
+                    scale = e[0];
+                    less = e[1];
+                }
                 f32x4_t c[FA];
-                const f32x2_t scale = scales[(scale_slot * G + g) * TN + (wn * FB + j) * 16 + low];
 #pragma unroll
-                for (int i = 0; i < FA; ++i) c[i] = ZEROS ? sum[i] * scale[1] : sum[i];
+                for (int i = 0; i < FA; ++i) c[i] = sum[i] * less;
 #pragma unroll
                 for (int s = 0; s < GW; ++s) {
                     uint32_t word;
-                    if constexpr (GW == 1) word = v.w[j][g];
-                    else word = v.w[j][g][s];
-                    const td_u32x4 codes = sixteen_more(word);
+                    if constexpr (GW == 1) word = words;
+                    else word = words[s];
+                    const td_u32x4 codes = sixteen.more(word);
 #pragma unroll
                     for (int i = 0; i < FA; ++i) c[i] = mma(x[i][s], codes, c[i]);
                 }
 #pragma unroll
                 for (int i = 0; i < FA; ++i)
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[i][j][q] = fmaf(scale[0], c[i][q], acc[i][j][q]);
-                __builtin_amdgcn_sched_barrier(0);
+                    for (int q = 0; q < 4; ++q) acc[i][j][q] = fmaf(scale, c[i][q], acc[i][j][q]);
             }
         }
     };
-    Words now, next;
-    Scales coming;
     if (b.nk > 0) {
-        load_tokens(b.s0, 0, 0);
-        load_words(next, b.s0);
-        load_scales(coming, b.s0);
+        load_x(step_of(0), 0, 0);
+        load_codes(step_of(0), 0);
     }
-    uint32_t slot = 0;
+    uint32_t x_slot = 0;
 #pragma unroll 1
     for (int at = 0; at < b.nk; ++at) {
-        const bool more = at + 1 < b.nk;
-        now = next;
-        store_scales(coming, at & 1);
+        const uint32_t slot = (uint32_t)at & 1;
 #pragma unroll 1
         for (int part = 0; part < PARTS; ++part) {
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
-            if (part + 1 < PARTS) load_tokens(b.s0 + at, part + 1, slot ^ 1);
-            else if (more) load_tokens(b.s0 + at + 1, 0, slot ^ 1);
-            if (part == 0 && more) {
-                load_words(next, b.s0 + at + 1);
-                load_scales(coming, b.s0 + at + 1);
-            }
-            products(now, slot, at & 1, part == 0);
-            slot ^= 1;
+            if (part + 1 < PARTS) load_x(step_of(at), part + 1, x_slot ^ 1);
+            else if (at + 1 < b.nk) load_x(step_of(at + 1), 0, x_slot ^ 1);
+            if (part == 0 && at + 1 < b.nk) load_codes(step_of(at + 1), slot ^ 1);
+            products(x_slot, slot, part == 0);
+            x_slot ^= 1;
         }
     }
     __syncthreads();
-    finish_linear<four_t, false, W, FA, FB, WM, WN, 1, S::RB, true>(p, b, acc, lds, tid);
+    finish_linear<four_t, false, WN, FA, FB, 1, WN, 1, S::RB, true>(p, b, acc, lds, tid);
 }
 
 template <typename T, int GW> void launch(const FourArgs& p, int tokens, dim3 grid, hipStream_t s) {
@@ -416,35 +429,30 @@ template <typename T> void launch(const FourArgs& p, int group, int tokens, dim3
 }
 
 
-// f(group words, zeros, token blocks of a wavefront, row blocks, grid of wavefronts)
-template <typename F> void for_four_tile(int group, bool zeros, int shape, F f) {
-    auto with_tile = [&](auto gw, auto z) {
-        if (shape == 0) f(gw, z, num<2>{}, num<4>{}, num<2>{}, num<4>{});
-        else f(gw, z, num<4>{}, num<4>{}, num<2>{}, num<4>{});
+// f(parts of a token, group words, token blocks, row blocks of a wavefront, wavefronts)
+template <typename F> void for_four_tile(bool f32, int group, F f) {
+    auto with_parts = [&](auto gw) {
+        if (f32) f(num<3>{}, gw, num<4>{}, num<4>{}, num<4>{});
+        else f(num<1>{}, gw, num<4>{}, num<4>{}, num<4>{});
     };
-    auto with_zeros = [&](auto gw) {
-        if (zeros) with_tile(gw, std::true_type{});
-        else with_tile(gw, std::false_type{});
-    };
-    if (group == 32) with_zeros(num<1>{});
-    else if (group == 64) with_zeros(num<2>{});
-    else with_zeros(num<4>{});
+    if (group == 32) with_parts(num<1>{});
+    else if (group == 64) with_parts(num<2>{});
+    else with_parts(num<4>{});
 }
+constexpr int kTileTokens = 64, kTileRows = 256;
 
 tardis_status_t init_tiles() {
     static td_once once;
     return once.run([]() -> tardis_status_t {
         bool ok = true;
         for (int group = 32; group <= 128; group *= 2)
-            for (int zeros = 0; zeros < 2; ++zeros)
-                for (int shape = 0; shape < 2; ++shape)
-                    for_four_tile(group, zeros, shape, [&](auto gw, auto z, auto fa, auto fb, auto wm, auto wn) {
-                        constexpr int bytes = FourTileShape<fa, fb, wm, wn, 4 / gw>::kLds;
-                        ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(linear4_tile_kernel<1, gw, decltype(z)::value, fa, fb, wm, wn>),
-                                                  hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
-                        ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(linear4_tile_kernel<3, gw, decltype(z)::value, fa, fb, wm, wn>),
-                                                  hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess;
-                    });
+            for (int f32 = 0; f32 < 2; ++f32)
+                for_four_tile(f32, group, [&](auto parts, auto gw, auto fa, auto fb, auto wn) {
+                    typedef FourTileShape<parts, gw, fa, fb, wn> S;
+                    ok &= S::TM == kTileTokens && S::TN == kTileRows;
+                    ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(linear4_tile_kernel<parts, gw, fa, fb, wn>),
+                                              hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds) == hipSuccess;
+                });
         return ok ? TARDIS_OK : TARDIS_ERR_HIP;
     });
 }
@@ -452,25 +460,29 @@ tardis_status_t init_tiles() {
 // How a call is done, by its sizes and the working memory that it has
 struct FourPlan {
     bool tiles;
-    int shape, splits, slices, tm, tn;
-    int64_t n_parts, units, at_sums, at_part, work;
+    int splits, slices;
+    int64_t units, all_groups, sum_pitch, table_pitch, at_sums, at_table, at_part, work;
 };
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 FourPlan plan_four(const tardis_linear_4bit_desc* d, int64_t n, int64_t room) {
     FourPlan p{};
     if (n <= 64) return p;
-    p.shape = d->dtype == TARDIS_F32 || n <= 64 ? 0 : 1;
-    p.tm = p.shape == 0 ? 64 : 128;
-    p.tn = 256;
-    p.n_parts = d->dtype == TARDIS_F32 ? 3 : 1;
-    const int64_t steps = (d->n_in + kStep - 1) / kStep, tiles = ((n + p.tm - 1) / p.tm) * ((d->n_out + p.tn - 1) / p.tn);
+    const bool f32 = d->dtype == TARDIS_F32;
+    const int64_t steps = (d->n_in + kStep - 1) / kStep, tiles = ((n + kTileTokens - 1) / kTileTokens) * ((d->n_out + kTileRows - 1) / kTileRows);
     p.units = steps * (kStep / 8);
-    p.at_sums = round_up(p.n_parts * n * p.units * 16, 256);
-    p.at_part = p.at_sums + round_up(steps * (kStep / d->group) * n * 4, 256);
-    if (tiles >= 1 << 21 || p.units * 16 * p.tm >= kNowhere || n * p.units >= kMostThreads || p.at_part > room) return FourPlan{};
+    p.all_groups = steps * (kStep / d->group);
+    p.sum_pitch = round_up(n, 4);
+    p.table_pitch = round_up(d->n_out, kTileRows);
+    p.at_sums = round_up((f32 ? 3 : 1) * n * p.units * 16, 256);
+    p.at_table = p.at_sums + round_up(p.all_groups * p.sum_pitch * 4, 256);
+    p.at_part = p.at_table + p.all_groups * p.table_pitch * (f32 ? 8 : 4);
+    // (offsets of a tile's rows, of four groups' sums and of the table are 32 bits)
+    if (tiles >= 1 << 21 || p.units * 16 * kTileTokens >= kNowhere || 4 * p.sum_pitch * 4 >= kNowhere || n * p.units + p.all_groups * p.table_pitch >= kMostThreads ||
+        p.at_part > room)
+        return FourPlan{};
     p.splits = 1;
-    while (p.splits < 16 && tiles * p.splits * 2 <= 256 && steps >= 4 * p.splits * 2 && p.at_part + 2 * p.splits * n * d->n_out * 4 <= room) p.splits *= 2;
+    while (p.splits < 16 && tiles * p.splits * 2 <= 512 && steps >= 4 * p.splits * 2 && p.at_part + 2 * p.splits * n * d->n_out * 4 <= room) p.splits *= 2;
     p.slices = (int)((steps + p.splits - 1) / p.splits);
     p.work = p.at_part + (p.splits > 1 ? p.splits * n * d->n_out * 4 : 0);
     p.tiles = true;
@@ -483,12 +495,21 @@ tardis_status_t run_tiles(const tardis_linear_4bit_desc* d, const FourPlan& plan
     const bool f32 = d->dtype == TARDIS_F32;
     FourTokens t{};
     t.x = static_cast<const unsigned char*>(x);
+    t.scales = d->scales;
+    t.zeros = d->zeros;
     t.parts = reinterpret_cast<td_u32x4*>(work);
     t.sums = reinterpret_cast<float*>(work + plan.at_sums);
+    t.table = work + plan.at_table;
     t.n = n;
+    t.N = d->n_out;
     t.x_pitch = x_pitch * (int64_t)td_elem_size(d->dtype);
+    t.sum_pitch = plan.sum_pitch;
+    t.table_pitch = plan.table_pitch;
     t.k = (uint32_t)d->n_in;
     t.units = (uint32_t)plan.units;
+    t.groups = (uint32_t)((d->n_in + d->group - 1) / d->group);
+    t.all_groups = (uint32_t)plan.all_groups;
+    t.token_blocks = (uint32_t)((n * plan.units + 255) / 256);
     FourTile p{};
     p.x = work;
     p.W = reinterpret_cast<const unsigned char*>(d->W);
@@ -500,31 +521,27 @@ tardis_status_t run_tiles(const tardis_linear_4bit_desc* d, const FourPlan& plan
     p.k = (uint32_t)(plan.units * 16);
     p.act = d->act == TARDIS_ACT_GELU_ERF && d->out_dtype == TARDIS_BF16 && !residual ? kActGelu16 : d->act;
     p.out_f32 = d->out_dtype == TARDIS_F32;
-    p.tiles_m = (int)((n + plan.tm - 1) / plan.tm);
-    p.tiles_n = (int)((d->n_out + plan.tn - 1) / plan.tn);
+    p.tiles_m = (int)((n + kTileTokens - 1) / kTileTokens);
+    p.tiles_n = (int)((d->n_out + kTileRows - 1) / kTileRows);
     p.splits = plan.splits;
     p.slices = plan.slices;
-    p.scales = d->scales;
-    p.zeros = d->zeros;
     p.sums = t.sums;
-    p.groups = (uint32_t)((d->n_in + d->group - 1) / d->group);
-    p.scales_f32 = f32;
+    p.table = t.table;
+    p.sum_pitch = plan.sum_pitch;
+    p.table_pitch = plan.table_pitch;
+    p.groups = t.groups;
     FourTile q = p;
     if (plan.splits > 1) {
         q.part = reinterpret_cast<float*>(work + plan.at_part);
         q.act = TARDIS_ACT_IDENTITY;
     }
-    const dim3 token_grid((unsigned)((n * plan.units + 255) / 256));
+    const dim3 prepare(t.token_blocks + (unsigned)((plan.all_groups * plan.table_pitch + 255) / 256));
     const int blocks = (int)(((int64_t)p.tiles_m * p.tiles_n * p.splits + 7) / 8 * 8);
-    for_four_tile(d->group, d->zeros != nullptr, plan.shape, [&](auto gw, auto z, auto fa, auto fb, auto wm, auto wn) {
-        constexpr int bytes = FourTileShape<fa, fb, wm, wn, 4 / gw>::kLds, threads = 64 * wm * wn;
-        if (f32) {
-            hipLaunchKernelGGL((linear4_tokens_kernel<float, gw>), token_grid, dim3(256), 0, s, t);
-            hipLaunchKernelGGL((linear4_tile_kernel<3, gw, decltype(z)::value, fa, fb, wm, wn>), dim3((unsigned)blocks), dim3(threads), bytes, s, q);
-        } else {
-            hipLaunchKernelGGL((linear4_tokens_kernel<bf16_t, gw>), token_grid, dim3(256), 0, s, t);
-            hipLaunchKernelGGL((linear4_tile_kernel<1, gw, decltype(z)::value, fa, fb, wm, wn>), dim3((unsigned)blocks), dim3(threads), bytes, s, q);
-        }
+    for_four_tile(f32, d->group, [&](auto parts, auto gw, auto fa, auto fb, auto wn) {
+        constexpr int bytes = FourTileShape<parts, gw, fa, fb, wn>::kLds, threads = 64 * wn;
+        if constexpr (decltype(parts)::value == 3) hipLaunchKernelGGL((linear4_prepare_kernel<float, gw>), prepare, dim3(256), 0, s, t);
+        else hipLaunchKernelGGL((linear4_prepare_kernel<bf16_t, gw>), prepare, dim3(256), 0, s, t);
+        hipLaunchKernelGGL((linear4_tile_kernel<parts, gw, fa, fb, wn>), dim3((unsigned)blocks), dim3(threads), bytes, s, q);
     });
     if (plan.splits > 1) {
         p.part = q.part;
