@@ -19,10 +19,9 @@ struct FourArgs {
     const void *scales, *b, *r;
     const uint8_t* zeros;
     void* y;
-    float* part;                   // not null: sums of one range of K each go here, [range][n][N], and nothing else is done
     int64_t n, N, x_pitch;         // (bytes)
-    uint32_t k, groups;            // columns; groups of a row
-    int act, out_f32, tiles_n, splits;
+    uint32_t k, groups, chunk;     // columns; groups of a row; steps whose columns of all tokens are in LDS together
+    int act, out_f32;
 };
 
 constexpr int kWaves = 8;
@@ -87,111 +86,176 @@ template <typename T> __device__ __forceinline__ void load_token_end(Token<T>& t
     }
 }
 
-// A block has 16 rows of W and 16 TT tokens, its wavefronts every eighth group of a range of K.  GW: words of a group in a lane (32 GW columns a group).
-// Lane l holds, of W's row l % 16, the columns 8 GW (l / 16) .. of a group, which is one load, and the same columns of token l % 16.
-template <typename T, int GW, int TT>
-__global__ void __launch_bounds__(64 * kWaves, 2) linear4_kernel(FourArgs p) {
-    typedef typename words_of<GW>::type words_t;
-    constexpr int D = 4;                           // groups whose weights are under way together
-    __shared__ f32x4_t sums[kWaves * TT * 64];
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), low = lane & 15, high = lane >> 4;
-    const int tile_n = (int)(blockIdx.x % (uint32_t)p.tiles_n), rest = (int)(blockIdx.x / (uint32_t)p.tiles_n), range = rest % p.splits, tile_m = rest / p.splits;
-    const Sixteen sixteen;
-    const int64_t n0 = (int64_t)tile_n * 16, m0 = (int64_t)tile_m * (16 * TT);
-    // (rows and tokens that are not there: the last one's, of which nothing is kept)
-    const int64_t row = min(n0 + low, p.N - 1);
-    const uint32_t* W = p.W + row * ((int64_t)p.groups * (4 * GW)) + high * GW;
-    const uint8_t* zeros = p.zeros ? p.zeros + row * p.groups : nullptr;
-    const T* scales[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) scales[q] = static_cast<const T*>(p.scales) + min(n0 + 4 * high + q, p.N - 1) * (int64_t)p.groups;
-    const unsigned char* x[TT];
-#pragma unroll
-    for (int t = 0; t < TT; ++t) x[t] = p.x + min(m0 + 16 * t + low, p.n - 1) * p.x_pitch + high * (8 * GW) * sizeof(T);
+constexpr int kStep = 128;                          // columns of a step: 64 bytes of a row's codes
 
-    f32x4_t acc[TT];
-#pragma unroll
-    for (int t = 0; t < TT; ++t) acc[t] = f32x4_t{0, 0, 0, 0};
-    auto add = [&](uint32_t g, const words_t& w, uint32_t zero, const float (&scale)[4], auto load) {
-        f32x4_t c[TT];
-#pragma unroll
-        for (int t = 0; t < TT; ++t) c[t] = f32x4_t{0, 0, 0, 0};
-        const uint32_t less = sixteen_less(zero);
-#pragma unroll
-        for (int s = 0; s < GW; ++s) {
-            uint32_t word;
-            if constexpr (GW == 1) word = w;
-            else word = w[s];
-            const td_u32x4 codes = sixteen.more(word);
-#pragma unroll
-            for (int t = 0; t < TT; ++t) {
-                Token<T> v;
-                load(v, x[t] + ((size_t)g * (32 * GW) + 8 * s) * sizeof(T), (int)p.k - (int)(g * (32 * GW) + high * (8 * GW) + 8 * s));
-#pragma unroll
-                for (int i = 0; i < Token<T>::PARTS; ++i) {
-                    c[t] = mma(codes, v.part[i], c[t]);
-                    c[t] = mma(td_u32x4{less, less, less, less}, v.part[i], c[t]);
-                }
-            }
+// ---------------------------------------------------------------- up to 16 tokens
+// A block has 16 RT rows of W and all tokens, which it puts into LDS, with the table of scales and zero points, as many columns at a time as there is room for.
+// Its wavefronts are RT times KW: one has 16 rows and a KW-th of the steps, whose codes come straight to a ring of its own in LDS, D - 2 steps ahead of the two
+// that are multiplied, without barriers.  The loop is a step long and not unrolled: a block runs through its code once, and what it has to fetch of it counts
+// (1 token, 1024 -> 1024: 7.9 us with three batches of four groups in registers, all unrolled, REPLACE).
+// Lane l multiplies, of W's row l % 16, the columns 8 GW (l / 16) .. of a group, and the same columns of token l % 16.
+template <typename T, int RT> struct FourBlock {
+    static constexpr int KW = kWaves / RT, PARTS = Token<T>::PARTS, ENTRY = PARTS == 1 ? 4 : 8, D = 8, kRing = kWaves * D * 1024;
+    static constexpr int64_t token_pitch(int64_t steps) { return steps * (2 * kStep) + 16; }             // (16 bytes more: other banks)
+    static constexpr int64_t lds(int64_t n, int64_t steps, int64_t groups) { return kRing + n * PARTS * token_pitch(steps) + steps * groups * (16 * RT) * ENTRY; }
+};
+template <typename T, int GW, int RT>
+__global__ void __launch_bounds__(64 * kWaves, 4) linear4_kernel(FourArgs p) {
+    typedef typename words_of<GW>::type words_t;
+    typedef FourBlock<T, RT> S;
+    constexpr int D = S::D, KW = S::KW, G = 4 / GW, PARTS = S::PARTS, THREADS = 64 * kWaves;
+    extern __shared__ __align__(1024) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), low = lane & 15, high = lane >> 4, kw = wave % KW, rt = wave / KW, n = (int)p.n;
+    const int64_t block0 = (int64_t)blockIdx.x * (16 * RT), n0 = block0 + rt * 16;
+    const uint32_t pitch = p.chunk * (2 * kStep) + 16, part_pitch = pitch * (uint32_t)n;
+    unsigned char *tokens = lds + S::kRing, *table = tokens + PARTS * part_pitch;      // table: [group][row of the block]
+
+    // codes: a load is 16 rows of 64 bytes, as they lie.  (What lies behind a row or the last one has tokens of 0 or is kept nowhere)
+    const uint32_t row_bytes = p.groups * (16u * GW), base = (uint32_t)uniform((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds);
+    const int rows = (int)max((int64_t)0, min((int64_t)16, p.N - n0));
+    const i32x4_t rw = buffer_of(reinterpret_cast<const unsigned char*>(p.W) + min(n0, p.N - 1) * row_bytes, (uint32_t)rows * row_bytes);
+    const uint32_t off = (uint32_t)(lane >> 2) * row_bytes + (uint32_t)(lane & 3) * 16u, ring = base + (uint32_t)wave * (D * 1024);
+    const uint32_t steps = (p.k + kStep - 1) / kStep, share = ((p.chunk + KW - 1) / KW + 1) & ~1u;   // (of a chunk's steps, for a wavefront: even)
+    uint32_t ask_chunk = 0, ask = 0, ask_slot = 0;                                            // the step that is asked for next
+    auto load_step = [&]() {                       // (past the last one: an empty buffer)
+        const uint32_t in = (uint32_t)kw * share + ask, step = ask_chunk + in;
+        i32x4_t r = rw;
+        r.z = in < p.chunk && step < steps ? r.z : 0;
+        const uint32_t soff = r.z ? step * (kStep / 2) : 0u;
+        load_to_lds<true>(ring + ask_slot * 1024u, off, r, soff);
+        ask_slot = ask_slot + 1 == D ? 0 : ask_slot + 1;
+        if (++ask == share) {
+            ask = 0;
+            ask_chunk += p.chunk;
         }
-#pragma unroll
-        for (int t = 0; t < TT; ++t)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) acc[t][q] = fmaf(scale[q], c[t][q], acc[t][q]);
     };
-    const uint32_t step = (uint32_t)(kWaves * p.splits), first = (uint32_t)(range * kWaves + wave), whole = p.k / (32 * GW);
 #pragma unroll 1
-    for (uint32_t g0 = first; g0 < whole; g0 += D * step) {
-        words_t w[D];
-        uint32_t zero[D];
-        float scale[D][4];
-#pragma unroll
-        for (int i = 0; i < D; ++i) {                  // (past the last whole group: that one, with scales of 0)
-            const uint32_t g = min(g0 + i * step, whole - 1);
-            w[i] = __builtin_nontemporal_load(reinterpret_cast<const words_t*>(W + (size_t)g * (4 * GW)));
-            zero[i] = zeros ? zeros[g] : 8u;
-#pragma unroll
-            for (int q = 0; q < 4; ++q) scale[i][q] = g0 + i * step < whole ? td_load<T>(scales[q] + g) : 0.0f;
-        }
-#pragma unroll
-        for (int i = 0; i < D; ++i) {
-            const uint32_t g = min(g0 + i * step, whole - 1);
-            add(g, w[i], zero[i], scale[i], [](Token<T>& v, const unsigned char* at, int) { load_token<T>(v, at); });
-        }
-    }
-    if (whole < p.groups && whole % step == first) {   // the last group, which is not whole
-        float scale[4];
-#pragma unroll
-        for (int q = 0; q < 4; ++q) scale[q] = td_load<T>(scales[q] + whole);
-        add(whole, *reinterpret_cast<const words_t*>(W + (size_t)whole * (4 * GW)), zeros ? zeros[whole] : 8u, scale,
-            [](Token<T>& v, const unsigned char* at, int left) { load_token_end<T>(v, at, left); });
-    }
-    // the wavefronts' sums, in their order; a thread has four neighbouring columns of a token
-#pragma unroll
-    for (int t = 0; t < TT; ++t) sums[(wave * TT + t) * 64 + lane] = acc[t];
-    __syncthreads();
-    if (tid >= TT * 64) return;
-    f32x4_t v = sums[tid];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) v += sums[w * TT * 64 + tid];
-    const int64_t m = m0 + (tid >> 6) * 16 + low, n = n0 + 4 * high;
-    const int columns = (int)min((int64_t)4, p.N - n);
-    if (m >= p.n || columns <= 0) return;
-    const int64_t at = m * p.N + n;
-    if (p.part) {
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (q < columns) p.part[(int64_t)range * p.n * p.N + at + q] = v[q];
-        return;
-    }
+    for (int i = 0; i < D - 2; ++i) load_step();
+
+    // what a thread finishes: four neighbouring rows of a token.  (Bias and residual are asked for before the products)
+    const int tile = tid >> 6, token = lane >> 2, four = lane & 3;
+    const int64_t first_n = block0 + tile * 16 + 4 * four, at_y = (int64_t)token * p.N + first_n;
+    const int columns = tid < RT * 64 && token < n ? (int)max((int64_t)0, min((int64_t)4, p.N - first_n)) : 0;
     auto element = [&](const void* from, int64_t i) { return p.out_f32 ? static_cast<const float*>(from)[i] : td_load<bf16_t>(static_cast<const bf16_t*>(from) + i); };
     float bias[4] = {}, r[4] = {};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         if (q >= columns) continue;
-        if (p.b) bias[q] = element(p.b, n + q);
-        if (p.r) r[q] = element(p.r, at + q);
+        if (p.b) bias[q] = element(p.b, first_n + q);
+        if (p.r) r[q] = element(p.r, at_y + q);
     }
+
+    const Sixteen sixteen;
+    f32x4_t acc = {0, 0, 0, 0};                     // tokens 4 high + q, row low
+    uint32_t slot = 0;
+#pragma unroll 1
+    for (uint32_t chunk = 0; chunk < steps; chunk += p.chunk) {
+        const uint32_t here = min(p.chunk, steps - chunk), units = here * (kStep / 8), entries = here * G, all_units = units * (uint32_t)n, all_entries = entries * (16 * RT);
+        if (chunk > 0) __syncthreads();
+        // (so many pieces of tokens and entries of the table of a thread side by side: one after the other they would wait for memory each)
+        constexpr int X = PARTS == 1 ? 4 : 2, E = 4;
+        uint32_t u0 = 0, e0 = 0;
+#pragma unroll 1
+        do {
+            Token<T> v[X];
+            uint32_t x_to[X], group[E], e_row[E], zero[E];
+            float scale[E];
+#pragma unroll
+            for (int i = 0; i < X; ++i) {
+                uint32_t unit;
+                const uint32_t u = min(u0 + i * THREADS + tid, all_units - 1), t = divide(u, units, unit), column = chunk * kStep + unit * 8;
+                const unsigned char* at = p.x + t * p.x_pitch + (size_t)column * sizeof(T);
+                x_to[i] = t * pitch + unit * 16;
+                if (column + 8 <= p.k) load_token<T>(v[i], at);
+                else load_token_end<T>(v[i], at, (int)p.k - (int)column);
+            }
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                e_row[i] = divide(min(e0 + i * THREADS + tid, all_entries - 1), entries, group[i]);
+                const int64_t at = min(block0 + e_row[i], p.N - 1) * (int64_t)p.groups + min(chunk * G + group[i], p.groups - 1);
+                scale[i] = td_load<T>(static_cast<const T*>(p.scales) + at);
+                zero[i] = p.zeros ? p.zeros[at] : 8u;
+            }
+#pragma unroll
+            for (int i = 0; i < X; ++i)
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) *reinterpret_cast<td_u32x4*>(tokens + part * part_pitch + x_to[i]) = v[i].part[part];
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float less = -16.0f - (float)min(zero[i], 128u);
+                unsigned char* to = table + (group[i] * (16 * RT) + e_row[i]) * S::ENTRY;
+                if (chunk * G + group[i] >= p.groups) scale[i] = 0.0f;
+                if constexpr (PARTS == 1) *reinterpret_cast<uint32_t*>(to) = __float_as_uint(scale[i]) | __float_as_uint(less) >> 16;
+                else *reinterpret_cast<f32x2_t*>(to) = f32x2_t{scale[i], less};
+            }
+            u0 += X * THREADS;
+            e0 += E * THREADS;
+        } while (u0 < all_units || e0 < all_entries);
+        __syncthreads();
+        // two steps at a time: a step's instructions wait for one another
+#pragma unroll 1
+        for (uint32_t in = 0; in < share; in += 2) {
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(D - 4) : "memory");
+            words_t words[2][G];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const unsigned char* codes_at = lds + wave * (D * 1024) + (slot + h) * 1024 + low * (kStep / 2) + high * (4 * GW);
+#pragma unroll
+                for (int g = 0; g < G; ++g) words[h][g] = *reinterpret_cast<const words_t*>(codes_at + g * (16 * GW));
+            }
+            load_step();                           // (into the slots that were read in the turn before)
+            load_step();
+            slot = slot + 2 == D ? 0 : slot + 2;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t step = (uint32_t)kw * share + in + h;
+                if (step >= here) continue;        // (a place in the ring all the same)
+                const unsigned char* x_at = tokens + min(low, n - 1) * pitch + step * (2 * kStep) + high * (16 * GW);
+                const unsigned char* entry_at = table + (step * G * (16 * RT) + rt * 16 + low) * S::ENTRY;
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    float scale;
+                    uint32_t less;
+                    if constexpr (PARTS == 1) {
+                        const uint32_t e = *reinterpret_cast<const uint32_t*>(entry_at + g * (16 * RT) * S::ENTRY);
+                        scale = __uint_as_float(e & 0xffff0000u);
+                        less = __builtin_amdgcn_perm(e, e, 0x01000100u);
+                    } else {
+                        const f32x2_t e = *reinterpret_cast<const f32x2_t*>(entry_at + g * (16 * RT) * S::ENTRY);
+                        scale = e[0];
+                        less = __builtin_amdgcn_perm(__float_as_uint(e[1]), __float_as_uint(e[1]), 0x03020302u);
+                    }
+                    f32x4_t c = {0, 0, 0, 0}, d = {0, 0, 0, 0};
+#pragma unroll
+                    for (int s = 0; s < GW; ++s) {
+                        uint32_t word;
+                        if constexpr (GW == 1) word = words[h][g];
+                        else word = words[h][g][s];
+                        const td_u32x4 codes = sixteen.more(word);
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part) {
+                            const td_u32x4 x = *reinterpret_cast<const td_u32x4*>(x_at + part * part_pitch + (g * (4 * GW) + s) * 16);
+                            c = mma(x, codes, c);
+                            d = mma(x, td_u32x4{less, less, less, less}, d);
+                        }
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[q] = fmaf(scale, c[q] + d[q], acc[q]);
+                }
+            }
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    // the wavefronts' sums of a row tile, in their order: [row tile][part][token][row]
+    float* sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sums[((wave * 16) + 4 * high + q) * 16 + low] = acc[q];
+    __syncthreads();
+    if (columns == 0) return;
+    f32x4_t v = {0, 0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < KW; ++w) v += *reinterpret_cast<const f32x4_t*>(sums + ((tile * KW + w) * 16 + token) * 16 + 4 * four);
     with_linear_act(p.act, [&](auto act) {
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = linear_act<decltype(act)::value>(v[q] + bias[q]) + r[q];
@@ -199,13 +263,12 @@ __global__ void __launch_bounds__(64 * kWaves, 2) linear4_kernel(FourArgs p) {
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         if (q >= columns) continue;
-        if (p.out_f32) static_cast<float*>(p.y)[at + q] = v[q];
-        else td_store<bf16_t>(static_cast<bf16_t*>(p.y) + at + q, v[q]);
+        if (p.out_f32) static_cast<float*>(p.y)[at_y + q] = v[q];
+        else td_store<bf16_t>(static_cast<bf16_t*>(p.y) + at_y + q, v[q]);
     }
 }
 
 // ---------------------------------------------------------------- many tokens
-constexpr int kStep = 128;                          // columns of a step
 // What the tiles read beside the codes, made by one launch before theirs:
 //   tokens  PARTS parts in bf16, [part][token][units], zeros behind the last column
 //   sums    of every group's columns, [group][sum_pitch]
@@ -416,18 +479,24 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
     finish_linear<four_t, false, WN, FA, FB, 1, WN, 1, S::RB, true>(p, b, acc, lds, tid);
 }
 
-template <typename T, int GW> void launch(const FourArgs& p, int tokens, dim3 grid, hipStream_t s) {
-    const dim3 block(64 * kWaves);
-    if (tokens == 1) hipLaunchKernelGGL((linear4_kernel<T, GW, 1>), grid, block, 0, s, p);
-    else if (tokens == 2) hipLaunchKernelGGL((linear4_kernel<T, GW, 2>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((linear4_kernel<T, GW, 4>), grid, block, 0, s, p);
+template <typename T, int GW, int RT> void launch(const FourArgs& p, unsigned blocks, size_t lds, hipStream_t s) {
+    hipLaunchKernelGGL((linear4_kernel<T, GW, RT>), dim3(blocks), dim3(64 * kWaves), lds, s, p);
 }
-template <typename T> void launch(const FourArgs& p, int group, int tokens, dim3 grid, hipStream_t s) {
-    if (group == 32) launch<T, 1>(p, tokens, grid, s);
-    else if (group == 64) launch<T, 2>(p, tokens, grid, s);
-    else launch<T, 4>(p, tokens, grid, s);
+// f(element type, group words, row tiles of a block)
+template <typename F> void for_four(bool f32, int group, int rows, F f) {
+    auto with_rows = [&](auto type, auto gw) {
+        if (rows == 1) f(type, gw, num<1>{});
+        else if (rows == 2) f(type, gw, num<2>{});
+        else f(type, gw, num<4>{});
+    };
+    auto with_group = [&](auto type) {
+        if (group == 32) with_rows(type, num<1>{});
+        else if (group == 64) with_rows(type, num<2>{});
+        else with_rows(type, num<4>{});
+    };
+    if (f32) with_group(float{});
+    else with_group(bf16_t{});
 }
-
 
 // f(parts of a token, group words, token blocks, row blocks of a wavefront, wavefronts)
 template <typename F> void for_four_tile(bool f32, int group, F f) {
@@ -441,18 +510,24 @@ template <typename F> void for_four_tile(bool f32, int group, F f) {
 }
 constexpr int kTileTokens = 64, kTileRows = 256;
 
-tardis_status_t init_tiles() {
+tardis_status_t init_four() {
     static td_once once;
     return once.run([]() -> tardis_status_t {
         bool ok = true;
         for (int group = 32; group <= 128; group *= 2)
-            for (int f32 = 0; f32 < 2; ++f32)
+            for (int f32 = 0; f32 < 2; ++f32) {
+                for (int rows = 1; rows <= 4; rows *= 2)
+                    for_four(f32, group, rows, [&](auto type, auto gw, auto rt) {
+                        ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(linear4_kernel<decltype(type), gw, rt>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                  kLdsBytes) == hipSuccess;
+                    });
                 for_four_tile(f32, group, [&](auto parts, auto gw, auto fa, auto fb, auto wn) {
                     typedef FourTileShape<parts, gw, fa, fb, wn> S;
                     ok &= S::TM == kTileTokens && S::TN == kTileRows;
                     ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(linear4_tile_kernel<parts, gw, fa, fb, wn>),
                                               hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds) == hipSuccess;
                 });
+            }
         return ok ? TARDIS_OK : TARDIS_ERR_HIP;
     });
 }
@@ -467,7 +542,7 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 FourPlan plan_four(const tardis_linear_4bit_desc* d, int64_t n, int64_t room) {
     FourPlan p{};
-    if (n <= 64) return p;
+    if (n <= 16) return p;
     const bool f32 = d->dtype == TARDIS_F32;
     const int64_t steps = (d->n_in + kStep - 1) / kStep, tiles = ((n + kTileTokens - 1) / kTileTokens) * ((d->n_out + kTileRows - 1) / kTileRows);
     p.units = steps * (kStep / 8);
@@ -491,7 +566,7 @@ FourPlan plan_four(const tardis_linear_4bit_desc* d, int64_t n, int64_t room) {
 
 tardis_status_t run_tiles(const tardis_linear_4bit_desc* d, const FourPlan& plan, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y,
                           unsigned char* work, hipStream_t s) {
-    TD_TRY(init_tiles());
+    TD_TRY(init_four());
     const bool f32 = d->dtype == TARDIS_F32;
     FourTokens t{};
     t.x = static_cast<const unsigned char*>(x);
@@ -562,7 +637,9 @@ tardis_status_t td_linear_4bit(const tardis_linear_4bit_desc* d, const void* x, 
                                int64_t work_bytes, hipStream_t s) {
     const FourPlan plan = plan_four(d, n, work_bytes);
     if (plan.tiles) return run_tiles(d, plan, x, n, x_pitch, residual, y, static_cast<unsigned char*>(work), s);
+    TD_TRY(init_four());
     FourArgs p{};
+    const bool f32 = d->dtype == TARDIS_F32;
     const int64_t es = (int64_t)td_elem_size(d->dtype), eo = (int64_t)td_elem_size(d->out_dtype);
     p.x = static_cast<const unsigned char*>(x);
     p.W = d->W;
@@ -571,26 +648,27 @@ tardis_status_t td_linear_4bit(const tardis_linear_4bit_desc* d, const void* x, 
     p.b = d->b;
     p.r = residual;
     p.y = y;
-    p.n = n;
     p.N = d->n_out;
     p.x_pitch = (n > 1 ? x_pitch : d->n_in) * es;
     p.k = (uint32_t)d->n_in;
     p.groups = (uint32_t)((d->n_in + d->group - 1) / d->group);
     p.act = d->act == TARDIS_ACT_GELU_ERF && d->out_dtype == TARDIS_BF16 && !residual ? kActGelu16 : d->act;
     p.out_f32 = d->out_dtype == TARDIS_F32;
-    p.tiles_n = (int)((d->n_out + 15) / 16);
-    p.splits = 1;
-    const int tokens = n <= 16 ? 1 : n <= 32 ? 2 : 4;                   // (in 16s)
-    const int64_t rows = 16 * tokens, most = std::max<int64_t>(1, kMostThreads / (64 * kWaves) / p.tiles_n) * rows;   // tokens of a launch
-    for (int64_t at = 0; at < n; at += most) {
+    for (int64_t at = 0; at < n; at += 16) {
         FourArgs q = p;
-        q.n = std::min(most, n - at);
+        q.n = std::min<int64_t>(16, n - at);
         q.x += at * p.x_pitch;
         q.y = static_cast<unsigned char*>(y) + at * p.N * eo;
         if (residual) q.r = static_cast<const unsigned char*>(residual) + at * p.N * eo;
-        const dim3 grid((unsigned)(p.tiles_n * ((q.n + rows - 1) / rows)));
-        if (d->dtype == TARDIS_F32) launch<float>(q, d->group, tokens, grid, s);
-        else launch<bf16_t>(q, d->group, tokens, grid, s);
+        const int64_t tiles = (p.N + 15) / 16, steps = (d->n_in + kStep - 1) / kStep, groups = kStep / d->group;
+        const int rows = tiles >= 1024 || (tiles >= 512 && q.n > 4) ? 4 : tiles >= 512 ? 2 : 1;
+        for_four(f32, d->group, rows, [&](auto type, auto gw, auto rt) {
+            typedef FourBlock<decltype(type), rt> S;
+            const int64_t room = kLdsBytes - S::lds(q.n, 0, groups), each = S::lds(q.n, 1, groups) - S::lds(q.n, 0, groups);
+            const int64_t fit = room / each;               // (at least 6 steps: 16 tokens in three parts, four groups of 64 rows)
+            q.chunk = (uint32_t)std::min(steps, fit >= S::KW ? fit / S::KW * S::KW : fit);
+            launch<decltype(type), gw, rt>(q, (unsigned)((tiles + rows - 1) / rows), (size_t)S::lds(q.n, q.chunk, groups), s);
+        });
     }
     TD_HIP(hipGetLastError());
     return TARDIS_OK;
