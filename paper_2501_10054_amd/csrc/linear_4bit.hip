@@ -286,24 +286,41 @@ struct FourTokens {
 };
 template <typename T, int GW>
 __global__ void __launch_bounds__(256) linear4_prepare_kernel(FourTokens p) {
-    if (blockIdx.x >= p.token_blocks) {
-        const int64_t i = (int64_t)(blockIdx.x - p.token_blocks) * 256 + threadIdx.x;
-        const uint32_t group = (uint32_t)(i / p.table_pitch);
-        const int64_t row = i - group * p.table_pitch;
-        if (group >= p.all_groups) return;
-        float scale = 0.0f;
-        uint32_t zero = 8;
-        if (row < p.N && group < p.groups) {
-            scale = td_load<T>(static_cast<const T*>(p.scales) + row * p.groups + group);
-            if (p.zeros) zero = min((uint32_t)p.zeros[row * p.groups + group], 128u);
+    if (blockIdx.x >= p.token_blocks) {            // a thread has 8 groups of a row
+        const uint32_t i = (blockIdx.x - p.token_blocks) * 256u + threadIdx.x, first = i / (uint32_t)p.table_pitch * 8, row = i % (uint32_t)p.table_pitch;
+        if (first >= p.all_groups) return;
+        const int64_t at = (int64_t)row * p.groups + first;
+        T scale[8];
+        uint8_t zero[8];
+        if (row < p.N && first + 8 <= p.groups) {
+            typedef T scales_t __attribute__((ext_vector_type(8), aligned(sizeof(T))));
+            typedef uint8_t zeros_t __attribute__((ext_vector_type(8), aligned(1)));
+            const scales_t s = *reinterpret_cast<const scales_t*>(static_cast<const T*>(p.scales) + at);
+            zeros_t z = {8, 8, 8, 8, 8, 8, 8, 8};
+            if (p.zeros) z = *reinterpret_cast<const zeros_t*>(p.zeros + at);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) scale[q] = s[q], zero[q] = z[q];
+        } else {
+#pragma unroll
+            for (uint32_t q = 0; q < 8; ++q) {
+                const bool in = row < p.N && first + q < p.groups;
+                scale[q] = in ? static_cast<const T*>(p.scales)[at + q] : (T)0;
+                zero[q] = in && p.zeros ? p.zeros[at + q] : (uint8_t)8;
+            }
         }
-        const float less = -16.0f - (float)zero;
-        if constexpr (sizeof(T) == 2) reinterpret_cast<uint32_t*>(p.table)[i] = __float_as_uint(scale) | __float_as_uint(less) >> 16;
-        else reinterpret_cast<f32x2_t*>(p.table)[i] = f32x2_t{scale, less};
+#pragma unroll
+        for (uint32_t q = 0; q < 8; ++q) {
+            if (first + q >= p.all_groups) continue;
+            const int64_t to = (int64_t)(first + q) * p.table_pitch + row;
+            const float less = -16.0f - (float)min((uint32_t)zero[q], 128u);
+            if constexpr (sizeof(T) == 2) reinterpret_cast<uint32_t*>(p.table)[to] = (uint32_t)scale[q] << 16 | __float_as_uint(less) >> 16;
+            else reinterpret_cast<f32x2_t*>(p.table)[to] = f32x2_t{scale[q], less};
+        }
         return;
     }
-    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / p.units;
-    const uint32_t unit = (uint32_t)(u - row * p.units);
+    const uint32_t u = blockIdx.x * 256u + threadIdx.x;
+    const int64_t row = u / p.units;
+    const uint32_t unit = u % p.units;
     if (row >= p.n) return;                        // (rows are whole groups: no group is divided)
     const unsigned char* at = p.x + row * p.x_pitch + (size_t)unit * 8 * sizeof(T);
     const int left = (int)p.k - (int)unit * 8;
@@ -329,25 +346,29 @@ struct FourTile : LinearArgs {                     // (x: the parts; k: bytes of
     uint32_t groups;
 };
 
-template <int PARTS, int GW, int FA, int FB, int WN> struct FourTileShape {
+// D steps in LDS.  The table's and the sums' pieces of 1024 bytes are dealt out to the wavefronts, AUX for each.
+template <int PARTS, int GW, int FA, int FB, int WN, int D> struct FourTileShape {
     static constexpr int TM = 16 * FA, TN = 16 * FB * WN, G = 4 / GW;
-    static constexpr int X = TM * 2 * kStep, CODES = TN * kStep / 2, ROW = PARTS == 1 ? 4 : 8, TABLE = G * TN * ROW, SUMS = 1024;
-    static constexpr int kLds = 2 * (X + CODES + TABLE + SUMS), kRowBytes = WN * 16 * FB * 16 * 4;
+    static constexpr int X = TM * 2 * kStep, CODES = TN * kStep / 2, ROW = PARTS == 1 ? 4 : 8, PIECE = TN * ROW < 1024 ? TN * ROW : 1024;   // (of a group's rows in one load)
+    static constexpr int TABLE = (G * TN * ROW + 1023) / 1024 * 1024, SUMS = 1024, LX = X / (1024 * WN), LC = CODES / (1024 * WN), LT = TABLE / 1024;
+    static constexpr int AUX = (LT + 1 + WN - 1) / WN, LOADS = LX + LC + AUX;
+    static constexpr int kLds = D * (X + CODES + TABLE + SUMS), kRowBytes = WN * 16 * FB * 16 * 4;
     static constexpr int RB = FA * kRowBytes <= kLds ? FA : FA % 2 == 0 && 2 * kRowBytes <= kLds ? 2 : 1;   // row blocks behind the products
-    static_assert(X % (1024 * WN) == 0 && CODES % (1024 * WN) == 0 && TABLE % 1024 == 0 && RB * kRowBytes <= kLds && G * TM * 4 <= SUMS && kLds <= kLdsBytes, "slots");
+    static_assert(X % (1024 * WN) == 0 && CODES % (1024 * WN) == 0 && RB * kRowBytes <= kLds && G * TM * 4 <= SUMS && kLds <= kLdsBytes, "slots");
+    static_assert(D >= 2 && (D - 2) * LOADS <= 63 && (PARTS == 1 || D == 2), "steps under way");
 };
 
-// A tile of TM = 16 FA tokens x TN = 16 FB WN rows of W.  A step of 128 columns - tokens, codes, table, sums - goes to LDS, which has room for two, and two blocks
+// A tile of TM = 16 FA tokens x TN = 16 FB WN rows of W.  A step of 128 columns - tokens, codes, table, sums - goes to LDS, D - 1 steps ahead, and two blocks
 // are on a CU: while one waits for its step the other multiplies.  A wavefront has 16 FB rows to itself, makes the codes of 16 of them into bf16
 // and multiplies them with all tokens, group by group: a group's sum begins with -(16 + zero) times the sum of the token's columns, and is
 // added to the result with the group's scale.
-template <int PARTS, int GW, int FA, int FB, int WN>
+template <int PARTS, int GW, int FA, int FB, int WN, int D>
 __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
     typedef typename words_of<GW>::type words_t;
-    typedef FourTileShape<PARTS, GW, FA, FB, WN> S;
-    constexpr int TM = S::TM, TN = S::TN, G = S::G, LX = S::X / (1024 * WN), LC = S::CODES / (1024 * WN), LT = S::TABLE / 1024;
+    typedef FourTileShape<PARTS, GW, FA, FB, WN, D> S;
+    constexpr int TM = S::TM, TN = S::TN, G = S::G, LX = S::LX, LC = S::LC, LT = S::LT;
     extern __shared__ __align__(1024) unsigned char lds[];
-    unsigned char *at_x = lds, *at_codes = at_x + 2 * S::X, *at_table = at_codes + 2 * S::CODES, *at_sums = at_table + 2 * S::TABLE;
+    unsigned char *at_x = lds, *at_codes = at_x + D * S::X, *at_table = at_codes + D * S::CODES, *at_sums = at_table + D * S::TABLE;
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), low = lane & 15, high = lane >> 4;
     uint32_t t, in_range;
     if (!number_of(blockIdx.x, (uint32_t)(p.tiles_m * p.tiles_n * p.splits), t)) return;
@@ -381,25 +402,36 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
         const int row = wave * (TN / WN) + 16 * i + (lane >> 2);
         off_codes[i] = (row < rows_w ? (uint32_t)row * row_bytes : kNowhere) + (uint32_t)(lane & 3) * 16u;
     }
-    const uint32_t off_sums = high < G && 4 * low < b.rows ? (uint32_t)(high * p.sum_pitch + 4 * low) * 4u : kNowhere;
+    const uint32_t off_sums = high < G && 4 * low < min(b.rows, TM) ? (uint32_t)(high * p.sum_pitch + 4 * low) * 4u : kNowhere;
     const i32x4_t rc = buffer_of(p.W + b.n0 * row_bytes, (uint32_t)rows_w * row_bytes);
-    auto load_x = [&](uint32_t step, int part, uint32_t slot) {
-        const i32x4_t r = buffer_of(p.x + ((int64_t)part * p.n + b.first) * p.k, (uint32_t)b.rows * p.k);
+    // (live: past the last step nothing is fetched, from empty buffers)
+    auto load_x = [&](uint32_t step, int part, uint32_t slot, bool live) {
+        i32x4_t r = buffer_of(p.x + ((int64_t)part * p.n + b.first) * p.k, (uint32_t)b.rows * p.k);
+        r.z = live ? r.z : 0;
 #pragma unroll
-        for (int i = 0; i < LX; ++i) load_to_lds(base + slot * S::X + (uint32_t)wave * (S::X / WN) + i * 1024u, off_x[i], r, step * (2 * kStep));
+        for (int i = 0; i < LX; ++i) load_to_lds(base + slot * S::X + (uint32_t)wave * (S::X / WN) + i * 1024u, off_x[i], r, live ? step * (2 * kStep) : 0u);
     };
-    auto load_codes = [&](uint32_t step, uint32_t slot) {
+    auto load_codes = [&](uint32_t step, uint32_t slot, bool live) {
+        i32x4_t r = rc;
+        r.z = live ? r.z : 0;
 #pragma unroll
-        for (int i = 0; i < LC; ++i) load_to_lds(base + 2 * S::X + slot * S::CODES + (uint32_t)wave * (S::CODES / WN) + i * 1024u, off_codes[i], rc, step * (kStep / 2));
-        const i32x4_t rt = buffer_of(p.table + ((int64_t)step * G * p.table_pitch + b.n0) * S::ROW, (uint32_t)(((G - 1) * p.table_pitch + TN) * S::ROW));
-        for (int i = wave; i < LT; i += WN) {
-            const uint32_t group = (uint32_t)i / (LT / G), in = (uint32_t)i % (LT / G);
-            const uint32_t to = (uint32_t)uniform((int)(base + 2 * S::X + 2 * S::CODES + slot * S::TABLE + (uint32_t)i * 1024u));
-            load_to_lds(to, (uint32_t)(group * p.table_pitch) * S::ROW + in * 1024u + lane * 16u, rt, 0);
-        }
-        if (wave == WN - 1) {
-            const i32x4_t rs = buffer_of(p.sums + (int64_t)step * G * p.sum_pitch + b.first, (uint32_t)((G - 1) * p.sum_pitch + p.sum_pitch - b.first) * 4u);
-            load_to_lds(base + 2 * (S::X + S::CODES + S::TABLE) + slot * S::SUMS, off_sums, rs, 0);
+        for (int i = 0; i < LC; ++i)
+            load_to_lds(base + D * S::X + slot * S::CODES + (uint32_t)wave * (S::CODES / WN) + i * 1024u, off_codes[i], r, live ? step * (kStep / 2) : 0u);
+#pragma unroll
+        for (int i = 0; i < S::AUX; ++i) {
+            const int piece = wave + i * WN;
+            if (piece < LT) {
+                // lane -> 16 bytes of the step's groups, one behind the other
+                const uint32_t in = (uint32_t)piece * 1024u + (uint32_t)lane * 16u, group = in / (TN * S::ROW), at = in % (TN * S::ROW);
+                i32x4_t rt = buffer_of(p.table + ((int64_t)step * G * p.table_pitch + b.n0) * S::ROW, (uint32_t)(((G - 1) * p.table_pitch + TN) * S::ROW));
+                rt.z = live ? rt.z : 0;
+                load_to_lds((uint32_t)uniform((int)(base + D * (S::X + S::CODES) + slot * S::TABLE + (uint32_t)piece * 1024u)),
+                            group < (uint32_t)G ? group * (uint32_t)p.table_pitch * S::ROW + at : kNowhere, rt, 0);
+            } else {
+                i32x4_t rs = buffer_of(p.sums + (int64_t)step * G * p.sum_pitch + b.first, (uint32_t)((G - 1) * p.sum_pitch + p.sum_pitch - b.first) * 4u);
+                rs.z = live ? rs.z : 0;
+                load_to_lds(base + D * (S::X + S::CODES + S::TABLE) + slot * S::SUMS, off_sums, rs, 0);
+            }
         }
     };
     const Sixteen sixteen;
@@ -455,24 +487,48 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
             }
         }
     };
-    if (b.nk > 0) {
-        load_x(step_of(0), 0, 0);
-        load_codes(step_of(0), 0);
-    }
-    uint32_t x_slot = 0;
+    auto arrived = [&]() {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((D - 2) * S::LOADS) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    if constexpr (PARTS == 1) {
+        auto load_step = [&](int at, uint32_t slot) {
+            const bool live = at < b.nk;
+            const uint32_t step = live ? step_of(at) : 0u;
+            load_x(step, 0, slot, live);
+            load_codes(step, slot, live);
+        };
 #pragma unroll 1
-    for (int at = 0; at < b.nk; ++at) {
-        const uint32_t slot = (uint32_t)at & 1;
+        for (int at = 0; at < D - 1; ++at) load_step(at, (uint32_t)at);
+        uint32_t slot = 0, free_slot = D - 1;
 #pragma unroll 1
-        for (int part = 0; part < PARTS; ++part) {
-            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            if (part + 1 < PARTS) load_x(step_of(at), part + 1, x_slot ^ 1);
-            else if (at + 1 < b.nk) load_x(step_of(at + 1), 0, x_slot ^ 1);
-            if (part == 0 && at + 1 < b.nk) load_codes(step_of(at + 1), slot ^ 1);
-            products(x_slot, slot, part == 0);
-            x_slot ^= 1;
+        for (int at = 0; at < b.nk; ++at) {
+            arrived();
+            load_step(at + D - 1, free_slot);
+            products(slot, slot, true);
+            free_slot = slot;
+            slot = slot + 1 == D ? 0 : slot + 1;
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
+        if (b.nk > 0) {
+            load_x(step_of(0), 0, 0, true);
+            load_codes(step_of(0), 0, true);
+        }
+        uint32_t x_slot = 0;
+#pragma unroll 1
+        for (int at = 0; at < b.nk; ++at) {
+            const uint32_t slot = (uint32_t)at & 1;
+#pragma unroll 1
+            for (int part = 0; part < PARTS; ++part) {
+                arrived();
+                if (part + 1 < PARTS) load_x(step_of(at), part + 1, x_slot ^ 1, true);
+                else if (at + 1 < b.nk) load_x(step_of(at + 1), 0, x_slot ^ 1, true);
+                if (part == 0 && at + 1 < b.nk) load_codes(step_of(at + 1), slot ^ 1, true);
+                products(x_slot, slot, part == 0);
+                x_slot ^= 1;
+            }
         }
     }
     __syncthreads();
@@ -498,17 +554,29 @@ template <typename F> void for_four(bool f32, int group, int rows, F f) {
     else with_group(bf16_t{});
 }
 
-// f(parts of a token, group words, token blocks, row blocks of a wavefront, wavefronts)
-template <typename F> void for_four_tile(bool f32, int group, F f) {
+// The tiles: tokens, rows of W, steps in LDS (for tokens in fp32 two)
+struct FourShape { int m, n, steps; };
+constexpr FourShape kFourShape[] = {{16, 64, 6}, {32, 64, 5}, {64, 64, 3}, {64, 256, 2}};
+constexpr int kFourShapes = sizeof(kFourShape) / sizeof(FourShape);
+// f(parts of a token, group words, token blocks, row blocks of a wavefront, wavefronts, steps in LDS)
+template <typename F> void for_four_tile(bool f32, int group, int shape, F f) {
+    auto with_shape = [&](auto parts, auto gw) {
+        constexpr bool deep = decltype(parts)::value == 1;
+        switch (shape) {
+            case 0: f(parts, gw, num<1>{}, num<1>{}, num<4>{}, num<deep ? 6 : 2>{}); break;
+            case 1: f(parts, gw, num<2>{}, num<1>{}, num<4>{}, num<deep ? 5 : 2>{}); break;
+            case 2: f(parts, gw, num<4>{}, num<1>{}, num<4>{}, num<deep ? 3 : 2>{}); break;
+            default: f(parts, gw, num<4>{}, num<4>{}, num<4>{}, num<2>{}); break;
+        }
+    };
     auto with_parts = [&](auto gw) {
-        if (f32) f(num<3>{}, gw, num<4>{}, num<4>{}, num<4>{});
-        else f(num<1>{}, gw, num<4>{}, num<4>{}, num<4>{});
+        if (f32) with_shape(num<3>{}, gw);
+        else with_shape(num<1>{}, gw);
     };
     if (group == 32) with_parts(num<1>{});
     else if (group == 64) with_parts(num<2>{});
     else with_parts(num<4>{});
 }
-constexpr int kTileTokens = 64, kTileRows = 256;
 
 tardis_status_t init_four() {
     static td_once once;
@@ -521,12 +589,13 @@ tardis_status_t init_four() {
                         ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(linear4_kernel<decltype(type), gw, rt>), hipFuncAttributeMaxDynamicSharedMemorySize,
                                                   kLdsBytes) == hipSuccess;
                     });
-                for_four_tile(f32, group, [&](auto parts, auto gw, auto fa, auto fb, auto wn) {
-                    typedef FourTileShape<parts, gw, fa, fb, wn> S;
-                    ok &= S::TM == kTileTokens && S::TN == kTileRows;
-                    ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(linear4_tile_kernel<parts, gw, fa, fb, wn>),
-                                              hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds) == hipSuccess;
-                });
+                for (int shape = 0; shape < kFourShapes; ++shape)
+                    for_four_tile(f32, group, shape, [&](auto parts, auto gw, auto fa, auto fb, auto wn, auto d) {
+                        typedef FourTileShape<parts, gw, fa, fb, wn, d> S;
+                        ok &= S::TM == kFourShape[shape].m && S::TN == kFourShape[shape].n;
+                        ok &= hipFuncSetAttribute(reinterpret_cast<const void*>(linear4_tile_kernel<parts, gw, fa, fb, wn, d>),
+                                                  hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds) == hipSuccess;
+                    });
             }
         return ok ? TARDIS_OK : TARDIS_ERR_HIP;
     });
@@ -535,29 +604,36 @@ tardis_status_t init_four() {
 // How a call is done, by its sizes and the working memory that it has
 struct FourPlan {
     bool tiles;
-    int splits, slices;
+    int shape, splits, slices;
     int64_t units, all_groups, sum_pitch, table_pitch, at_sums, at_table, at_part, work;
 };
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 FourPlan plan_four(const tardis_linear_4bit_desc* d, int64_t n, int64_t room) {
     FourPlan p{};
-    if (n <= 16) return p;
     const bool f32 = d->dtype == TARDIS_F32;
-    const int64_t steps = (d->n_in + kStep - 1) / kStep, tiles = ((n + kTileTokens - 1) / kTileTokens) * ((d->n_out + kTileRows - 1) / kTileRows);
+    // up to 16 tokens: every block of linear4_kernel has them whole, so not where that is long (16 tokens 16384 -> 4096: 512 KB, 29 us; as tiles in 8 ranges 25)
+    if (n <= 16 && n * d->n_in * (f32 ? 6 : 2) <= 300 * 1024) return p;
+    const int64_t steps = (d->n_in + kStep - 1) / kStep;
     p.units = steps * (kStep / 8);
     p.all_groups = steps * (kStep / d->group);
     p.sum_pitch = round_up(n, 4);
-    p.table_pitch = round_up(d->n_out, kTileRows);
+    p.table_pitch = round_up(d->n_out, 256);
     p.at_sums = round_up((f32 ? 3 : 1) * n * p.units * 16, 256);
     p.at_table = p.at_sums + round_up(p.all_groups * p.sum_pitch * 4, 256);
     p.at_part = p.at_table + p.all_groups * p.table_pitch * (f32 ? 8 : 4);
     // (offsets of a tile's rows, of four groups' sums and of the table are 32 bits)
-    if (tiles >= 1 << 21 || p.units * 16 * kTileTokens >= kNowhere || 4 * p.sum_pitch * 4 >= kNowhere || n * p.units + p.all_groups * p.table_pitch >= kMostThreads ||
-        p.at_part > room)
-        return FourPlan{};
+    if (p.units * 16 * 64 >= kNowhere || 4 * p.sum_pitch * 4 >= kNowhere || n * p.units + p.all_groups * p.table_pitch >= kMostThreads || p.at_part > room) return FourPlan{};
+    auto tiles_of = [&](const FourShape& t) { return ((n + t.m - 1) / t.m) * ((d->n_out + t.n - 1) / t.n); };
+    // (100 tokens 4096 -> 16384, us: 64 x 64 in one range 37, 64 x 256 in two 42; 300 tokens 84 and 77; 1000 tokens 4096 -> 4096 72 and 61)
+    p.shape = n <= 16 ? 0 : n <= 32 ? 1 : n <= 64 || tiles_of(kFourShape[3]) < 256 ? 2 : 3;
+    const int64_t tiles = tiles_of(kFourShape[p.shape]);
+    if (tiles >= 1 << 21) return FourPlan{};
+    // (256 CUs; a range is 8 steps at least, and where it has many a second block on each CU is worth the longer join)
     p.splits = 1;
-    while (p.splits < 16 && tiles * p.splits * 2 <= 512 && steps >= 4 * p.splits * 2 && p.at_part + 2 * p.splits * n * d->n_out * 4 <= room) p.splits *= 2;
+    while (p.splits < 16 && (tiles * p.splits <= 128 || (tiles * p.splits <= 256 && steps >= 32 * p.splits)) && steps >= 16 * p.splits &&
+           p.at_part + 2 * p.splits * n * d->n_out * 4 <= room)
+        p.splits *= 2;
     p.slices = (int)((steps + p.splits - 1) / p.splits);
     p.work = p.at_part + (p.splits > 1 ? p.splits * n * d->n_out * 4 : 0);
     p.tiles = true;
@@ -596,8 +672,9 @@ tardis_status_t run_tiles(const tardis_linear_4bit_desc* d, const FourPlan& plan
     p.k = (uint32_t)(plan.units * 16);
     p.act = d->act == TARDIS_ACT_GELU_ERF && d->out_dtype == TARDIS_BF16 && !residual ? kActGelu16 : d->act;
     p.out_f32 = d->out_dtype == TARDIS_F32;
-    p.tiles_m = (int)((n + kTileTokens - 1) / kTileTokens);
-    p.tiles_n = (int)((d->n_out + kTileRows - 1) / kTileRows);
+    const FourShape& shape = kFourShape[plan.shape];
+    p.tiles_m = (int)((n + shape.m - 1) / shape.m);
+    p.tiles_n = (int)((d->n_out + shape.n - 1) / shape.n);
     p.splits = plan.splits;
     p.slices = plan.slices;
     p.sums = t.sums;
@@ -610,13 +687,13 @@ tardis_status_t run_tiles(const tardis_linear_4bit_desc* d, const FourPlan& plan
         q.part = reinterpret_cast<float*>(work + plan.at_part);
         q.act = TARDIS_ACT_IDENTITY;
     }
-    const dim3 prepare(t.token_blocks + (unsigned)((plan.all_groups * plan.table_pitch + 255) / 256));
+    const dim3 prepare(t.token_blocks + (unsigned)(((plan.all_groups + 7) / 8 * plan.table_pitch + 255) / 256));
     const int blocks = (int)(((int64_t)p.tiles_m * p.tiles_n * p.splits + 7) / 8 * 8);
-    for_four_tile(f32, d->group, [&](auto parts, auto gw, auto fa, auto fb, auto wn) {
-        constexpr int bytes = FourTileShape<parts, gw, fa, fb, wn>::kLds, threads = 64 * wn;
+    for_four_tile(f32, d->group, plan.shape, [&](auto parts, auto gw, auto fa, auto fb, auto wn, auto deep) {
+        constexpr int bytes = FourTileShape<parts, gw, fa, fb, wn, deep>::kLds, threads = 64 * wn;
         if constexpr (decltype(parts)::value == 3) hipLaunchKernelGGL((linear4_prepare_kernel<float, gw>), prepare, dim3(256), 0, s, t);
         else hipLaunchKernelGGL((linear4_prepare_kernel<bf16_t, gw>), prepare, dim3(256), 0, s, t);
-        hipLaunchKernelGGL((linear4_tile_kernel<parts, gw, fa, fb, wn>), dim3((unsigned)blocks), dim3(threads), bytes, s, q);
+        hipLaunchKernelGGL((linear4_tile_kernel<parts, gw, fa, fb, wn, deep>), dim3((unsigned)blocks), dim3(threads), bytes, s, q);
     });
     if (plan.splits > 1) {
         p.part = q.part;
@@ -661,7 +738,15 @@ tardis_status_t td_linear_4bit(const tardis_linear_4bit_desc* d, const void* x, 
         q.y = static_cast<unsigned char*>(y) + at * p.N * eo;
         if (residual) q.r = static_cast<const unsigned char*>(residual) + at * p.N * eo;
         const int64_t tiles = (p.N + 15) / 16, steps = (d->n_in + kStep - 1) / kStep, groups = kStep / d->group;
-        const int rows = tiles >= 1024 || (tiles >= 512 && q.n > 4) ? 4 : tiles >= 512 ? 2 : 1;
+        // row tiles of a block: 256 CUs have one or two blocks each, which take about 5 us and what their codes (25 bytes a ns and CU) and tokens (50) take
+        int rows = 1;
+        double least = 1e300;
+        for (int r = 1; r <= 4; r *= 2) {
+            const int64_t blocks = (tiles + r - 1) / r, tokens = (f32 ? 3 : 1) * q.n * steps * (2 * kStep), bytes = kWaves * 8 * 1024 + tokens + steps * groups * 16 * r * (f32 ? 8 : 4);
+            const int64_t on_cu = std::min<int64_t>(2 * bytes <= kLdsBytes ? 2 : 1, (blocks + 255) / 256);
+            const double us = (double)((blocks + 256 * on_cu - 1) / (256 * on_cu)) * (5.0 + (double)on_cu * ((double)(r * 16 * steps * (kStep / 2)) / 25e3 + (double)tokens / 50e3));
+            if (us < least) least = us, rows = r;
+        }
         for_four(f32, d->group, rows, [&](auto type, auto gw, auto rt) {
             typedef FourBlock<decltype(type), rt> S;
             const int64_t room = kLdsBytes - S::lds(q.n, 0, groups), each = S::lds(q.n, 1, groups) - S::lds(q.n, 0, groups);

@@ -469,6 +469,17 @@ def tardis_moe_combine(z, place, weights, residual=None, out_dtype=None, y=None,
 
 # ---------------------------------------------------------------- norms, layers in 8 and 4 bits
 FP8 = torch.float8_e4m3fn
+
+
+def _at(t):
+    """Where a tensor is (None: nowhere)"""
+    return None if t is None else t.data_ptr()
+
+
+def _empty1(n, dtype, device):
+    return torch.empty_strided((n,), (1,), dtype=dtype, device=device)
+
+
 _OUT_CODE = {torch.float32: F32, torch.bfloat16: BF16, FP8: FP8_E4M3}
 
 
@@ -482,30 +493,29 @@ def tardis_rms_norm(x, weight=None, residual=None, eps: float = 1e-6, out_dtype=
             return tardis_rms_norm(x, weight, residual, eps, out_dtype, sum, y, scales)
     d = x.shape[-1]
     n, pitch = _rows(x, d)
-    dt, dev = x.dtype, x.get_device()
-    out_dtype = out_dtype or dt
+    dt, device, dev = x.dtype, x.device, x.get_device()
+    if out_dtype is None:
+        out_dtype = dt
     codes = out_dtype == FP8
     assert weight is None or (weight.is_contiguous() and weight.dtype == dt and weight.numel() == d and weight.get_device() == dev)
-    assert residual is None or (residual.is_contiguous() and residual.dtype == dt and residual.shape == (n, d) and residual.get_device() == dev)
-    assert codes or scales is None
-    if residual is not None and sum is None:
-        sum = _empty(n, d, dt, x.device)
-    elif sum is not None:
-        assert sum.is_contiguous() and sum.dtype == dt and sum.shape == (n, d) and sum.get_device() == dev
+    if residual is not None:
+        assert residual.is_contiguous() and residual.dtype == dt and residual.shape == (n, d) and residual.get_device() == dev
+        if sum is None:
+            sum = _empty(n, d, dt, device)
+    assert sum is None or (sum.is_contiguous() and sum.dtype == dt and sum.shape == (n, d) and sum.get_device() == dev)
     if y is None:
-        y = _empty(n, d, out_dtype, x.device)
+        y = _empty(n, d, out_dtype, device)
     else:
         assert y.is_contiguous() and y.dtype == out_dtype and y.shape == (n, d) and y.get_device() == dev
     if codes and scales is None:
-        scales = torch.empty_strided((n,), (1,), dtype=torch.float32, device=x.device)
-    elif codes:
-        assert scales.is_contiguous() and scales.dtype == torch.float32 and scales.shape == (n,) and scales.get_device() == dev
-    desc = tardis_norm_desc(d, _DTYPE_CODE[dt], _OUT_CODE[out_dtype], eps, 0, None if weight is None else weight.data_ptr())
-    _check(lib().tardis_rms_norm(desc, x.data_ptr(), n, pitch, _ptr(residual), _ptr(sum), y.data_ptr(), _ptr(scales), _stream(None)), "tardis_rms_norm")
-    outs = (y, scales) if codes else (y,)
-    if residual is not None:
-        outs += (sum,)
-    return outs if len(outs) > 1 else y
+        scales = _empty1(n, torch.float32, device)
+    else:
+        assert scales is None or (codes and scales.is_contiguous() and scales.dtype == torch.float32 and scales.shape == (n,) and scales.get_device() == dev)
+    desc = tardis_norm_desc(d, _DTYPE_CODE[dt], _OUT_CODE[out_dtype], eps, 0, _at(weight))
+    _check(lib().tardis_rms_norm(desc, x.data_ptr(), n, pitch, _at(residual), _at(sum), y.data_ptr(), _at(scales), _stream(None)), "tardis_rms_norm")
+    if codes:
+        return (y, scales) if residual is None else (y, scales, sum)
+    return y if residual is None else (y, sum)
 
 
 def tardis_fp8_rows(x, codes=None, scales=None, stream=None):
@@ -521,7 +531,7 @@ def tardis_fp8_rows(x, codes=None, scales=None, stream=None):
     else:
         assert codes.is_contiguous() and codes.dtype == FP8 and codes.shape == (n, d) and codes.get_device() == dev
     if scales is None:
-        scales = torch.empty_strided((n,), (1,), dtype=torch.float32, device=x.device)
+        scales = _empty1(n, torch.float32, x.device)
     else:
         assert scales.is_contiguous() and scales.dtype == torch.float32 and scales.shape == (n,) and scales.get_device() == dev
     _check(lib().tardis_fp8_rows(x.data_ptr(), n, d, pitch, _DTYPE_CODE[x.dtype], codes.data_ptr(), scales.data_ptr(), _stream(None)), "tardis_fp8_rows")
@@ -569,10 +579,10 @@ def tardis_linear_fp8(x, x_scales, W, W_scales, b=None, act: str = "identity", r
     assert W_scales is None or (W_scales.is_contiguous() and W_scales.dtype == torch.float32 and W_scales.numel() == n_out and W_scales.get_device() == dev)
     y = _layer_outputs(n, n_out, out_dtype, b, residual, y, x)
     out, a, x_at, W_at = _DTYPE_CODE[out_dtype], ACT[act], x.data_ptr(), W.data_ptr()
-    desc = tardis_linear_fp8_desc(n_in, n_out, out, a, W_at, None if W_scales is None else W_scales.data_ptr(), None if b is None else b.data_ptr())
+    desc = tardis_linear_fp8_desc(n_in, n_out, out, a, W_at, _at(W_scales), _at(b))
     bytes_ = _fp8_work_bytes(n_in, n_out, out, a, n, pitch, x_at & 15, W_at & 15)
     work = torch.empty(bytes_, dtype=torch.uint8, device=x.device) if bytes_ else None
-    _check(lib().tardis_linear_fp8(desc, x_at, _ptr(x_scales), n, pitch, _ptr(residual), y.data_ptr(), _ptr(work), bytes_, _stream(None)), "tardis_linear_fp8")
+    _check(lib().tardis_linear_fp8(desc, x_at, _at(x_scales), n, pitch, _at(residual), y.data_ptr(), _at(work), bytes_, _stream(None)), "tardis_linear_fp8")
     return y
 
 
@@ -604,8 +614,8 @@ def tardis_linear_4bit(x, W, scales, zeros=None, b=None, group: int = 128, act: 
     assert zeros is None or (zeros.is_contiguous() and zeros.dtype == torch.uint8 and zeros.shape == (n_out, groups) and zeros.get_device() == dev)
     y = _layer_outputs(n, n_out, out_dtype, b, residual, y, x)
     sizes = (n_in, n_out, _DTYPE_CODE[dt], _DTYPE_CODE[out_dtype], ACT[act], group)
-    desc = tardis_linear_4bit_desc(*sizes, W.data_ptr(), scales.data_ptr(), None if zeros is None else zeros.data_ptr(), None if b is None else b.data_ptr())
+    desc = tardis_linear_4bit_desc(*sizes, W.data_ptr(), scales.data_ptr(), _at(zeros), _at(b))
     bytes_ = _four_work_bytes(*sizes, n, pitch)
     work = torch.empty(bytes_, dtype=torch.uint8, device=x.device) if bytes_ else None
-    _check(lib().tardis_linear_4bit(desc, x.data_ptr(), n, pitch, _ptr(residual), y.data_ptr(), _ptr(work), bytes_, _stream(None)), "tardis_linear_4bit")
+    _check(lib().tardis_linear_4bit(desc, x.data_ptr(), n, pitch, _at(residual), y.data_ptr(), _at(work), bytes_, _stream(None)), "tardis_linear_4bit")
     return y
