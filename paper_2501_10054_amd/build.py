@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libtardis.so")
 SIGMA_PROBE = os.path.join(OBJ, "sigma_probe.so")
 LINEAR_PROBE = os.path.join(OBJ, "linear_probe.so")
 
-SOURCES = ["api.hip", "decode.hip", "experts.hip", "forward.hip", "gemm.hip", "linear.hip", "linear_4bit.hip", "linear_bf16.hip", "linear_f32.hip", "linear_fp8.hip", "linear_quad.hip", "norm.hip", "offline.hip", "prefill.hip", "stack.hip", "stream.hip"]
+SOURCES = ["api.hip", "decode.hip", "experts.hip", "forward.hip", "gemm.hip", "linear.hip", "linear_4bit.hip", "linear_bf16.hip", "linear_f32.hip", "linear_fp8.hip", "linear_fp8_quad.hip", "linear_quad.hip", "norm.hip", "offline.hip", "prefill.hip", "stack.hip", "stream.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-fPIC", "-std=c++17", "-Wall", "-Wno-unused-function",

@@ -55,6 +55,8 @@ constexpr LinearShape kLinearQuad[] = {{256, 256, 128}, {192, 256, 128}, {256, 1
 // (rows with which its tiles of groups are full, if the kernel decides so)
 constexpr int linear_least_rows(int m) { return m == 256 ? 192 : m; }
 constexpr int kLinearQuads = sizeof(kLinearQuad) / sizeof(LinearShape);
+constexpr LinearShape kLinearQuadFp8[] = {{256, 256, 128}, {256, 128, 128}};
+constexpr int kLinearQuadsFp8 = sizeof(kLinearQuadFp8) / sizeof(LinearShape);
 
 // sums of ranges and the epilogue, with a bias of y's type (scales: as above)
 void td_linear_join(const LinearArgs& p, hipStream_t s);
@@ -63,6 +65,8 @@ void td_linear_launch_quad(const LinearArgs& p, bool grouped, int shape, int blo
 tardis_status_t td_linear_init_bf16();
 tardis_status_t td_linear_init_f32();
 void td_linear_launch_bf16(const LinearArgs& p, bool grouped, bool direct, int shape, int blocks, hipStream_t s);
+tardis_status_t td_linear_init_fp8_quad();
+void td_linear_launch_fp8_quad(const LinearArgs& p, int shape, int blocks, hipStream_t s);
 tardis_status_t td_linear_init_fp8();
 void td_linear_launch_fp8(const LinearArgs& p, bool direct, int shape, int blocks, hipStream_t s);
 void td_linear_launch_f32(const LinearArgs& p, bool grouped, bool direct, int shape, int blocks, hipStream_t s);

@@ -116,9 +116,10 @@ constexpr Rate kRateStaged[] = {{2, 0.246f, 0.231f, 4.77f, 3.34f}, {1, 0.389f, 0
 constexpr Rate kRateStagedF32[] = {{2, 0.104f, 0.250f, 4.45f, 4.01f}, {1, 0.377f, 0.377f, 4.45f, 4.01f}, {2, 0.053f, 0.305f, 4.21f, 4.46f},
                                    {2, 0.556f, 0.550f, 4.53f, 5.00f}, {1, 2.042f, 2.042f, 6.55f, 4.71f}};
 constexpr Rate kRateFp8[] = {{2, 0.244f, 0.223f, 3.80f, 5.50f}, {2, 0.415f, 0.400f, 3.74f, 5.51f}, {1, 0.369f, 0.369f, 4.39f, 5.47f}, {1, 0.399f, 0.399f, 4.31f, 4.24f},
-                             {1, 0.450f, 0.450f, 4.53f, 5.33f}, {1, 1.000f, 1.000f, 6.21f, 5.25f}, {2, 0.725f, 0.639f, 4.82f, 3.77f}, {5, 0.489f, 0.262f, 3.07f, 3.94f}};
+                             {1, 0.450f, 0.450f, 4.53f, 5.33f}, {1, 1.000f, 1.000f, 6.21f, 5.25f}, {2, 0.725f, 0.639f, 4.82f, 3.77f}, {5, 0.489f, 0.262f, 3.07f, 3.94f},
+                             {1, 0.903f, 0.903f, 14.60f, 3.45f}, {1, 0.788f, 0.788f, 7.70f, 3.77f}};
 constexpr Rate kRateStagedFp8[] = {{2, 0.246f, 0.231f, 4.77f, 3.34f}, {2, 0.176f, 0.227f, 4.35f, 4.73f}, {2, 0.228f, 0.214f, 4.34f, 2.79f}, {1, 0.560f, 0.560f, 7.05f, 2.77f}};
-static_assert(sizeof(kRateFp8) / sizeof(Rate) == kLinearShapesFp8 && sizeof(kRateStagedFp8) / sizeof(Rate) == kLinearStagedShapesFp8, "a rate for each tile");
+static_assert(sizeof(kRateFp8) / sizeof(Rate) == kLinearShapesFp8 + kLinearQuadsFp8 && sizeof(kRateStagedFp8) / sizeof(Rate) == kLinearStagedShapesFp8, "a rate for each tile");
 static_assert(sizeof(kRate) / sizeof(Rate) == kLinearShapes + kLinearQuads && sizeof(kRateF32) / sizeof(Rate) == kLinearShapes &&
               sizeof(kRateStaged) / sizeof(Rate) == kLinearStagedShapes && sizeof(kRateStagedF32) / sizeof(Rate) == kLinearStagedShapes, "a rate for each tile");
 // one more launch (2.5 on the GPU; callers that are not a graph wait for their host); a byte copied, of partial sums and outputs joined; sigma of an element of a tile, of eight wavefronts and of four
@@ -142,10 +143,11 @@ struct Plan {
 
 // (es: bytes of an element - 1 e4m3, 2 bf16, 4 fp32)
 int shapes_below_quads(bool direct, int es) { return es == 1 ? (direct ? kLinearShapesFp8 : kLinearStagedShapesFp8) : direct ? kLinearShapes : kLinearStagedShapes; }
-int shapes_of(bool direct, int es) { return shapes_below_quads(direct, es) + (direct && es == 2 ? kLinearQuads : 0); }
+// (e4m3: with outputs in bf16)
+int shapes_of(bool direct, int es, int eo) { return shapes_below_quads(direct, es) + (!direct || es == 4 ? 0 : es == 2 ? kLinearQuads : eo == 2 ? kLinearQuadsFp8 : 0); }
 bool is_quad(bool direct, int es, int s) { return direct && s >= shapes_below_quads(direct, es); }
 const LinearShape& shape_of(bool direct, int es, int s) {
-    if (is_quad(direct, es, s)) return kLinearQuad[s - shapes_below_quads(direct, es)];
+    if (is_quad(direct, es, s)) return (es == 1 ? kLinearQuadFp8 : kLinearQuad)[s - shapes_below_quads(direct, es)];
     return es == 1 ? (direct ? kLinearShapeFp8[s] : kLinearStagedFp8[s]) : direct ? kLinearShape[s] : kLinearStaged[s];
 }
 const Rate& rate_of(bool direct, int es, int s) {
@@ -188,7 +190,7 @@ Plan make_plan(const Call& c, int64_t room) {
             if (p.pitch >= 1 << 23 || p.k >= 1 << 23 || (c.gather && (c.x_rows - 1) * p.pitch + p.k >= (int64_t)kNowhere)) continue;
         }
         if (p.at_part > room) continue;
-        for (int s = 0; s < shapes_of(p.direct, c.es); ++s) {
+        for (int s = 0; s < shapes_of(p.direct, c.es, c.eo); ++s) {
             const bool quad = is_quad(p.direct, c.es, s);
             if (c.es != 1 && !quad && !linear_has(c.es, p.direct, c.experts > 0, s)) continue;
             const LinearShape& t = shape_of(p.direct, c.es, s);
@@ -254,7 +256,7 @@ tardis_status_t run(LinearArgs p, const Call& c, void* work, int64_t work_bytes,
     p.splits = plan.splits;
     p.slices = plan.slices;
     const int64_t tiles = most_tiles_m(c, quad, t) * p.tiles_n * plan.splits;
-    if (fp8) TD_TRY(td_linear_init_fp8());
+    if (fp8) TD_TRY(quad ? td_linear_init_fp8_quad() : td_linear_init_fp8());
     else if (f32) TD_TRY(td_linear_init_f32());
     else TD_TRY(quad ? td_linear_init_quad() : td_linear_init_bf16());
     unsigned char* memory = static_cast<unsigned char*>(work);
@@ -283,7 +285,8 @@ tardis_status_t run(LinearArgs p, const Call& c, void* work, int64_t work_bytes,
         q.act = TARDIS_ACT_IDENTITY;
     }
     const int blocks = (int)((tiles + 7) / 8 * 8);
-    if (fp8) td_linear_launch_fp8(q, plan.direct, plan.shape, blocks, s);
+    if (fp8 && quad) td_linear_launch_fp8_quad(q, plan.shape - kLinearShapesFp8, blocks, s);
+    else if (fp8) td_linear_launch_fp8(q, plan.direct, plan.shape, blocks, s);
     else if (quad) td_linear_launch_quad(q, grouped, plan.shape - kLinearShapes, blocks, s);
     else if (f32) td_linear_launch_f32(q, grouped, plan.direct, plan.shape, blocks, s);
     else td_linear_launch_bf16(q, grouped, plan.direct, plan.shape, blocks, s);

@@ -532,7 +532,7 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
         }
     }
     __syncthreads();
-    finish_linear<four_t, false, WN, FA, FB, 1, WN, 1, S::RB, true>(p, b, acc, lds, tid);
+    finish_linear<four_t, false, WN, FA, FB, 1, WN, 1, S::RB, kAccAcross>(p, b, acc, lds, tid);
 }
 
 template <typename T, int GW, int RT> void launch(const FourArgs& p, unsigned blocks, size_t lds, hipStream_t s) {

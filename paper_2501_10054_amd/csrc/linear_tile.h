@@ -48,6 +48,7 @@ template <> __device__ __forceinline__ void mma_pieces<e4m3_t>(f32x4_t& c, const
 // sums of many products 1e-4 of their root of squares at most, against the 2e-3 by which outputs in bf16 are rounded.  So it is for these
 // outputs, and where tiles are large enough for the matrix cores to count.
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x16_t __attribute__((ext_vector_type(16)));
 __device__ __forceinline__ void mma_two_pieces(f32x4_t& c, const td_u32x4& w0, const td_u32x4& w1, const td_u32x4& x0, const td_u32x4& x1) {
     const i32x8_t w = {(int)w0[0], (int)w0[1], (int)w0[2], (int)w0[3], (int)w1[0], (int)w1[1], (int)w1[2], (int)w1[3]};
     const i32x8_t x = {(int)x0[0], (int)x0[1], (int)x0[2], (int)x0[3], (int)x1[0], (int)x1[1], (int)x1[2], (int)x1[3]};
@@ -221,10 +222,12 @@ template <bool GROUPED> __device__ __forceinline__ int64_t token_of_row(const Li
 // Loads and stores are counted by one counter, in their order: a load in the loop would wait for the stores of the turn before, 1.5 us each
 // (behind the products of a 256 x 256 tile with GELU 21.4 us, as here 15.6, of which the activation's instructions are 8.5).  So which rows are
 // there is known before the first store, bias is waited for there, and residuals are loaded for several rows at once, in a loop of their own.
-// ACROSS: acc[i][j][q] = row (WM i + wm) 16 + 4 (lane / 16) + q, column (wn FB + j) 16 + lane % 16.
-template <typename T, bool GROUPED, int W, int FA, int FB, int WM, int WN, int WK, int RB, bool ACROSS = false>
-__device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearBlock& b, f32x4_t (&acc)[FA][FB], unsigned char* lds, int tid) {
-    static_assert(FA % RB == 0, "all row blocks");
+// That is kAccRows.  kAccAcross: acc[i][j][q] = row (WM i + wm) 16 + 4 (lane / 16) + q, column (wn FB + j) 16 + lane % 16.
+// kAccWide, of 32 x 32 results: acc[i][j][4 g + q] = row (WM (2 i + lane / 16 % 2) + wm) 16 + lane % 16, column (wn FB + 2 j) 16 + 8 g + 4 (lane / 32) + q.
+enum { kAccRows, kAccAcross, kAccWide };
+template <typename T, bool GROUPED, int W, int FA, int FB, int WM, int WN, int WK, int RB, int LAYOUT = kAccRows, typename Acc>
+__device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearBlock& b, Acc& acc, unsigned char* lds, int tid) {
+    static_assert(FA % RB == 0 && (LAYOUT != kAccWide || (RB % 2 == 0 && FB % 2 == 0)), "all row blocks");
     constexpr bool OWN = WK == 1;
     constexpr int COLS = OWN ? FB * 16 : WN * FB * 16, ROWS = OWN ? RB * 16 : WM * RB * 16, UNITS = COLS / 8, STRIDE = (OWN ? 64 : W * 64) / UNITS;
     static constexpr int TURNS = (ROWS + STRIDE - 1) / STRIDE, kAtOnce = OWN && TURNS % 4 == 0 ? 4 : TURNS % 2 == 0 ? 2 : 1;
@@ -284,7 +287,7 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
         for (int q = 0; q < 8; ++q) scale[q] = p.W_scales && !p.part && columns > 0 ? value(w, true, q) : 1.0f;
 #pragma unroll
         for (int i = 0; i < FA; ++i) {
-            const int m = (WM * i + wm) * 16 + frow;
+            const int m = (WM * (LAYOUT == kAccWide ? (i & ~1) + (lane >> 4 & 1) : i) + wm) * 16 + frow;
             token_scale[i] = p.x_scales && !p.part && m < b.rows ? p.x_scales[b.first + m] : 1.0f;
         }
 #pragma unroll
@@ -315,10 +318,18 @@ __device__ __forceinline__ void finish_linear(const LinearArgs& p, const LinearB
         for (int i = 0; i < RB; ++i)
 #pragma unroll
             for (int j = 0; j < FB; ++j)
-                if constexpr (ACROSS) {
+                if constexpr (LAYOUT == kAccAcross) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
                         stage[place_of(wk, ((OWN ? 0 : wm * RB) + i) * 16 + 4 * fp + q, ((OWN ? 0 : wn * FB) + j) * 4 + frow / 4) + frow % 4] = acc[i0 + i][j][q];
+                } else if constexpr (LAYOUT == kAccWide) {
+                    // (a pair of row blocks and one of column blocks have four pieces: number 2 (i % 2) + j % 2)
+                    const auto& from = acc[(i0 + i) / 2][j / 2];
+                    constexpr int per = 4;
+                    const int g = 2 * (i % 2) + j % 2;
+                    const f32x4_t v = f32x4_t{from[per * g], from[per * g + 1], from[per * g + 2], from[per * g + 3]} * token_scale[(i0 + i) & ~1];
+                    *reinterpret_cast<f32x4_t*>(stage + place_of(wk, ((OWN ? 0 : wm * RB) + (i & ~1) + (lane >> 4 & 1)) * 16 + frow,
+                                                                 (OWN ? 0 : wn * FB * 4) + j / 2 * 8 + 2 * g + (lane >> 5))) = v;
                 } else
                     *reinterpret_cast<f32x4_t*>(stage + place_of(wk, ((OWN ? 0 : wm * RB) + i) * 16 + frow, ((OWN ? 0 : wn * FB) + j) * 4 + fp)) = SCALED ? acc[i0 + i][j] * token_scale[i0 + i] : acc[i0 + i][j];
         sync();
