@@ -78,7 +78,10 @@ __device__ __forceinline__ void linear_quad(const LinearArgs& p) {
                               : buffer_of(p.x + b.first * p.x_pitch, (uint32_t)((b.rows - 1) * p.x_pitch) + p.k);
     const i32x4_t rb = buffer_of(W, (uint32_t)rows_w * p.k);
     // a load is 8 rows of 128 bytes: lane -> row lane / 8, piece (lane % 8) ^ row; wavefront w loads rows [w TM / 4, (w + 1) TM / 4) of x, of W alike
+    // (e4m3: ^ 1 more in the second row block of each pair, whose lanes read in one cycle with the first's)
     const uint32_t lrow = (uint32_t)lane >> 3, piece = (((uint32_t)lane & 7u) ^ lrow) * 16u;
+    auto piece_a = [&](int i) { return WIDE ? piece ^ ((uint32_t)i / 4 % 2 * 16u) : piece; };
+    auto piece_b = [&](int i) { return WIDE ? piece ^ ((uint32_t)i / 2 % 2 * 16u) : piece; };
     uint32_t off_a[NA], off_b[NB];
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
@@ -88,12 +91,12 @@ __device__ __forceinline__ void linear_quad(const LinearArgs& p) {
             const int64_t token = token_of_row<GROUPED>(p, b, row);
             at = token < 0 ? kNowhere : (uint32_t)token * (uint32_t)p.x_pitch;
         }
-        off_a[i] = at + piece;
+        off_a[i] = at + piece_a(i);
     }
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
         const int row = wave * (TN / 4) + i * 8 + (int)lrow;
-        off_b[i] = (row < rows_w ? (uint32_t)row * p.k : kNowhere) + piece;
+        off_b[i] = (row < rows_w ? (uint32_t)row * p.k : kNowhere) + piece_b(i);
     }
 #pragma unroll
     for (int i = 0; i < NA; ++i) asm volatile("" : "+v"(off_a[i]));
@@ -169,7 +172,7 @@ __device__ __forceinline__ void linear_quad(const LinearArgs& p) {
         for (int s = 0; s < 2; ++s)
 #pragma unroll
             for (int u = 0; u < PER; ++u) {
-                const uint32_t sw = (uint32_t)(frow * SL + (((s * 4 + fp + u) ^ (frow & 7)) * 16));
+                const uint32_t sw = (uint32_t)(frow * SL + (((s * 4 + fp + u) ^ (frow & 7) ^ second) * 16));
                 frag_a[s][u] = (uint32_t)((wm + 2 * second) * 16 * SL) + sw;
                 frag_b[s][u] = (uint32_t)(SA * G::UA + (wn * NB + second) * 16 * SL) + sw;
             }
@@ -288,10 +291,10 @@ __device__ __forceinline__ void linear_quad(const LinearArgs& p) {
             oa.soff = ob.soff = from;
             oa.to = lds_a;
             ob.to = lds_b;
-            const uint32_t back = piece < rest ? 0u : piece;
+            auto back = [&](uint32_t at) { return at < rest ? 0u : at; };
             asm volatile("s_nop 4" : "+s"(oa.rs), "+s"(ob.rs));
-            for_constants<NA>([&](auto i) { load(i, oa, off_a[decltype(i)::value] - back); });
-            for_constants<NB>([&](auto i) { load(i, ob, off_b[decltype(i)::value] - back); });
+            for_constants<NA>([&](auto i) { load(i, oa, off_a[decltype(i)::value] - back(piece_a(decltype(i)::value))); });
+            for_constants<NB>([&](auto i) { load(i, ob, off_b[decltype(i)::value] - back(piece_b(decltype(i)::value))); });
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
@@ -321,7 +324,7 @@ __device__ __forceinline__ void linear_quad(const LinearArgs& p) {
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_nop 15\n\ts_nop 15" ::: "memory");
         __builtin_amdgcn_s_barrier();
         hold();
-        finish_linear<T, GROUPED, 4, NR, NB, 2, 2, 1, WIDE ? 2 : G::fit(NR, NR), WIDE ? kAccWide : kAccRows>(p, b, acc, lds, tid);
+        finish_linear<T, GROUPED, 4, NR, NB, 2, 2, 1, WIDE && NR % 4 ? 2 : WIDE ? 4 : G::fit(NR, NR), WIDE ? kAccWide : kAccRows>(p, b, acc, lds, tid);
     };
     // The rows of a product or group are divided evenly between its tiles, and the row blocks of a tile are dealt out to the wavefronts in turns, so
     // that a tile which is not full takes fewer MFMAs.  (Each number of row blocks with its own accumulators and epilogue: where loops share them the
