@@ -45,7 +45,8 @@ constexpr bool linear_has(int es, bool direct, bool grouped, int shape) {
     return !(shape == 2 || (shape >= 4 && shape <= 9) || shape == 12 || (grouped && (shape == 10 || shape == 15)));
 }
 // of e4m3; from kLinearNearFp8 on with outputs in bf16 by the faster instruction, which takes two half-lines of each wavefront
-constexpr LinearShape kLinearShapeFp8[] = {{16, 16, 512}, {16, 32, 512}, {16, 16, 1024}, {32, 32, 512}, {64, 64, 256}, {128, 128, 256}, {128, 128, 128}, {64, 64, 128}};
+constexpr LinearShape kLinearShapeFp8[] = {{16, 16, 512}, {16, 32, 512}, {16, 16, 1024}, {32, 32, 512}, {64, 64, 256}, {128, 128, 256}, {128, 128, 128}, {64, 64, 128},
+                                           {32, 64, 512}, {64, 128, 256}, {128, 64, 256}};
 constexpr int kLinearNearFp8 = 3;
 constexpr int kLinearShapesFp8 = sizeof(kLinearShapeFp8) / sizeof(LinearShape);
 constexpr LinearShape kLinearStagedFp8[] = {{16, 16, 512}, {32, 32, 256}, {64, 64, 128}, {128, 128, 128}};

@@ -19,7 +19,10 @@ template <typename F> void for_fp8_tile(bool direct, int shape, F f) {
             case 4: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<5>{}); break;
             case 5: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}); break;
             case 6: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
-            default: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
+            case 7: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
+            case 8: f(std::true_type{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<2>{}, num<3>{}); break;
+            case 9: f(std::true_type{}, num<2>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<3>{}); break;
+            default: f(std::true_type{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<3>{}); break;
         }
     } else {
         switch (shape) {

@@ -17,6 +17,7 @@ struct NormArgs {
     double inv_d, eps;
 };
 
+constexpr int64_t kBusy = 4096;
 constexpr float kE4m3Most = 448.0f, kLeastScale = 0x1p-126f;
 // (rows begin at any element's address)
 typedef uint32_t norm_u32x4_t __attribute__((ext_vector_type(4), aligned(2)));
@@ -217,7 +218,8 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs p) {
 template <typename T, int OUT> void launch(const NormArgs& p, int each, dim3 grid, dim3 block, hipStream_t s) {
     if (each == 1) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, 1>), grid, block, 0, s, p);
     else if (each == 2) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, 2>), grid, block, 0, s, p);
-    else if (each <= 4) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, 4>), grid, block, 0, s, p);
+    else if (each == 4) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, 4>), grid, block, 0, s, p);
+    else if (each == 8) hipLaunchKernelGGL((rms_norm_kernel<T, OUT, 8>), grid, block, 0, s, p);
     else hipLaunchKernelGGL((rms_norm_kernel<T, OUT, 0>), grid, block, 0, s, p);
 }
 
@@ -245,9 +247,13 @@ tardis_status_t td_rms_norm(const void* x, int64_t n, int64_t d, int64_t x_pitch
     p.norm = norm;
     p.inv_d = 1.0 / (double)d;
     p.eps = (double)eps;
-    p.waves = 1;
-    while (p.waves < 16 && (int64_t)p.waves * 64 < p.units) p.waves *= 2;
-    const int each = (int)((p.units + p.waves * 64 - 1) / (p.waves * 64));
+    // Pieces of a thread and wavefronts of a row: as few wavefronts as keep 4096 of them busy (16 for each CU), since what they share of a row goes by
+    // way of barriers; fewer rows are divided among more
+    int each = 8;
+    auto waves_of = [&](int u) { return (int64_t)(p.units + 64 * u - 1) / (64 * u); };
+    while (each > 1 && n * waves_of(each) < kBusy && waves_of(each / 2) <= 16) each /= 2;
+    p.waves = (int)std::min<int64_t>(16, waves_of(each));
+    if (waves_of(each) > 16) each = 0;                                 // (rows that do not fit into registers)
     const int rows = std::max(1, 4 / p.waves), threads = 64 * p.waves * rows;
     const int64_t most = kMostThreads / threads;                       // blocks of a launch
     const int64_t blocks = (n + rows - 1) / rows;
