@@ -412,8 +412,8 @@ tardis_status_t tardis_moe_combine(const void* z, int64_t rows, const int32_t* p
  *     norm (codes and scales) -> tardis_linear_fp8 -> tardis_fp8_rows -> tardis_linear_fp8
  *     norm (bf16) -> tardis_linear_4bit -> tardis_linear_4bit
  * As above: no handle, no allocation, no synchronisation, pointers aligned to their elements,
- * rows and distances up to 2^30, a call with no rows is TARDIS_OK and does nothing, equal calls
- * give equal bits.  Nothing is written but the outputs named. */
+ * rows and distances up to 2^30, a call with no rows is TARDIS_OK and does nothing.  Equal calls (sizes, types,
+ * pitch, alignment, working memory) give equal bits; a token's result need not be the same bits next to other tokens. */
 typedef struct {
     int64_t d;           /* 1 .. 2^22 */
     int32_t dtype;       /* of x, weight, residual and sum: TARDIS_F32 or TARDIS_BF16 */
@@ -430,8 +430,8 @@ typedef struct {
  *   sum       n x d, dtype: s, rounded; or NULL.  May be residual itself, or x itself where x_pitch = d.
  *   y         n x d, out_dtype; must not overlap the others.
  *   scales    n floats, where out_dtype is TARDIS_FP8_E4M3 (else NULL): a row's y is its codes
- *             times scale = max(max |y| / 448, 2^-126), codes rounded to nearest even.  A NaN is a NaN
- *             code; a row with an infinity has scale infinity and codes of 0 (finite) and NaN. */
+ *             times scale = max(max |y| / 448, 2^-126), codes rounded to nearest even.  A NaN in y is a NaN
+ *             code and counts for nothing in the scale; with an infinite y the scale is infinite, codes are 0 and NaN. */
 tardis_status_t tardis_rms_norm(const tardis_norm_desc* desc, const void* x, int64_t n, int64_t x_pitch, const void* residual,
                                 void* sum, void* y, float* scales, void* stream);
 
@@ -449,8 +449,10 @@ typedef struct {
     const void* b;           /* n_out, or NULL for zero */
 } tardis_linear_fp8_desc;
 
-/* y = sigma(x W^T + b) + residual with x and W in e4m3, a scale for each row of either: products are exact,
- * sums fp32, scales applied to the sums (the token's first).  sigma, residual, y and work as tardis_linear's.
+/* y = sigma(x W^T + b) + residual with x and W in e4m3, a scale for each row of either: scales are applied to
+ * the fp32 sums (the token's first).  With out_dtype TARDIS_F32 products are exact and sums as tardis_linear's; with
+ * TARDIS_BF16 the matrix instructions of larger calls drop of each product what is below 2^-13 of the largest of the 32 that
+ * they add up first (of sums of many products 1e-4 of the root of their squares).  sigma, residual, y and work as tardis_linear's.
  *   x         n rows of n_in codes, x_pitch >= n_in bytes apart.
  *   x_scales  n floats, or NULL for ones. */
 tardis_status_t tardis_linear_fp8(const tardis_linear_fp8_desc* desc, const void* x, const float* x_scales, int64_t n, int64_t x_pitch,

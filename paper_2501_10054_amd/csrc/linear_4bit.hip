@@ -1,9 +1,13 @@
 // The linear layer with 4-bit weights: y = sigma(sum_G scale_jG sum_(k in G) (q_jk - zero_jG) x_k + b_j) + r.
 //
 // A code q becomes a bf16 value without a conversion: put under the exponent of 16, with the weight 1 three bits up in the mantissa, it is 16 + q, and
-// a word's layout is such that a shift, an and and an or make two neighbouring columns at once.  16 + zero is multiplied with the same tokens by matrix
-// instructions that take it away again, so that an accumulator holds sum (q - zero) x of a group, every product exact; the group's scale goes to
-// the sum.  Tokens in fp32 are three bf16 parts each, which together hold all of their 24 bits.
+// a word's layout is such that a shift and an and-or make two neighbouring columns at once.  16 + zero is multiplied with the same tokens and taken away
+// again (few tokens: by matrix instructions; many: as a product with the sum of the group's columns), so that a group's accumulator ends with
+// sum (q - zero) x, every product exact; the group's scale goes to that sum.  Tokens in fp32 are three bf16 parts each, which together hold all of their 24 bits.
+//
+// What bounds it: one token - launch, the way of the first bytes, and 0.5 bytes a weight from HBM (16384 -> 4096: 11.5 us, 34.7 MB; the stream alone takes 5); a
+// prompt - vector instructions beside the matrix cores, of which a group's product needs 8 for each 64 bytes of codes and one for each result
+// (2048 tokens 4096 -> 16384: 306 us, 0.9 PFLOP/s; 512 tokens 84 us).
 #include <algorithm>
 
 #include "linear_tile.h"
@@ -38,9 +42,10 @@ struct Sixteen {
         return {(w << 3 & mask) | exponent, (w >> 1 & mask) | exponent, (w >> 5 & mask) | exponent, (w >> 9 & mask) | exponent};
     }
 };
-// -(16 + z), twice in a word
-__device__ __forceinline__ uint32_t sixteen_less(uint32_t z) {
-    return (__float_as_uint(-16.0f - (float)min(z, 128u)) >> 16) * 0x10001u;
+// Vector instructions have written the descriptor's registers, and the loads that read them are inline assembly, which the compiler takes for ready: 5 wait states
+__device__ __forceinline__ i32x4_t settled(i32x4_t r) {
+    asm volatile("s_nop 4" : "+s"(r));
+    return r;
 }
 
 // The eight columns of a token that a matrix instruction takes of a lane, as parts in bf16 (fp32: head, middle, end)
@@ -92,7 +97,7 @@ constexpr int kStep = 128;                          // columns of a step: 64 byt
 // A block has 16 RT rows of W and all tokens, which it puts into LDS, with the table of scales and zero points, as many columns at a time as there is room for.
 // Its wavefronts are RT times KW: one has 16 rows and a KW-th of the steps, whose codes come straight to a ring of its own in LDS, D - 2 steps ahead of the two
 // that are multiplied, without barriers.  The loop is a step long and not unrolled: a block runs through its code once, and what it has to fetch of it counts
-// (1 token, 1024 -> 1024: 7.9 us with three batches of four groups in registers, all unrolled, REPLACE).
+// (1 token, 1024 -> 1024: 7.9 us with three batches of four groups in registers, all unrolled; 5.2).
 // Lane l multiplies, of W's row l % 16, the columns 8 GW (l / 16) .. of a group, and the same columns of token l % 16.
 template <typename T, int RT> struct FourBlock {
     static constexpr int KW = kWaves / RT, PARTS = Token<T>::PARTS, ENTRY = PARTS == 1 ? 4 : 8, D = 8, kRing = kWaves * D * 1024;
@@ -113,7 +118,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) linear4_kernel(FourArgs p) {
     // codes: a load is 16 rows of 64 bytes, as they lie.  (What lies behind a row or the last one has tokens of 0 or is kept nowhere)
     const uint32_t row_bytes = p.groups * (16u * GW), base = (uint32_t)uniform((int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds);
     const int rows = (int)max((int64_t)0, min((int64_t)16, p.N - n0));
-    const i32x4_t rw = buffer_of(reinterpret_cast<const unsigned char*>(p.W) + min(n0, p.N - 1) * row_bytes, (uint32_t)rows * row_bytes);
+    const i32x4_t rw = settled(buffer_of(reinterpret_cast<const unsigned char*>(p.W) + min(n0, p.N - 1) * row_bytes, (uint32_t)rows * row_bytes));
     const uint32_t off = (uint32_t)(lane >> 2) * row_bytes + (uint32_t)(lane & 3) * 16u, ring = base + (uint32_t)wave * (D * 1024);
     const uint32_t steps = (p.k + kStep - 1) / kStep, share = ((p.chunk + KW - 1) / KW + 1) & ~1u;   // (of a chunk's steps, for a wavefront: even)
     uint32_t ask_chunk = 0, ask = 0, ask_slot = 0;                                            // the step that is asked for next
@@ -403,10 +408,10 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
         off_codes[i] = (row < rows_w ? (uint32_t)row * row_bytes : kNowhere) + (uint32_t)(lane & 3) * 16u;
     }
     const uint32_t off_sums = high < G && 4 * low < min(b.rows, TM) ? (uint32_t)(high * p.sum_pitch + 4 * low) * 4u : kNowhere;
-    const i32x4_t rc = buffer_of(p.W + b.n0 * row_bytes, (uint32_t)rows_w * row_bytes);
+    const i32x4_t rc = settled(buffer_of(p.W + b.n0 * row_bytes, (uint32_t)rows_w * row_bytes));
     // (live: past the last step nothing is fetched, from empty buffers)
     auto load_x = [&](uint32_t step, int part, uint32_t slot, bool live) {
-        i32x4_t r = buffer_of(p.x + ((int64_t)part * p.n + b.first) * p.k, (uint32_t)b.rows * p.k);
+        i32x4_t r = settled(buffer_of(p.x + ((int64_t)part * p.n + b.first) * p.k, (uint32_t)b.rows * p.k));
         r.z = live ? r.z : 0;
 #pragma unroll
         for (int i = 0; i < LX; ++i) load_to_lds(base + slot * S::X + (uint32_t)wave * (S::X / WN) + i * 1024u, off_x[i], r, live ? step * (2 * kStep) : 0u);
@@ -423,12 +428,12 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
             if (piece < LT) {
                 // lane -> 16 bytes of the step's groups, one behind the other
                 const uint32_t in = (uint32_t)piece * 1024u + (uint32_t)lane * 16u, group = in / (TN * S::ROW), at = in % (TN * S::ROW);
-                i32x4_t rt = buffer_of(p.table + ((int64_t)step * G * p.table_pitch + b.n0) * S::ROW, (uint32_t)(((G - 1) * p.table_pitch + TN) * S::ROW));
+                i32x4_t rt = settled(buffer_of(p.table + ((int64_t)step * G * p.table_pitch + b.n0) * S::ROW, (uint32_t)(((G - 1) * p.table_pitch + TN) * S::ROW)));
                 rt.z = live ? rt.z : 0;
                 load_to_lds((uint32_t)uniform((int)(base + D * (S::X + S::CODES) + slot * S::TABLE + (uint32_t)piece * 1024u)),
                             group < (uint32_t)G ? group * (uint32_t)p.table_pitch * S::ROW + at : kNowhere, rt, 0);
             } else {
-                i32x4_t rs = buffer_of(p.sums + (int64_t)step * G * p.sum_pitch + b.first, (uint32_t)((G - 1) * p.sum_pitch + p.sum_pitch - b.first) * 4u);
+                i32x4_t rs = settled(buffer_of(p.sums + (int64_t)step * G * p.sum_pitch + b.first, (uint32_t)((G - 1) * p.sum_pitch + p.sum_pitch - b.first) * 4u));
                 rs.z = live ? rs.z : 0;
                 load_to_lds(base + D * (S::X + S::CODES + S::TABLE) + slot * S::SUMS, off_sums, rs, 0);
             }

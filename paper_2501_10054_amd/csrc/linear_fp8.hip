@@ -1,4 +1,5 @@
-// The linear layer for x and W in e4m3 with a scale for each row: linear_tile.h's tiles
+// The linear layer for x and W in e4m3 with a scale for each row: linear_tile.h's tiles.  One token 16384 -> 4096: 14.5 us, 67 MB, 4.6 TB/s (launch and first
+// bytes 5 us); 333 tokens 11008 -> 4096 with a residual: 33 us, 0.9 PFLOP/s.
 #include "linear_tile.h"
 
 namespace {
@@ -8,40 +9,38 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, 2) linear_fp8_kernel(Linear
     linear_tile<T, false, DIRECT, FA, FB, WM, WN, WK, KS, D>(p);
 }
 
-// f(direct, row and column blocks of a wavefront, grid of wavefronts, wavefronts and half-lines of each in K, slices in LDS)
-template <typename F> void for_fp8_tile(bool direct, int shape, F f) {
+// f(element type, direct, row and column blocks of a wavefront, grid of wavefronts, wavefronts and half-lines of each in K, slices in LDS)
+template <typename F> void for_fp8_shape(bool direct, int shape, bool out_f32, F f) {
+    auto use = [&](auto number, auto d, auto... tile) {
+        constexpr int s = decltype(number)::value;
+        constexpr bool DIRECT = decltype(d)::value;
+        if constexpr (DIRECT && s >= kLinearNearFp8) {
+            if (!out_f32) return f(e4m3_near_t{}, d, tile...);
+        }
+        if constexpr (linear_has_fp8(DIRECT, DIRECT && s >= kLinearNearFp8, s)) f(e4m3_t{}, d, tile...);
+    };
     if (direct) {
         switch (shape) {
-            case 0: f(std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<5>{}); break;
-            case 1: f(std::true_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<3>{}); break;
-            case 2: f(std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<2>{}, num<5>{}); break;
-            case 3: f(std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<2>{}, num<5>{}); break;
-            case 4: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<5>{}); break;
-            case 5: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}); break;
-            case 6: f(std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
-            case 7: f(std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
-            case 8: f(std::true_type{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<2>{}, num<3>{}); break;
-            case 9: f(std::true_type{}, num<2>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<3>{}); break;
-            default: f(std::true_type{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<3>{}); break;
+            case 0: use(num<0>{}, std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<5>{}); break;
+            case 1: use(num<1>{}, std::true_type{}, num<1>{}, num<2>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<3>{}); break;
+            case 2: use(num<2>{}, std::true_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<2>{}, num<5>{}); break;
+            case 3: use(num<3>{}, std::true_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<2>{}, num<5>{}); break;
+            case 4: use(num<4>{}, std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<5>{}); break;
+            case 5: use(num<5>{}, std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}); break;
+            case 6: use(num<6>{}, std::true_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
+            case 7: use(num<7>{}, std::true_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<2>{}); break;
+            case 8: use(num<8>{}, std::true_type{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}, num<4>{}, num<2>{}, num<3>{}); break;
+            case 9: use(num<9>{}, std::true_type{}, num<2>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<3>{}); break;
+            default: use(num<10>{}, std::true_type{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<3>{}); break;
         }
     } else {
         switch (shape) {
-            case 0: f(std::false_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<6>{}); break;
-            case 1: f(std::false_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<4>{}); break;
-            case 2: f(std::false_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}); break;
-            default: f(std::false_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}); break;
+            case 0: use(num<0>{}, std::false_type{}, num<1>{}, num<1>{}, num<1>{}, num<1>{}, num<8>{}, num<1>{}, num<6>{}); break;
+            case 1: use(num<1>{}, std::false_type{}, num<2>{}, num<1>{}, num<1>{}, num<2>{}, num<4>{}, num<1>{}, num<4>{}); break;
+            case 2: use(num<2>{}, std::false_type{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<4>{}); break;
+            default: use(num<3>{}, std::false_type{}, num<4>{}, num<4>{}, num<2>{}, num<2>{}, num<2>{}, num<1>{}, num<2>{}); break;
         }
     }
-}
-
-// f(element type, what for_fp8_tile gives)
-template <typename F> void for_fp8_shape(bool direct, int shape, bool out_f32, F f) {
-    for_fp8_tile(direct, shape, [&](auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
-        if constexpr (decltype(d)::value && decltype(ks)::value % 2 == 0) {
-            if (shape >= kLinearNearFp8 && !out_f32) return f(e4m3_near_t{}, d, fa, fb, wm, wn, wk, ks, ring);
-        }
-        f(e4m3_t{}, d, fa, fb, wm, wn, wk, ks, ring);
-    });
 }
 
 }  // namespace

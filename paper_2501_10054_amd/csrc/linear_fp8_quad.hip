@@ -9,8 +9,7 @@ __global__ void __launch_bounds__(256, 1) linear_fp8_quad_kernel(LinearArgs p) {
 }
 
 template <typename F> void for_fp8_quad_shape(int shape, F f) {
-    if (shape == 0) f(num<8>{}, num<8>{});
-    else f(num<8>{}, num<4>{});
+    if (shape == 0) f(num<8>{}, num<4>{});
 }
 
 }  // namespace

@@ -1,5 +1,7 @@
 // The root-mean-square norm in front of a layer, with the residual's addition in front of it, and rows put into 8 bits:
 //     s = x + residual,  y = s / sqrt(mean(s^2) + eps) * weight,  output in bf16, fp32, or e4m3 codes with a scale for each row.
+// A row is read once and stays in registers.  What bounds it: HBM (8192 rows of 4096, bf16 with residual to e4m3: 235 MB, 49 us, 4.8 TB/s of reads and writes mixed);
+// few rows: the launch (1 row 2.8 us).
 #include <algorithm>
 
 #include "tiles.h"
@@ -248,8 +250,9 @@ tardis_status_t td_rms_norm(const void* x, int64_t n, int64_t d, int64_t x_pitch
     p.inv_d = 1.0 / (double)d;
     p.eps = (double)eps;
     // Pieces of a thread and wavefronts of a row: as few wavefronts as keep 4096 of them busy (16 for each CU), since what they share of a row goes by
-    // way of barriers; fewer rows are divided among more
-    int each = 8;
+    // way of barriers; fewer rows are divided among more.  More than 4 pieces only for rows that need them (8192 rows of 4096 in bf16 to e4m3, us: 8 pieces
+    // 55.8, 4 and 1 49)
+    int each = (int64_t)(p.units + 255) / 256 <= 16 ? 4 : 8;
     auto waves_of = [&](int u) { return (int64_t)(p.units + 64 * u - 1) / (64 * u); };
     while (each > 1 && n * waves_of(each) < kBusy && waves_of(each / 2) <= 16) each /= 2;
     p.waves = (int)std::min<int64_t>(16, waves_of(each));

@@ -8,6 +8,7 @@ import math
 import pytest
 import torch
 
+from low_bits_calls import FOUR
 from paper_2501_10054_amd import tardis as T
 from test_gpu_linear import ACTS, check, inside, sigma
 
@@ -154,3 +155,16 @@ def test_without_working_memory():
 def test_no_rows():
     W, scales = torch.zeros(16, 16, dtype=torch.int32, device=DEV), torch.ones(16, 1, device=DEV)
     assert T.tardis_linear_4bit(torch.zeros(0, 128, device=DEV), W, scales).shape == (0, 16)
+
+
+@pytest.mark.parametrize("call", range(len(FOUR)))
+def test_every_kernel(call):
+    """The calls of low_bits_calls.py, by which every kernel is reached."""
+    _, n, n_in, n_out, group, dtype = FOUR[call]
+    gen = torch.Generator(device=DEV).manual_seed(call)
+    x = inside((n, n_in), T._TORCH_DTYPE[dtype], gen)
+    q, scales, zeros = weights(n_out, n_in, group, x.dtype, gen, True)
+    r = torch.randn(n, n_out, device=DEV, generator=gen)
+    y = T.tardis_linear_4bit(x, T.tardis_pack_4bit(q, group), scales, zeros, group=group, act="relu", residual=r, out_dtype=torch.float32)
+    want, off = layer64(x, q, scales, zeros, None, "relu", group)
+    check(y, want + r.double(), off)

@@ -9,6 +9,7 @@ import math
 import pytest
 import torch
 
+from low_bits_calls import EIGHT
 from paper_2501_10054_amd import tardis as T
 from test_gpu_linear import ACTS, SIZES, check, inside, sigma
 
@@ -123,3 +124,16 @@ def test_without_working_memory():
 def test_no_rows():
     W = torch.zeros(16, 64, device=DEV).to(T.FP8)
     assert T.tardis_linear_fp8(torch.zeros(0, 64, device=DEV).to(T.FP8), None, W, None).shape == (0, 16)
+
+
+@pytest.mark.parametrize("call", range(len(EIGHT)))
+def test_every_kernel(call):
+    """The calls of low_bits_calls.py, by which every kernel is reached."""
+    _, n, n_in, n_out, gap, out = EIGHT[call]
+    gen = torch.Generator(device=DEV).manual_seed(call)
+    out = T._TORCH_DTYPE[out]
+    x, W, sx, sw = codes((n, n_in), gen, gap=gap), codes((n_out, n_in), gen), scales(n, gen, n_in), scales(n_out, gen, n_in)
+    b, r = torch.randn(n_out, device=DEV, generator=gen).to(out), torch.randn(n, n_out, device=DEV, generator=gen).to(out)
+    y = T.tardis_linear_fp8(x, sx, W, sw, b, act="relu", residual=r, out_dtype=out)
+    want, off = layer64(x, sx, W, sw, b, "relu", out)
+    check(y, want + r.double(), off)

@@ -9,6 +9,7 @@ import math
 import pytest
 import torch
 
+from low_bits_calls import NORM
 from paper_2501_10054_amd import tardis as T
 from test_gpu_linear import inside
 
@@ -176,3 +177,14 @@ def test_no_rows():
     y, total = T.tardis_rms_norm(x, residual=x)
     codes, scales = T.tardis_fp8_rows(x)
     assert y.shape == total.shape == codes.shape == (0, 64) and scales.shape == (0,)
+
+
+@pytest.mark.parametrize("call", range(len(NORM)))
+def test_every_kernel(call):
+    """The calls of low_bits_calls.py, by which every kernel is reached."""
+    _, n, d, dtype, out = NORM[call]
+    gen = torch.Generator(device=DEV).manual_seed(call)
+    dtype, out = T._TORCH_DTYPE[dtype], T.FP8 if out == T.FP8_E4M3 else T._TORCH_DTYPE[out]
+    x, r = inside((n, d), dtype, gen), inside((n, d), dtype, gen)
+    weight = torch.randn(d, device=DEV, generator=gen).to(dtype)
+    check_norm(T.tardis_rms_norm(x, weight, residual=r, out_dtype=out), x, weight, r, 1e-6, out)
