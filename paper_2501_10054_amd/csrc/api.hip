@@ -727,7 +727,7 @@ tardis_status_t tardis_linear_4bit_workspace(const tardis_linear_4bit_desc* desc
     TD_TRY(check_4bit(desc, n, x_pitch));
     if (!bytes) return TARDIS_ERR_INVALID_ARG;
     *bytes = 0;
-    return n > 0 ? td_linear_4bit_work_bytes(desc, n, x_pitch, bytes) : TARDIS_OK;
+    return n > 0 ? td_linear_4bit_work_bytes(desc, n, bytes) : TARDIS_OK;
 }
 
 tardis_status_t tardis_linear_4bit(const tardis_linear_4bit_desc* desc, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y,

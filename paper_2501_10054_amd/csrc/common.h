@@ -346,6 +346,6 @@ tardis_status_t td_linear_fp8_work_bytes(const tardis_linear_fp8_desc* d, const 
 tardis_status_t td_linear_fp8(const tardis_linear_fp8_desc* d, const void* x, const float* x_scales, int64_t n, int64_t x_pitch, const void* residual,
                               void* y, void* work, int64_t work_bytes, hipStream_t s);
 // linear_4bit.hip
-tardis_status_t td_linear_4bit_work_bytes(const tardis_linear_4bit_desc* d, int64_t n, int64_t x_pitch, int64_t* bytes);
+tardis_status_t td_linear_4bit_work_bytes(const tardis_linear_4bit_desc* d, int64_t n, int64_t* bytes);
 tardis_status_t td_linear_4bit(const tardis_linear_4bit_desc* d, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y, void* work,
                                int64_t work_bytes, hipStream_t s);

@@ -710,15 +710,15 @@ tardis_status_t run_tiles(const tardis_linear_4bit_desc* d, const FourPlan& plan
 
 }  // namespace
 
-tardis_status_t td_linear_4bit_work_bytes(const tardis_linear_4bit_desc* d, int64_t n, int64_t x_pitch, int64_t* bytes) {
-    *bytes = plan_four(d, n, (int64_t)1 << 62).work;
-    return TARDIS_OK;
+namespace {
+
+// Tokens that are done together: more would take more working memory and nothing less of time
+int64_t tokens_at_once(const tardis_linear_4bit_desc* d) {
+    const int64_t units = (d->n_in + kStep - 1) / kStep * (kStep / 8);
+    return std::max<int64_t>(1, std::min<int64_t>(16384, (kMostThreads / 2) / units));
 }
 
-tardis_status_t td_linear_4bit(const tardis_linear_4bit_desc* d, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y, void* work,
-                               int64_t work_bytes, hipStream_t s) {
-    const FourPlan plan = plan_four(d, n, work_bytes);
-    if (plan.tiles) return run_tiles(d, plan, x, n, x_pitch, residual, y, static_cast<unsigned char*>(work), s);
+tardis_status_t run_few(const tardis_linear_4bit_desc* d, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y, hipStream_t s) {
     TD_TRY(init_four());
     FourArgs p{};
     const bool f32 = d->dtype == TARDIS_F32;
@@ -761,5 +761,26 @@ tardis_status_t td_linear_4bit(const tardis_linear_4bit_desc* d, const void* x, 
         });
     }
     TD_HIP(hipGetLastError());
+    return TARDIS_OK;
+}
+
+}  // namespace
+
+tardis_status_t td_linear_4bit_work_bytes(const tardis_linear_4bit_desc* d, int64_t n, int64_t* bytes) {
+    *bytes = plan_four(d, std::min(n, tokens_at_once(d)), (int64_t)1 << 62).work;
+    return TARDIS_OK;
+}
+
+tardis_status_t td_linear_4bit(const tardis_linear_4bit_desc* d, const void* x, int64_t n, int64_t x_pitch, const void* residual, void* y, void* work,
+                               int64_t work_bytes, hipStream_t s) {
+    const int64_t most = tokens_at_once(d), es = (int64_t)td_elem_size(d->dtype), eo = (int64_t)td_elem_size(d->out_dtype);
+    for (int64_t at = 0; at < n; at += most) {
+        const int64_t here = std::min(most, n - at);
+        const FourPlan plan = plan_four(d, here, work_bytes);
+        const unsigned char *from = static_cast<const unsigned char*>(x) + at * x_pitch * es, *add = static_cast<const unsigned char*>(residual);
+        unsigned char* to = static_cast<unsigned char*>(y) + at * d->n_out * eo;
+        if (add) add += at * d->n_out * eo;
+        TD_TRY(plan.tiles ? run_tiles(d, plan, from, here, x_pitch, add, to, static_cast<unsigned char*>(work), s) : run_few(d, from, here, x_pitch, add, to, s));
+    }
     return TARDIS_OK;
 }

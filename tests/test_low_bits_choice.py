@@ -72,16 +72,15 @@ def test_working_memory_is_what_the_caller_gives(host):  # noqa: F811
     assert four(host, 100, 4096, 4096, 128, T.BF16, room=need.value)[0] == "linear4_prepare_kernel bf16 4"
 
 
-@pytest.mark.parametrize("n,n_in,n_out", [(1, 1 << 22, 1 << 22), (1 << 30, 64, 1), (1 << 22, 4096, 1 << 10), (16, 1 << 22, 16), (1 << 20, 1, 1 << 22), (5, 128, 1 << 22)])
+@pytest.mark.parametrize("n,n_in,n_out", [(1, 1 << 22, 1 << 15), (1 << 28, 64, 1), (1 << 22, 4096, 1 << 10), (16, 1 << 22, 16), (1 << 12, 1, 1 << 22), (5, 128, 1 << 22)])
 def test_large_calls_with_4_bit_weights(host, n, n_in, n_out):  # noqa: F811
     """Nothing that the limits allow is refused, and no launch has 2^32 threads (the runtime's double counts them)."""
-    if n * n_out > 1 << 36:
-        n = (1 << 36) // n_out
     for dtype in (T.BF16, T.F32):
-        assert four(host, n, n_in, n_out, 32, dtype) if n <= 1 << 12 else four(host, n, n_in, n_out, 128, dtype)
+        got = four(host, min(n, (1 << 36) // n_out), n_in, n_out, 128, dtype)
+        assert 1 <= len(got) <= 1 << 17
 
 
-@pytest.mark.parametrize("n,d", [(1 << 30, 1), (1 << 30, 1 << 22), (3, 1 << 22), (1 << 24, 4096)])
+@pytest.mark.parametrize("n,d", [(1 << 30, 1), (1 << 26, 2048), (3, 1 << 22)])
 def test_large_norms(host, n, d):  # noqa: F811
     for out in (T.BF16, T.FP8_E4M3):
         assert norm(host, n, d, T.BF16, out)
