@@ -476,7 +476,7 @@ typedef struct {
 } tardis_linear_4bit_desc;
 
 /* y = sigma(sum_G scale_jG sum_(k in G) (q_jk - zero_jG) x_k + b_j) + residual, codes q of 4 bits, 0 .. 15.  Products
- * are exact, sums fp32 (of code and zero point each: tokens up to 2^115), scales applied to the sums of their groups; a
+ * are exact, sums fp32 (of code and zero point each: tokens up to 2^112), scales applied to the sums of their groups; a
  * token with an infinity or a NaN is NaN.  x, sigma, residual and y as tardis_linear's.
  *   work      as tardis_linear's: tardis_linear_4bit_workspace says how much the call can use (0 for many). */
 tardis_status_t tardis_linear_4bit(const tardis_linear_4bit_desc* desc, const void* x, int64_t n, int64_t x_pitch, const void* residual,
