@@ -249,12 +249,14 @@ tardis_status_t td_rms_norm(const void* x, int64_t n, int64_t d, int64_t x_pitch
     p.norm = norm;
     p.inv_d = 1.0 / (double)d;
     p.eps = (double)eps;
-    // Pieces of a thread and wavefronts of a row: as few wavefronts as keep 4096 of them busy (16 for each CU), since what they share of a row goes by
-    // way of barriers; fewer rows are divided among more.  More than 4 pieces only for rows that need them (8192 rows of 4096 in bf16 to e4m3, us: 8 pieces
-    // 55.8, 4 and 1 49)
+    // Pieces of a thread and wavefronts of a row.  Outputs in bf16 and fp32: as many wavefronts as the row divides into (8192 rows of 4096 in bf16, us: 1, 2 and 4
+    // pieces of a thread 45.2, 47.2, 51.7).  Codes, for which the wavefronts wait for one another a second time: as few as keep 4096 of them
+    // busy (16 for each CU), so that fewer rows are divided among more (8192 rows of 4096 54.4, 46.4, 48.0 and with 8 pieces 55.8; 2048 of 16384 21.2, 23.9, 21.5; 2048 of
+    // 4096 15.0, 13.9, 13.4).  8 pieces only for rows that need them.
+    const bool codes = out_dtype == TARDIS_FP8_E4M3;
     int each = (int64_t)(p.units + 255) / 256 <= 16 ? 4 : 8;
     auto waves_of = [&](int u) { return (int64_t)(p.units + 64 * u - 1) / (64 * u); };
-    while (each > 1 && n * waves_of(each) < kBusy && waves_of(each / 2) <= 16) each /= 2;
+    while (each > 1 && (!codes || n * waves_of(each) < kBusy) && waves_of(each / 2) <= 16) each /= 2;
     p.waves = (int)std::min<int64_t>(16, waves_of(each));
     if (waves_of(each) > 16) each = 0;                                 // (rows that do not fit into registers)
     const int rows = std::max(1, 4 / p.waves), threads = 64 * p.waves * rows;

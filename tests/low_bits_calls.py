@@ -40,4 +40,5 @@ for _group, _words in ((32, 1), (64, 2), (128, 4)):
 
 # rows, columns, type of x, type of y
 NORM = [(f"rms_norm_kernel {name} {out} {each}", n, d, dtype, out) for name, dtype in (("bf16", BF16), ("f32", F32)) for out in (F32, BF16, FP8_E4M3)
-        for each, n, d in ((1, 3, 4096), (2, 1021, 5137), (4, 2048, 4096), (8, 300, 40000), (0, 2, 70001))]
+        for each, n, d in ((1, 3, 4096), (2, 1021, 5137) if out == FP8_E4M3 else (2, 50, 16000), (4, 2048, 4096) if out == FP8_E4M3 else (4, 20, 30001), (8, 300, 40000),
+                           (0, 2, 70001))]
