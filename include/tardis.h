@@ -430,8 +430,8 @@ typedef struct {
  *   sum       n x d, dtype: s, rounded; or NULL.  May be residual itself, or x itself where x_pitch = d.
  *   y         n x d, out_dtype; must not overlap the others.
  *   scales    n floats, where out_dtype is TARDIS_FP8_E4M3 (else NULL): a row's y is its codes
- *             times scale = max(max |y| / 448, 2^-126), codes rounded to nearest even.  A NaN in y is a NaN
- *             code and counts for nothing in the scale; with an infinite y the scale is infinite, codes are 0 and NaN. */
+ *             times scale = max(max |y| / 448, 2^-126), codes y / scale (in fp32) rounded to nearest
+ *             even.  A NaN in y is a NaN code and counts for nothing in the scale; with an infinite y the scale is infinite, codes are 0 and NaN. */
 tardis_status_t tardis_rms_norm(const tardis_norm_desc* desc, const void* x, int64_t n, int64_t x_pitch, const void* residual,
                                 void* sum, void* y, float* scales, void* stream);
 

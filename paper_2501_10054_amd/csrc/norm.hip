@@ -71,13 +71,34 @@ template <bool F32> __device__ __forceinline__ void store8(unsigned char* to, co
     }
 }
 
-__device__ __forceinline__ void store_codes(unsigned char* to, const float (&v)[8], float inverse, uint32_t left) {
+// A row's scale as it divides: 1 / scale in two parts, of which v (high + low) rounded once is v / scale rounded (high alone is off by a rounding, and where
+// values have few bits that turns ties: of 960 rows of 4096 in bf16 52 had codes one step off).  Scales above 2^64 are made smaller by 2^64 first, with v, so that
+// the low part has its bits.  It costs four instructions an element of a kernel that waits for memory.
+struct CodeScale {
+    float up, high, low;
+};
+__device__ __forceinline__ CodeScale code_scale(float scale) {
+    CodeScale c;
+    c.up = scale > 0x1p64f ? 0x1p-64f : 1.0f;
+    const float s = scale * c.up;
+    c.high = 1.0f / s;
+    c.low = c.high > 0.0f ? fmaf(-s, c.high, 1.0f) * c.high : 0.0f;   // (an infinite scale: codes 0, and NaN of what is infinite)
+    return c;
+}
+
+__device__ __forceinline__ void store_codes(unsigned char* to, const float (&v)[8], const CodeScale& by, uint32_t left) {
     norm_u32x2_t c = {0, 0};
+    float q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float u = v[i] * by.up;
+        q[i] = copysignf(fmaf(u, by.high, u * by.low), u);   // (zeros keep their sign)
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         int w = 0;
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h] * inverse, v[4 * h + 1] * inverse, w, false);
-        w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2] * inverse, v[4 * h + 3] * inverse, w, true);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h], q[4 * h + 1], w, false);
+        w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * h + 2], q[4 * h + 3], w, true);
         c[h] = (uint32_t)w;
     }
     if (left >= 8) {
@@ -193,7 +214,8 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs p) {
             __syncthreads();
             for (int w = 0; w < p.waves; ++w) top = fmaxf(top, tops[wave - mine + w]);
         }
-        const float scale = fmaxf(top / kE4m3Most, kLeastScale), inverse = 1.0f / scale;
+        const float scale = fmaxf(top / kE4m3Most, kLeastScale);
+        const CodeScale by = code_scale(scale);
         if (there && mine == 0 && lane == 0) p.scales[row] = scale;
         over_row([&](uint32_t u, int i) {
             const uint32_t left = p.d - u * 8u;
@@ -202,7 +224,7 @@ __global__ void __launch_bounds__(1024) rms_norm_kernel(NormArgs p) {
                 if (p.sum) store8<sizeof(T) == 4>(p.sum + (at + (int64_t)u * 8) * sizeof(T), s[i], left);
                 weighed(u, s[i], r);
             }
-            store_codes(p.y + at + (int64_t)u * 8, s[i], inverse, left);
+            store_codes(p.y + at + (int64_t)u * 8, s[i], by, left);
         });
     } else {
         over_row([&](uint32_t u, int i) {
