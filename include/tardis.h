@@ -439,19 +439,22 @@ tardis_status_t tardis_rms_norm(const tardis_norm_desc* desc, const void* x, int
 tardis_status_t tardis_fp8_rows(const void* x, int64_t n, int64_t d, int64_t x_pitch, int32_t dtype, void* codes, float* scales,
                                 void* stream);
 
+enum { TARDIS_FP8_EXACT = 0x100 };   /* added to tardis_linear_fp8_desc.act */
+
 typedef struct {
     int64_t n_in;            /* 1 .. 2^22 */
     int64_t n_out;           /* 1 .. 2^22 */
     int32_t out_dtype;       /* of b, the residual and y: TARDIS_F32 or TARDIS_BF16 */
-    int32_t act;             /* tardis_act_t */
+    int32_t act;             /* tardis_act_t, or with TARDIS_FP8_EXACT added */
     const void* W;           /* n_out x n_in e4m3 codes */
     const float* W_scales;   /* n_out, or NULL for ones */
     const void* b;           /* n_out, or NULL for zero */
 } tardis_linear_fp8_desc;
 
 /* y = sigma(x W^T + b) + residual with x and W in e4m3, a scale for each row of either: scales are applied to
- * the fp32 sums (the token's first).  With out_dtype TARDIS_F32 products are exact and sums as tardis_linear's; with
- * TARDIS_BF16 the matrix instructions of larger calls drop of each product what is below 2^-13 of the largest of the 32 that
+ * the fp32 sums (the token's first).  With out_dtype TARDIS_F32, or with TARDIS_FP8_EXACT, products are exact and sums as
+ * tardis_linear's.  Otherwise
+ * the matrix instructions of larger calls drop of each product what is below 2^-13 of the largest of the 32 that
  * they add up first (of sums of many products 1e-4 of the root of their squares).  sigma, residual, y and work as tardis_linear's.
  *   x         n rows of n_in codes, x_pitch >= n_in bytes apart.
  *   x_scales  n floats, or NULL for ones. */

@@ -670,7 +670,7 @@ tardis_status_t check_layer(int64_t n_in, int64_t n_out, int32_t out_dtype, int3
 }
 tardis_status_t check_fp8(const tardis_linear_fp8_desc* d, int64_t n, int64_t pitch) {
     if (!d || !d->W || !aligned_to(d->W_scales, 4)) return TARDIS_ERR_INVALID_ARG;
-    TD_TRY(check_layer(d->n_in, d->n_out, d->out_dtype, d->act, d->b));
+    TD_TRY(check_layer(d->n_in, d->n_out, d->out_dtype, d->act & ~TARDIS_FP8_EXACT, d->b));
     return rows_fit(n, n > 1 ? pitch : 0) && pitch >= d->n_in ? TARDIS_OK : TARDIS_ERR_SHAPE;
 }
 tardis_status_t check_4bit(const tardis_linear_4bit_desc* d, int64_t n, int64_t pitch) {

@@ -22,7 +22,7 @@ struct LinearArgs {
 };
 
 struct e4m3_t { uint8_t code; };
-struct e4m3_near_t { uint8_t code; };             // multiplied by the faster instruction, for outputs in bf16
+struct e4m3_near_t { uint8_t code; };             // multiplied by the faster instruction, for outputs in bf16 whose sums need not be exact
 
 constexpr int kActGelu16 = 4;                     // behind tardis_act_t's: GELU for outputs in bf16 without a residual
 constexpr uint32_t kNowhere = 0xe0000000u;        // an offset past the end of any operand that is loaded by offsets
@@ -44,13 +44,13 @@ constexpr bool linear_has(int es, bool direct, bool grouped, int shape) {
     if (es == 2) return !(grouped && shape == 8);
     return !(shape == 2 || (shape >= 4 && shape <= 9) || shape == 12 || (grouped && (shape == 10 || shape == 15)));
 }
-// of e4m3; from kLinearNearFp8 on with outputs in bf16 by the faster instruction, which takes two half-lines of each wavefront
+// of e4m3; from kLinearNearFp8 on, unless sums are to be exact, by the faster instruction, which takes two half-lines of each wavefront
 constexpr LinearShape kLinearShapeFp8[] = {{16, 16, 512}, {16, 32, 512}, {16, 16, 1024}, {32, 32, 512}, {64, 64, 256}, {128, 128, 256}, {128, 128, 128}, {64, 64, 128},
                                            {32, 64, 512}, {64, 128, 256}, {128, 64, 256}};
 constexpr int kLinearNearFp8 = 3;
 constexpr int kLinearShapesFp8 = sizeof(kLinearShapeFp8) / sizeof(LinearShape);
-// (with outputs in fp32, where all codes are multiplied as bf16, the rule has no use for some of them)
-constexpr bool linear_has_fp8(bool direct, bool out_f32, int shape) { return !direct || !out_f32 || !(shape == 3 || shape == 5 || shape == 9 || shape == 10); }
+// (where all codes are multiplied as bf16 the rule has no use for some of them)
+constexpr bool linear_has_fp8(bool direct, bool near, int shape) { return !direct || near || !(shape == 3 || shape == 5 || shape == 9 || shape == 10); }
 constexpr LinearShape kLinearStagedFp8[] = {{16, 16, 512}, {32, 32, 256}, {64, 64, 128}, {128, 128, 128}};
 constexpr int kLinearStagedShapesFp8 = sizeof(kLinearStagedFp8) / sizeof(LinearShape);
 // of linear_quad_kernel (bf16, rows in whole pieces)
@@ -72,5 +72,5 @@ void td_linear_launch_bf16(const LinearArgs& p, bool grouped, bool direct, int s
 tardis_status_t td_linear_init_fp8_quad();
 void td_linear_launch_fp8_quad(const LinearArgs& p, int shape, int blocks, hipStream_t s);
 tardis_status_t td_linear_init_fp8();
-void td_linear_launch_fp8(const LinearArgs& p, bool direct, int shape, int blocks, hipStream_t s);
+void td_linear_launch_fp8(const LinearArgs& p, bool direct, bool near, int shape, int blocks, hipStream_t s);
 void td_linear_launch_f32(const LinearArgs& p, bool grouped, bool direct, int shape, int blocks, hipStream_t s);

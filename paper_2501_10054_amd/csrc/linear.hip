@@ -115,16 +115,17 @@ constexpr Rate kRateStaged[] = {{2, 0.246f, 0.231f, 4.77f, 3.34f}, {1, 0.389f, 0
                                 {2, 0.228f, 0.214f, 4.34f, 2.79f}, {1, 0.560f, 0.560f, 7.05f, 2.77f}};
 constexpr Rate kRateStagedF32[] = {{2, 0.104f, 0.250f, 4.45f, 4.01f}, {1, 0.377f, 0.377f, 4.45f, 4.01f}, {2, 0.053f, 0.305f, 4.21f, 4.46f},
                                    {2, 0.556f, 0.550f, 4.53f, 5.00f}, {1, 2.042f, 2.042f, 6.55f, 4.71f}};
-// (e4m3, outputs in bf16 and in fp32: 323 and 234 measurements of 15 products each, 3.1 and 1.1 % more than the best)
+// (e4m3, by the faster instruction and with exact sums: 323 and 234 measurements of 15 products each, 3.1 and 1.1 % more than the best; exact ones with outputs in
+// fp32; of rows through registers no measurements but estimates)
 constexpr Rate kRateFp8[] = {{2, 0.254f, 0.139f, 5.95f, 4.70f}, {3, 0.399f, 0.332f, 4.72f, 3.75f}, {1, 0.382f, 0.350f, 4.64f, 3.47f}, {1, 0.337f, 0.337f, 5.22f, 4.14f},
                              {1, 0.469f, 0.350f, 4.93f, 3.65f}, {1, 1.231f, 0.350f, 5.55f, 2.71f}, {3, 0.784f, 0.450f, 8.51f, 3.86f}, {3, 0.541f, 0.180f, 5.28f, 3.44f},
                              {1, 0.606f, 0.350f, 5.12f, 3.70f}, {2, 0.400f, 0.665f, 9.00f, 4.88f}, {1, 0.495f, 0.709f, 5.36f, 3.32f},
                              {1, 0.691f, 0.350f, 8.92f, 3.16f}};
-constexpr Rate kRateFp8F32[] = {{2, 0.271f, 0.271f, 4.83f, 4.60f}, {3, 0.438f, 0.343f, 4.78f, 4.04f}, {1, 0.280f, 0.280f, 4.98f, 3.63f}, {},
+constexpr Rate kRateFp8Exact[] = {{2, 0.271f, 0.271f, 4.83f, 4.60f}, {3, 0.438f, 0.343f, 4.78f, 4.04f}, {1, 0.280f, 0.280f, 4.98f, 3.63f}, {},
                                 {1, 0.647f, 0.350f, 5.48f, 3.08f}, {}, {3, 0.822f, 0.757f, 10.05f, 3.36f}, {3, 0.597f, 0.223f, 5.65f, 3.39f},
                                 {1, 0.756f, 0.415f, 5.19f, 3.54f}, {}, {}};
 constexpr Rate kRateStagedFp8[] = {{2, 0.320f, 0.300f, 6.30f, 3.30f}, {2, 0.230f, 0.300f, 5.90f, 3.50f}, {2, 0.300f, 0.280f, 5.90f, 2.80f}, {1, 0.750f, 0.750f, 8.50f, 2.60f}};
-static_assert(sizeof(kRateFp8) / sizeof(Rate) == kLinearShapesFp8 + kLinearQuadsFp8 && sizeof(kRateFp8F32) / sizeof(Rate) == kLinearShapesFp8 && sizeof(kRateStagedFp8) / sizeof(Rate) == kLinearStagedShapesFp8, "a rate for each tile");
+static_assert(sizeof(kRateFp8) / sizeof(Rate) == kLinearShapesFp8 + kLinearQuadsFp8 && sizeof(kRateFp8Exact) / sizeof(Rate) == kLinearShapesFp8 && sizeof(kRateStagedFp8) / sizeof(Rate) == kLinearStagedShapesFp8, "a rate for each tile");
 static_assert(sizeof(kRate) / sizeof(Rate) == kLinearShapes + kLinearQuads && sizeof(kRateF32) / sizeof(Rate) == kLinearShapes &&
               sizeof(kRateStaged) / sizeof(Rate) == kLinearStagedShapes && sizeof(kRateStagedF32) / sizeof(Rate) == kLinearStagedShapes, "a rate for each tile");
 // one more launch (2.5 on the GPU; callers that are not a graph wait for their host); a byte copied, of partial sums and outputs joined; sigma of an element of a tile, of eight wavefronts and of four
@@ -138,6 +139,7 @@ struct Call {
     int es, eo, act;
     int experts;                                   // 0: one matrix
     bool gather, x_aligned, W_aligned;             // (addresses)
+    bool near;                                     // e4m3: by the faster instruction where tiles are large
 };
 struct Plan {
     bool direct, pack_x, pack_W;
@@ -148,15 +150,14 @@ struct Plan {
 
 // (es: bytes of an element - 1 e4m3, 2 bf16, 4 fp32)
 int shapes_below_quads(bool direct, int es) { return es == 1 ? (direct ? kLinearShapesFp8 : kLinearStagedShapesFp8) : direct ? kLinearShapes : kLinearStagedShapes; }
-// (e4m3: with outputs in bf16)
-int shapes_of(bool direct, int es, int eo) { return shapes_below_quads(direct, es) + (!direct || es == 4 ? 0 : es == 2 ? kLinearQuads : eo == 2 ? kLinearQuadsFp8 : 0); }
+int shapes_of(bool direct, int es, bool near) { return shapes_below_quads(direct, es) + (!direct || es == 4 ? 0 : es == 2 ? kLinearQuads : near ? kLinearQuadsFp8 : 0); }
 bool is_quad(bool direct, int es, int s) { return direct && s >= shapes_below_quads(direct, es); }
 const LinearShape& shape_of(bool direct, int es, int s) {
     if (is_quad(direct, es, s)) return (es == 1 ? kLinearQuadFp8 : kLinearQuad)[s - shapes_below_quads(direct, es)];
     return es == 1 ? (direct ? kLinearShapeFp8[s] : kLinearStagedFp8[s]) : direct ? kLinearShape[s] : kLinearStaged[s];
 }
-const Rate& rate_of(bool direct, int es, int eo, int s) {
-    if (es == 1) return !direct ? kRateStagedFp8[s] : eo == 2 ? kRateFp8[s] : kRateFp8F32[s];
+const Rate& rate_of(bool direct, int es, bool near, int s) {
+    if (es == 1) return !direct ? kRateStagedFp8[s] : near ? kRateFp8[s] : kRateFp8Exact[s];
     return direct ? (es == 2 ? kRate[s] : kRateF32[s]) : es == 2 ? kRateStaged[s] : kRateStagedF32[s];
 }
 
@@ -195,11 +196,11 @@ Plan make_plan(const Call& c, int64_t room) {
             if (p.pitch >= 1 << 23 || p.k >= 1 << 23 || (c.gather && (c.x_rows - 1) * p.pitch + p.k >= (int64_t)kNowhere)) continue;
         }
         if (p.at_part > room) continue;
-        for (int s = 0; s < shapes_of(p.direct, c.es, c.eo); ++s) {
+        for (int s = 0; s < shapes_of(p.direct, c.es, c.near); ++s) {
             const bool quad = is_quad(p.direct, c.es, s);
-            if (!quad && !(c.es == 1 ? linear_has_fp8(p.direct, c.eo == 4, s) : linear_has(c.es, p.direct, c.experts > 0, s))) continue;
+            if (!quad && !(c.es == 1 ? linear_has_fp8(p.direct, c.near, s) : linear_has(c.es, p.direct, c.experts > 0, s))) continue;
             const LinearShape& t = shape_of(p.direct, c.es, s);
-            const Rate& r = rate_of(p.direct, c.es, c.eo, s);
+            const Rate& r = rate_of(p.direct, c.es, c.near, s);
             const int64_t slices = (p.k + t.slice - 1) / t.slice, tiles_n = (c.N + t.n - 1) / t.n;
             const double tiles_m = c.experts ? hit * std::max(1.0, (double)c.M / hit / t.m + 0.5) : (double)((c.M + t.m - 1) / t.m);
             if (most_tiles_m(c, quad, t) * tiles_n >= kMostTiles) continue;
@@ -244,7 +245,7 @@ const Plan& plan_of(const Call& c, int64_t room) {
     Kept& k = kept[h >> 58];
     const Call& o = k.call;
     const bool same = o.M == c.M && o.N == c.N && o.x_rows == c.x_rows && o.k == c.k && o.pitch == c.pitch && o.es == c.es && o.eo == c.eo && o.act == c.act &&
-                      o.experts == c.experts && o.gather == c.gather && o.x_aligned == c.x_aligned && o.W_aligned == c.W_aligned && k.room == room;
+                      o.experts == c.experts && o.gather == c.gather && o.x_aligned == c.x_aligned && o.W_aligned == c.W_aligned && o.near == c.near && k.room == room;
     if (!same) k = {c, room, make_plan(c, room)};
     return k.plan;
 }
@@ -291,7 +292,7 @@ tardis_status_t run(LinearArgs p, const Call& c, void* work, int64_t work_bytes,
     }
     const int blocks = (int)((tiles + 7) / 8 * 8);
     if (fp8 && quad) td_linear_launch_fp8_quad(q, plan.shape - kLinearShapesFp8, blocks, s);
-    else if (fp8) td_linear_launch_fp8(q, plan.direct, plan.shape, blocks, s);
+    else if (fp8) td_linear_launch_fp8(q, plan.direct, c.near, plan.shape, blocks, s);
     else if (quad) td_linear_launch_quad(q, grouped, plan.shape - kLinearShapes, blocks, s);
     else if (f32) td_linear_launch_f32(q, grouped, plan.direct, plan.shape, blocks, s);
     else td_linear_launch_bf16(q, grouped, plan.direct, plan.shape, blocks, s);
@@ -322,12 +323,15 @@ Call call_of(const tardis_linear_desc* d, int64_t experts, const void* x, int64_
     const int64_t es = (int64_t)td_elem_size(d->dtype);
     if (x_rows == 1) x_pitch = d->n_in;            // (of one row there is none, and none that is too long)
     return {rows, d->n_out, x_rows, d->n_in * es, x_pitch * es, (int)es, (int)td_elem_size(d->out_dtype), d->act, (int)experts, gather,
-            is_aligned16(x), is_aligned16(d->W)};
+            is_aligned16(x), is_aligned16(d->W), false};
 }
+
+int act_of(const tardis_linear_fp8_desc* d) { return d->act & ~TARDIS_FP8_EXACT; }
 
 Call call_of(const tardis_linear_fp8_desc* d, const void* x, int64_t n, int64_t x_pitch) {
     if (n == 1) x_pitch = d->n_in;
-    return {n, d->n_out, n, d->n_in, x_pitch, 1, (int)td_elem_size(d->out_dtype), d->act, 0, false, is_aligned16(x), is_aligned16(d->W)};
+    return {n, d->n_out, n, d->n_in, x_pitch, 1, (int)td_elem_size(d->out_dtype), act_of(d), 0, false, is_aligned16(x), is_aligned16(d->W),
+            d->out_dtype == TARDIS_BF16 && !(d->act & TARDIS_FP8_EXACT)};
 }
 
 constexpr int64_t kAnyRoom = (int64_t)1 << 62;
@@ -372,7 +376,7 @@ tardis_status_t td_linear_fp8(const tardis_linear_fp8_desc* d, const void* x, co
     p.n = p.x_rows = n;
     p.N = d->n_out;
     p.k = (uint32_t)d->n_in;
-    p.act = d->act == TARDIS_ACT_GELU_ERF && d->out_dtype == TARDIS_BF16 && !residual ? kActGelu16 : d->act;
+    p.act = act_of(d) == TARDIS_ACT_GELU_ERF && d->out_dtype == TARDIS_BF16 && !residual ? kActGelu16 : act_of(d);
     p.out_f32 = d->out_dtype == TARDIS_F32;
     p.x_scales = x_scales;
     p.W_scales = d->W_scales;

@@ -10,14 +10,14 @@ __global__ void __launch_bounds__(64 * WM * WN * WK, 2) linear_fp8_kernel(Linear
 }
 
 // f(element type, direct, row and column blocks of a wavefront, grid of wavefronts, wavefronts and half-lines of each in K, slices in LDS)
-template <typename F> void for_fp8_shape(bool direct, int shape, bool out_f32, F f) {
+template <typename F> void for_fp8_shape(bool direct, int shape, bool near, F f) {
     auto use = [&](auto number, auto d, auto... tile) {
         constexpr int s = decltype(number)::value;
         constexpr bool DIRECT = decltype(d)::value;
         if constexpr (DIRECT && s >= kLinearNearFp8) {
-            if (!out_f32) return f(e4m3_near_t{}, d, tile...);
+            if (near) return f(e4m3_near_t{}, d, tile...);
         }
-        if constexpr (linear_has_fp8(DIRECT, DIRECT && s >= kLinearNearFp8, s)) f(e4m3_t{}, d, tile...);
+        if constexpr (linear_has_fp8(DIRECT, !DIRECT || s < kLinearNearFp8, s)) f(e4m3_t{}, d, tile...);
     };
     if (direct) {
         switch (shape) {
@@ -51,8 +51,8 @@ tardis_status_t td_linear_init_fp8() {
         bool ok = true;
         for (int direct = 0; direct < 2; ++direct)
             for (int shape = 0; shape < (direct ? kLinearShapesFp8 : kLinearStagedShapesFp8); ++shape)
-                for (int out_f32 = 0; out_f32 < 2; ++out_f32)
-                    for_fp8_shape(direct, shape, out_f32, [&](auto type, auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
+                for (int near = 0; near < 2; ++near)
+                    for_fp8_shape(direct, shape, near, [&](auto type, auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
                         typedef LinearTile<decltype(type), decltype(d)::value, fa, fb, wm, wn, wk, ks, ring> G;
                         const LinearShape& is = direct ? kLinearShapeFp8[shape] : kLinearStagedFp8[shape];
                         ok &= is.m == G::TM && is.n == G::TN && is.slice == G::SL;
@@ -63,8 +63,8 @@ tardis_status_t td_linear_init_fp8() {
     });
 }
 
-void td_linear_launch_fp8(const LinearArgs& p, bool direct, int shape, int blocks, hipStream_t s) {
-    for_fp8_shape(direct, shape, p.out_f32, [&](auto type, auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
+void td_linear_launch_fp8(const LinearArgs& p, bool direct, bool near, int shape, int blocks, hipStream_t s) {
+    for_fp8_shape(direct, shape, near, [&](auto type, auto d, auto fa, auto fb, auto wm, auto wn, auto wk, auto ks, auto ring) {
         typedef LinearTile<decltype(type), decltype(d)::value, fa, fb, wm, wn, wk, ks, ring> G;
         constexpr int bytes = G::kLds, threads = 64 * G::W;
         hipLaunchKernelGGL((linear_fp8_kernel<decltype(type), decltype(d)::value, fa, fb, wm, wn, wk, ks, ring>), dim3((unsigned)blocks), dim3(threads), bytes, s, p);

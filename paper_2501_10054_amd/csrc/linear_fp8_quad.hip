@@ -1,4 +1,4 @@
-// The linear layer's large tiles for x and W in e4m3, outputs in bf16
+// The linear layer's large tiles for x and W in e4m3, outputs in bf16 whose sums need not be exact
 #include "linear_quad.h"
 
 namespace {

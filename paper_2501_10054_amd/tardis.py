@@ -469,6 +469,7 @@ def tardis_moe_combine(z, place, weights, residual=None, out_dtype=None, y=None,
 
 # ---------------------------------------------------------------- norms, layers in 8 and 4 bits
 FP8 = torch.float8_e4m3fn
+FP8_EXACT = 0x100                  # tardis.h's TARDIS_FP8_EXACT
 
 
 def _at(t):
@@ -565,12 +566,13 @@ def _layer_outputs(n, n_out, out_dtype, b, residual, y, x):
     return y
 
 
-def tardis_linear_fp8(x, x_scales, W, W_scales, b=None, act: str = "identity", residual=None, out_dtype=torch.bfloat16, y=None, stream=None):
+def tardis_linear_fp8(x, x_scales, W, W_scales, b=None, act: str = "identity", residual=None, out_dtype=torch.bfloat16, y=None, stream=None,
+                      exact: bool = False):
     """-> n x n_out: act(x W^T + b) + residual with x and W in e4m3, each row with a scale (None: ones).  Rows of x may have a pitch; out_dtype: of b,
-    residual and y."""
+    residual and y.  exact: sums of exact products also for outputs in bf16, which by default are not (tardis.h)."""
     if stream is not None:
         with _on(stream):
-            return tardis_linear_fp8(x, x_scales, W, W_scales, b, act, residual, out_dtype, y)
+            return tardis_linear_fp8(x, x_scales, W, W_scales, b, act, residual, out_dtype, y, exact=exact)
     n_out, n_in = W.shape
     n, pitch = _rows(x, n_in)
     dev = x.get_device()
@@ -578,7 +580,7 @@ def tardis_linear_fp8(x, x_scales, W, W_scales, b=None, act: str = "identity", r
     assert x_scales is None or (x_scales.is_contiguous() and x_scales.dtype == torch.float32 and x_scales.numel() == n and x_scales.get_device() == dev)
     assert W_scales is None or (W_scales.is_contiguous() and W_scales.dtype == torch.float32 and W_scales.numel() == n_out and W_scales.get_device() == dev)
     y = _layer_outputs(n, n_out, out_dtype, b, residual, y, x)
-    out, a, x_at, W_at = _DTYPE_CODE[out_dtype], ACT[act], x.data_ptr(), W.data_ptr()
+    out, a, x_at, W_at = _DTYPE_CODE[out_dtype], ACT[act] | (FP8_EXACT if exact else 0), x.data_ptr(), W.data_ptr()
     desc = tardis_linear_fp8_desc(n_in, n_out, out, a, W_at, _at(W_scales), _at(b))
     bytes_ = _fp8_work_bytes(n_in, n_out, out, a, n, pitch, x_at & 15, W_at & 15)
     work = torch.empty(bytes_, dtype=torch.uint8, device=x.device) if bytes_ else None
