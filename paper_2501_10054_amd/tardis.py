@@ -569,7 +569,7 @@ def _layer_outputs(n, n_out, out_dtype, b, residual, y, x):
 def tardis_linear_fp8(x, x_scales, W, W_scales, b=None, act: str = "identity", residual=None, out_dtype=torch.bfloat16, y=None, stream=None,
                       exact: bool = False):
     """-> n x n_out: act(x W^T + b) + residual with x and W in e4m3, each row with a scale (None: ones).  Rows of x may have a pitch; out_dtype: of b,
-    residual and y.  exact: sums of exact products also for outputs in bf16, which by default are not (tardis.h)."""
+    residual and y.  exact: sums of exact products also for outputs in bf16, which by default lose up to 2^-10 sum |x W| (tardis.h)."""
     if stream is not None:
         with _on(stream):
             return tardis_linear_fp8(x, x_scales, W, W_scales, b, act, residual, out_dtype, y, exact=exact)
