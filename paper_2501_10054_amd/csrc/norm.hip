@@ -273,12 +273,15 @@ tardis_status_t td_rms_norm(const void* x, int64_t n, int64_t d, int64_t x_pitch
     p.eps = (double)eps;
     // Pieces of a thread and wavefronts of a row.  Outputs in bf16 and fp32: as many wavefronts as the row divides into (8192 rows of 4096 in bf16, us: 1, 2 and 4
     // pieces of a thread 45.2, 47.2, 51.7).  Codes, for which the wavefronts wait for one another a second time: as few as keep 4096 of them
-    // busy (16 for each CU), so that fewer rows are divided among more (8192 rows of 4096 54.4, 46.4, 48.0 and with 8 pieces 55.8; 2048 of 16384 21.2, 23.9, 21.5; 2048 of
-    // 4096 15.0, 13.9, 13.4).  8 pieces only for rows that need them.
+    // busy (16 for each CU), so that fewer rows are divided among more (2048 rows of 4096 with residual, us: 1, 2, 4 and 8 pieces 14.3, 13.3, 12.8, 15.6; 1000 of
+    // 11008 17.1, 19.6, 17.2, 20.7); with four times as many rows two pieces in place of four, unless a row then takes more than 8 wavefronts (8192 rows of 4096
+    // 47.1, 44.4, 48.1, 50.3; 4096 of 8192 55.0, 45.0, 47.8, 49.9; 16384 of 4096 95.1, 89.5, 97.4, 110; without residual 2048 of 16384 21.3, 23.1,
+    // 21.2, 22.9).  8 pieces only for rows that need them.
     const bool codes = out_dtype == TARDIS_FP8_E4M3;
     int each = (int64_t)(p.units + 255) / 256 <= 16 ? 4 : 8;
     auto waves_of = [&](int u) { return (int64_t)(p.units + 64 * u - 1) / (64 * u); };
     while (each > 1 && (!codes || n * waves_of(each) < kBusy) && waves_of(each / 2) <= 16) each /= 2;
+    if (codes && each == 4 && n * waves_of(4) >= 4 * kBusy && waves_of(2) <= 8) each = 2;
     p.waves = (int)std::min<int64_t>(16, waves_of(each));
     if (waves_of(each) > 16) each = 0;                                 // (rows that do not fit into registers)
     const int rows = std::max(1, 4 / p.waves), threads = 64 * p.waves * rows;
