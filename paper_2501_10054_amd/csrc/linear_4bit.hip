@@ -4,6 +4,9 @@
 // a word's layout is such that a shift and an and-or make two neighbouring columns at once.  16 + zero is multiplied with the same tokens and taken away
 // again (few tokens: by matrix instructions; many: as a product with the sum of the group's columns), so that a group's accumulator ends with
 // sum (q - zero) x, every product exact; the group's scale goes to that sum.  Tokens in fp32 are three bf16 parts each, which together hold all of their 24 bits.
+// What is raised by 16 is 5 to 10 times what is left of it, and so is its rounding.  Hence every 32 columns' zero points follow their codes into one accumulator, and
+// each part has its own: the head's sums have few bits and round little, the others are 2^8 and 2^16 times smaller (fp32 tokens, groups of 128, up to 16 tokens: error of
+// the outputs 1.3e-7 of their root mean square, median of 3890 calls; with one sum of codes and one of zero points 2.2e-6.  More tokens 3.0e-7; with one sum for all parts 6.6e-7).
 //
 // What bounds it: one token - launch, the way of the first bytes, and 0.5 bytes a weight from HBM (16384 -> 4096: 11.5 us, 34.7 MB; the stream alone takes 5); a
 // prompt - vector instructions beside the matrix cores, of which a group's product needs 8 for each 64 bytes of codes and one for each result
@@ -109,6 +112,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) linear4_kernel(FourArgs p) {
     typedef typename words_of<GW>::type words_t;
     typedef FourBlock<T, RT> S;
     constexpr int D = S::D, KW = S::KW, G = 4 / GW, PARTS = S::PARTS, THREADS = 64 * kWaves;
+    constexpr int SUMS = PARTS > 1 ? PARTS : GW > 1 ? 2 : 1;                            // (independent ones, for the matrix cores)
     extern __shared__ __align__(1024) unsigned char lds[];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), low = lane & 15, high = lane >> 4, kw = wave % KW, rt = wave / KW, n = (int)p.n;
     const int64_t block0 = (int64_t)blockIdx.x * (16 * RT), n0 = block0 + rt * 16;
@@ -230,7 +234,9 @@ __global__ void __launch_bounds__(64 * kWaves, 4) linear4_kernel(FourArgs p) {
                         scale = e[0];
                         less = __builtin_amdgcn_perm(__float_as_uint(e[1]), __float_as_uint(e[1]), 0x03020302u);
                     }
-                    f32x4_t c = {0, 0, 0, 0}, d = {0, 0, 0, 0};
+                    f32x4_t c[SUMS];
+#pragma unroll
+                    for (int i = 0; i < SUMS; ++i) c[i] = f32x4_t{0, 0, 0, 0};
 #pragma unroll
                     for (int s = 0; s < GW; ++s) {
                         uint32_t word;
@@ -240,12 +246,15 @@ __global__ void __launch_bounds__(64 * kWaves, 4) linear4_kernel(FourArgs p) {
 #pragma unroll
                         for (int part = 0; part < PARTS; ++part) {
                             const td_u32x4 x = *reinterpret_cast<const td_u32x4*>(x_at + part * part_pitch + (g * (4 * GW) + s) * 16);
-                            c = mma(x, codes, c);
-                            d = mma(x, td_u32x4{less, less, less, less}, d);
+                            f32x4_t& sum = c[PARTS == 1 ? s % SUMS : part];
+                            sum = mma(x, codes, sum);
+                            sum = mma(x, td_u32x4{less, less, less, less}, sum);
                         }
                     }
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) acc[q] = fmaf(scale, c[q] + d[q], acc[q]);
+                    for (int i = SUMS - 1; i > 0; --i) c[i - 1] += c[i];
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) acc[q] = fmaf(scale, c[0][q], acc[q]);
                 }
             }
         }
@@ -276,7 +285,7 @@ __global__ void __launch_bounds__(64 * kWaves, 4) linear4_kernel(FourArgs p) {
 // ---------------------------------------------------------------- many tokens
 // What the tiles read beside the codes, made by one launch before theirs:
 //   tokens  PARTS parts in bf16, [part][token][units], zeros behind the last column
-//   sums    of every group's columns, [group][sum_pitch]
+//   sums    of every group's columns, [part][group][sum_pitch]
 //   table   of W's scales and zero points, [group][table_pitch] rows: scale and -(16 + zero), in bf16 side by side (of tokens in bf16) or in fp32
 // Groups are as many as whole steps have, those behind the last with scales of 0.
 struct FourTokens {
@@ -332,14 +341,15 @@ __global__ void __launch_bounds__(256) linear4_prepare_kernel(FourTokens p) {
     Token<T> t;
     if (left >= 8) load_token<T>(t, at);
     else load_token_end<T>(t, at, left);
-    double sum = 0.0;
 #pragma unroll
-    for (int i = 0; i < Token<T>::PARTS; ++i)
+    for (int i = 0; i < Token<T>::PARTS; ++i) {
+        double sum = 0.0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) sum += (double)__uint_as_float(t.part[i][q] << 16) + (double)__uint_as_float(t.part[i][q] & 0xffff0000u);
 #pragma unroll
-    for (int o = 1; o < 4 * GW; o *= 2) sum += __shfl_xor(sum, o, 64);
-    if (unit % (4 * GW) == 0) p.sums[(int64_t)(unit / (4 * GW)) * p.sum_pitch + row] = (float)sum;
+        for (int o = 1; o < 4 * GW; o *= 2) sum += __shfl_xor(sum, o, 64);
+        if (unit % (4 * GW) == 0) p.sums[((int64_t)i * p.all_groups + unit / (4 * GW)) * p.sum_pitch + row] = (float)sum;
+    }
 #pragma unroll
     for (int i = 0; i < Token<T>::PARTS; ++i) p.parts[((int64_t)i * p.n + row) * p.units + unit] = t.part[i];
 }
@@ -348,10 +358,11 @@ struct FourTile : LinearArgs {                     // (x: the parts; k: bytes of
     const float* sums;
     const unsigned char* table;
     int64_t sum_pitch, table_pitch;
-    uint32_t groups;
+    uint32_t groups, all_groups;
 };
 
-// D steps in LDS.  The table's and the sums' pieces of 1024 bytes are dealt out to the wavefronts, AUX for each.
+// D steps in LDS.  The table's and (tokens of one part) the sums' pieces of 1024 bytes are dealt out to the wavefronts, AUX for each; parts have their sums with
+// their tokens.
 template <int PARTS, int GW, int FA, int FB, int WN, int D> struct FourTileShape {
     static constexpr int TM = 16 * FA, TN = 16 * FB * WN, G = 4 / GW;
     static constexpr int X = TM * 2 * kStep, CODES = TN * kStep / 2, ROW = PARTS == 1 ? 4 : 8, PIECE = TN * ROW < 1024 ? TN * ROW : 1024;   // (of a group's rows in one load)
@@ -410,11 +421,18 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
     const uint32_t off_sums = high < G && 4 * low < min(b.rows, TM) ? (uint32_t)(high * p.sum_pitch + 4 * low) * 4u : kNowhere;
     const i32x4_t rc = settled(buffer_of(p.W + b.n0 * row_bytes, (uint32_t)rows_w * row_bytes));
     // (live: past the last step nothing is fetched, from empty buffers)
+    auto load_sums = [&](uint32_t step, int part, uint32_t slot, bool live) {
+        i32x4_t r = settled(buffer_of(p.sums + ((int64_t)part * p.all_groups + (int64_t)step * G) * p.sum_pitch + b.first,
+                                      (uint32_t)((G - 1) * p.sum_pitch + p.sum_pitch - b.first) * 4u));
+        r.z = live ? r.z : 0;
+        load_to_lds(base + D * (S::X + S::CODES + S::TABLE) + slot * S::SUMS, off_sums, r, 0);
+    };
     auto load_x = [&](uint32_t step, int part, uint32_t slot, bool live) {
         i32x4_t r = settled(buffer_of(p.x + ((int64_t)part * p.n + b.first) * p.k, (uint32_t)b.rows * p.k));
         r.z = live ? r.z : 0;
 #pragma unroll
         for (int i = 0; i < LX; ++i) load_to_lds(base + slot * S::X + (uint32_t)wave * (S::X / WN) + i * 1024u, off_x[i], r, live ? step * (2 * kStep) : 0u);
+        if (PARTS > 1 && wave == 0) load_sums(step, part, slot, live);
     };
     auto load_codes = [&](uint32_t step, uint32_t slot, bool live) {
         i32x4_t r = rc;
@@ -432,11 +450,8 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
                 rt.z = live ? rt.z : 0;
                 load_to_lds((uint32_t)uniform((int)(base + D * (S::X + S::CODES) + slot * S::TABLE + (uint32_t)piece * 1024u)),
                             group < (uint32_t)G ? group * (uint32_t)p.table_pitch * S::ROW + at : kNowhere, rt, 0);
-            } else {
-                i32x4_t rs = settled(buffer_of(p.sums + (int64_t)step * G * p.sum_pitch + b.first, (uint32_t)((G - 1) * p.sum_pitch + p.sum_pitch - b.first) * 4u));
-                rs.z = live ? rs.z : 0;
-                load_to_lds(base + D * (S::X + S::CODES + S::TABLE) + slot * S::SUMS, off_sums, rs, 0);
-            }
+            } else if (PARTS == 1)
+                load_sums(step, 0, slot, live);
         }
     };
     const Sixteen sixteen;
@@ -445,7 +460,7 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
     for (int i = 0; i < FA; ++i)
 #pragma unroll
         for (int j = 0; j < FB; ++j) acc[i][j] = f32x4_t{0, 0, 0, 0};
-    auto products = [&](uint32_t x_slot, uint32_t slot, bool first_part) {
+    auto products = [&](uint32_t x_slot, uint32_t slot) {
         const unsigned char* from = at_x + x_slot * S::X + low * (2 * kStep);
         const unsigned char* codes_from = at_codes + slot * S::CODES + (wave * FB * 16 + low) * (kStep / 2) + high * (4 * GW);
 #pragma unroll
@@ -456,8 +471,7 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
             for (int i = 0; i < FA; ++i) {
 #pragma unroll
                 for (int s = 0; s < GW; ++s) x[i][s] = *reinterpret_cast<const td_u32x4*>(from + i * 16 * (2 * kStep) + (((g * (4 * GW) + high * GW + s) ^ low) * 16));
-                sum[i] = *reinterpret_cast<const f32x4_t*>(at_sums + slot * S::SUMS + (g * 64 + i * 16 + 4 * high) * 4);
-                if (PARTS > 1 && !first_part) sum[i] = f32x4_t{0, 0, 0, 0};
+                sum[i] = *reinterpret_cast<const f32x4_t*>(at_sums + x_slot * S::SUMS + (g * 64 + i * 16 + 4 * high) * 4);
             }
 #pragma unroll
             for (int j = 0; j < FB; ++j) {
@@ -511,7 +525,7 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
         for (int at = 0; at < b.nk; ++at) {
             arrived();
             load_step(at + D - 1, free_slot);
-            products(slot, slot, true);
+            products(slot, slot);
             free_slot = slot;
             slot = slot + 1 == D ? 0 : slot + 1;
         }
@@ -531,7 +545,7 @@ __global__ void __launch_bounds__(64 * WN, 2) linear4_tile_kernel(FourTile p) {
                 if (part + 1 < PARTS) load_x(step_of(at), part + 1, x_slot ^ 1, true);
                 else if (at + 1 < b.nk) load_x(step_of(at + 1), 0, x_slot ^ 1, true);
                 if (part == 0 && at + 1 < b.nk) load_codes(step_of(at + 1), slot ^ 1, true);
-                products(x_slot, slot, part == 0);
+                products(x_slot, slot);
                 x_slot ^= 1;
             }
         }
@@ -625,7 +639,7 @@ FourPlan plan_four(const tardis_linear_4bit_desc* d, int64_t n, int64_t room) {
     p.sum_pitch = round_up(n, 4);
     p.table_pitch = round_up(d->n_out, 256);
     p.at_sums = round_up((f32 ? 3 : 1) * n * p.units * 16, 256);
-    p.at_table = p.at_sums + round_up(p.all_groups * p.sum_pitch * 4, 256);
+    p.at_table = p.at_sums + round_up((f32 ? 3 : 1) * p.all_groups * p.sum_pitch * 4, 256);
     p.at_part = p.at_table + p.all_groups * p.table_pitch * (f32 ? 8 : 4);
     // (offsets of a tile's rows, of four groups' sums and of the table are 32 bits)
     if (p.units * 16 * 64 >= kNowhere || 4 * p.sum_pitch * 4 >= kNowhere || n * p.units + p.all_groups * p.table_pitch >= kMostThreads || p.at_part > room) return FourPlan{};
@@ -687,6 +701,7 @@ tardis_status_t run_tiles(const tardis_linear_4bit_desc* d, const FourPlan& plan
     p.sum_pitch = plan.sum_pitch;
     p.table_pitch = plan.table_pitch;
     p.groups = t.groups;
+    p.all_groups = t.all_groups;
     FourTile q = p;
     if (plan.splits > 1) {
         q.part = reinterpret_cast<float*>(work + plan.at_part);
