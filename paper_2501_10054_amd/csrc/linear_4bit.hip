@@ -8,9 +8,9 @@
 // each part has its own: the head's sums have few bits and round little, the others are 2^8 and 2^16 times smaller (fp32 tokens, groups of 128, up to 16 tokens: error of
 // the outputs 1.3e-7 of their root mean square, median of 3890 calls; with one sum of codes and one of zero points 2.2e-6.  More tokens 3.0e-7; with one sum for all parts 6.6e-7).
 //
-// What bounds it: one token - launch, the way of the first bytes, and 0.5 bytes a weight from HBM (16384 -> 4096: 11.5 us, 34.7 MB; the stream alone takes 5); a
+// What bounds it: one token - launch, the way of the first bytes, and 0.5 bytes a weight from HBM (16384 -> 4096: 13.7 us, 34.7 MB, and from caches 11.7; the stream alone takes 7 and 5); a
 // prompt - vector instructions beside the matrix cores, of which a group's product needs 8 for each 64 bytes of codes and one for each result
-// (2048 tokens 4096 -> 16384: 306 us, 0.9 PFLOP/s; 512 tokens 84 us).
+// (2048 tokens 4096 -> 16384: 314 us, 0.88 PFLOP/s; 512 tokens 91 us).
 #include <algorithm>
 
 #include "linear_tile.h"

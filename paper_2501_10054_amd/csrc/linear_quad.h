@@ -11,7 +11,7 @@
 //
 // e4m3: a slice has the same bytes and takes the same cycles for twice as many products: an instruction of 32 x 32 results takes 64 bytes of K, in four gaps
 // of 16 cycles, from two pieces of a row in a lane.  (One of 16 x 16 takes 128 bytes, both halves of a slice, for which there are not registers twice.)
-// Lane l has row l % 32 of two row blocks, pieces 2 (l / 32) and the next of half a slice.  2048 x 4096 -> 16384 on 256 x 128 tiles: 134 us, 2.05 PFLOP/s; the
+// Lane l has row l % 32 of two row blocks, pieces 2 (l / 32) and the next of half a slice.  2048 x 4096 -> 16384 on 256 x 128 tiles, weights from HBM: 134 us, 2.05 PFLOP/s; the
 // matrix cores work 57 % of the cycles of a slice, the rest waits for the slices' way from L2 (39 bytes a ns and CU).
 #pragma once
 #include "linear_tile.h"
