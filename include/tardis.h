@@ -424,7 +424,7 @@ typedef struct {
 } tardis_norm_desc;
 
 /* s = x + residual (fp32);  y = s / sqrt(mean(s^2) + eps) * weight, rounded once; the squares are summed
- * in 64 bits (no row of finite values overflows).  y of a row of zeros is 0 also with eps = 0.
+ * in 64 bits (no row of finite s overflows).  y of a row of zeros is 0 also with eps = 0.
  *   x         n rows of d values, x_pitch >= d values apart.
  *   residual  n x d, dtype, or NULL.
  *   sum       n x d, dtype: s, rounded; or NULL.  May be residual itself, or x itself where x_pitch = d.
